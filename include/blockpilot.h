@@ -19,6 +19,8 @@
  * the final hidden states of the verified and drafted positions instead of their logits.
  * bp_tau_select evaluates Appendix A's acceptance-length model for a batch of requests.
  * bp_verify_commit rolls the KV lengths back to the accepted prefix on the device, closing the loop.
+ * bp_qk_norm_rope and bp_qkv_append take a layer's projections to normed, rotated queries and keys, the latter into the
+ * paged cache; bp_chunk_attention_paged attends for a prompt, or a chunk of one, over it: the prefill before the loop.
  *
  * Conventions shared by every entry point
  *   - Pointers to tensors are DEVICE pointers (cudaMalloc / torch allocations), owned by
@@ -149,6 +151,79 @@ BP_API int bp_kv_append(void* k_cache, void* v_cache, const void* k_new, const v
                         const int32_t* cu_kv, const int32_t* block_table, int pages_per_seq, int page_size,
                         int num_pages, int num_seqs, int total_new, int num_kv_heads, int head_dim, int dtype,
                         void* stream);
+
+/* ---------------------------------------------------------------------------------
+ * Queries and keys normed and rotated in one pass: what stands between a layer's projections and its attention.  For
+ * every token and head, a vector x of head_dim elements:
+ *
+ *   y = w * x / sqrt(mean(x^2) + eps)            (a NULL weight: y = x, no norm)
+ *   the i-th of rotary_dim / 2 pairs (a, b) of y:  a' = a c - b s,  b' = b c + a s,
+ *     c = cos_sin[pos][i],  s = cos_sin[pos][rotary_dim / 2 + i],  pos = positions[token]
+ *   pair i: elements i and rotary_dim / 2 + i (interleaved 0), or 2 i and 2 i + 1 (interleaved 1); the elements from
+ *   rotary_dim on are not turned.  fp32 inside, rounded once to dtype.
+ *
+ *   q, q_out  rows of [num_q_heads][head_dim] dtype, *_stride elements from a token to the next; k, k_out with
+ *             num_kv_heads likewise (either may have 0 heads and NULL pointers).  An output may be its own input, with
+ *             the same stride; other overlaps are not allowed.
+ *   q_weight, k_weight  [head_dim] dtype, or NULL
+ *   cos_sin   [max_pos][rotary_dim] fp32; rotary_dim 0: no rotation, cos_sin may be NULL
+ *   positions [num_tokens] int32, each in [0, max_pos) (else BP_ERR_DEVICE_FLAG; that token is not written)
+ * Limits: dtype BP_BF16 or BP_F32; head_dim a multiple of 8, at most 256; rotary_dim a multiple of 16; pointers and
+ * strides 16-byte aligned.  workspace: at least 256 bytes (the error word).
+ * ------------------------------------------------------------------------------- */
+BP_API int bp_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride, void* q_out,
+                           int64_t q_out_stride, void* k_out, int64_t k_out_stride, const void* q_weight,
+                           const void* k_weight, const float* cos_sin, const int32_t* positions, int num_tokens,
+                           int num_q_heads, int num_kv_heads, int head_dim, int rotary_dim, int max_pos,
+                           int interleaved, int dtype, float eps, void* workspace, size_t workspace_bytes,
+                           void* stream);
+
+/* The same on the way into a paged cache: the queries go to q_out, the normed and rotated keys and the values as they
+ * are to their sequences' pages, in one launch.  New token i of sequence s, row cu_new[s] + i of q, k_new and v_new,
+ * becomes key L_s + i, L_s = (cu_kv[s+1]-cu_kv[s]) - (cu_new[s+1]-cu_new[s]) -- cu_kv counts the new tokens, as in
+ * bp_kv_append.
+ *   q, k_new, v_new  as q and k above, each with its stride: views of one packed projection, or tensors of their own.
+ *             num_q_heads 0 (q, q_out NULL): keys and values only
+ *   positions NULL: a token's position is its key's number, L_s + i
+ *   k_cache, v_cache  [num_pages*page_size][num_kv_heads][head_dim] dtype; block_table, pages_per_seq, page_size as
+ *             bp_block_attention_paged; the pages that receive the rows must be in the block table
+ * A token whose key has no place there (a page id outside [0, num_pages), a key past the table) sets
+ * BP_ERR_DEVICE_FLAG and is not written.  Rows from cu_new[num_seqs] on are padding: nothing is written for them. */
+BP_API int bp_qkv_append(const void* q, int64_t q_stride, const void* k_new, int64_t k_stride, const void* v_new,
+                         int64_t v_stride, void* q_out, int64_t q_out_stride, const void* q_weight,
+                         const void* k_weight, const float* cos_sin, const int32_t* positions, void* k_cache,
+                         void* v_cache, const int32_t* cu_new, const int32_t* cu_kv, const int32_t* block_table,
+                         int pages_per_seq, int page_size, int num_pages, int num_seqs, int total_new, int num_q_heads,
+                         int num_kv_heads, int head_dim, int rotary_dim, int max_pos, int interleaved, int dtype,
+                         float eps, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------
+ * Attention of chunks of new tokens over a paged KV cache: prompts, whole or in chunks, and decoding sequences (chunks
+ * of one token) in one call; bp_block_attention_paged without its bound on a block.  New token i of sequence s, with
+ * B_s new tokens and n_s = cu_kv[s+1]-cu_kv[s] keys (the new tokens' own counted), stands at p = n_s - B_s + i and sees
+ *
+ *   keys lo <= j < hi,  hi = p + 1 (BP_MASK_CAUSAL_BLOCK) or n_s (BP_MASK_BIDIR_BLOCK),
+ *                       lo = max(0, p + 1 - window), or 0 where window is 0
+ *   O[i,h] = sum_j softmax_j(scale * <q_{i,h}, k_{j,h/g}>) v_{j,h/g},  g = num_q_heads / num_kv_heads
+ *
+ * A row that sees no key (a sequence with fewer keys than new tokens has such rows) gets 0, and -inf in lse.
+ *   q        rows of [num_q_heads][head_dim] bf16, q_stride elements from a token to the next; o [total_q][num_q_heads]
+ *            [head_dim] bf16; lse [total_q][num_q_heads] fp32 or NULL
+ *   cu_q, cu_kv, block_table, pages_per_seq, page_size, k_cache, v_cache  as bp_block_attention_paged, but of a page's
+ *            rows only those of the sequence's keys have to be finite: what is behind them is not used
+ *   max_q_len, max_kv_len  host-side upper bounds of B_s and n_s; pages_per_seq * page_size >= max_kv_len
+ * Limits: dtype BP_BF16, head_dim 64 or 128, g <= 128, num_pages * page_size < 2^31.  A page id outside [0, num_pages)
+ * or a sequence past its table row sets BP_ERR_DEVICE_FLAG.  The result does not depend on scheduling.
+ * ------------------------------------------------------------------------------- */
+BP_API size_t bp_chunk_attention_workspace_size(int num_seqs, int total_q, int num_q_heads, int num_kv_heads,
+                                                int head_dim);
+BP_API int bp_chunk_attention_paged(const void* q, int64_t q_stride, const void* k_cache, const void* v_cache, void* o,
+                                    float* lse, const int32_t* cu_q, const int32_t* cu_kv, const int32_t* block_table,
+                                    int pages_per_seq, int page_size, int num_pages, int num_seqs, int total_q,
+                                    int max_q_len, int max_kv_len, int num_q_heads, int num_kv_heads, int head_dim,
+                                    int dtype, int mask, int window, float softmax_scale, void* workspace,
+                                    size_t workspace_bytes, void* stream);
+
 /* ---------------------------------------------------------------------------------
  * Lossless speculative acceptance over the full vocabulary.  Figure 1 caption (the
  * target accepts the longest consistent prefix of the drafted block), Section 1 and

@@ -14,12 +14,16 @@ from ._binding import (  # noqa: F401
     block_attention,
     block_attention_paged,
     block_attention_workspace_size,
+    chunk_attention_paged,
+    chunk_attention_workspace_size,
     get_status,
     kv_append,
     library_path,
     load,
     policy_select,
     policy_select_workspace_size,
+    qk_norm_rope,
+    qkv_append,
     spec_accept,
     spec_accept_workspace_size,
     tau_select,

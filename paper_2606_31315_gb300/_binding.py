@@ -65,6 +65,17 @@ def load():
     lib.bp_block_attention_paged.restype = i32
     lib.bp_kv_append.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, i32, vp]
     lib.bp_kv_append.restype = i32
+    lib.bp_qk_norm_rope.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32,
+                                    i32, i32, f32, vp, sz, vp]
+    lib.bp_qk_norm_rope.restype = i32
+    lib.bp_qkv_append.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32,
+                                  i32, i32, i32, i32, i32, i32, i32, i32, i32, f32, vp, sz, vp]
+    lib.bp_qkv_append.restype = i32
+    lib.bp_chunk_attention_workspace_size.argtypes = [i32, i32, i32, i32, i32]
+    lib.bp_chunk_attention_workspace_size.restype = sz
+    lib.bp_chunk_attention_paged.argtypes = [vp, i64, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32,
+                                             i32, i32, i32, i32, i32, i32, f32, vp, sz, vp]
+    lib.bp_chunk_attention_paged.restype = i32
     lib.bp_spec_accept_workspace_size.argtypes = [i32, i32, i32]
     lib.bp_spec_accept_workspace_size.restype = sz
     lib.bp_spec_accept.argtypes = [vp, vp, vp, vp, i32, i32, i32, f32, vp, vp, vp, vp, vp, vp, sz, vp]
@@ -196,6 +207,182 @@ def kv_append(k_cache, v_cache, k_new, v_new, cu_new, cu_kv, block_table, page_s
                           _ptr(block_table), block_table.shape[1], int(page_size), k_cache.shape[0] // int(page_size),
                           cu_new.numel() - 1, total_new, hkv, d, dtype, _stream(stream))
     _check(rc, "bp_kv_append")
+
+
+# --------------------------------------------------------------------------- prefill
+def _heads(name: str, t, dtype):
+    """A [tokens, heads, head_dim] CUDA tensor whose heads are contiguous; its stride from a token to the next."""
+    if not (t.is_cuda and t.dim() == 3 and t.dtype == dtype):
+        raise ValueError(f"{name} must be a [tokens, heads, head_dim] CUDA tensor of the others' dtype")
+    token, head, elt = t.stride()
+    heads, dim = t.shape[1:]
+    if (elt != 1 and dim > 1) or (head != dim and heads > 1):
+        raise ValueError(f"{name}: the heads of a token must be contiguous")
+    return token if t.shape[0] > 1 else heads * dim
+
+
+def _rotation(cos_sin, weights, dtype, dim):
+    """(table, max_pos, rotary_dim) of a cos_sin tensor or None; checks the norms' weights."""
+    _cuda("q_weight k_weight", *weights)
+    for w in weights:
+        if w is not None and (w.dtype != dtype or w.numel() != dim):
+            raise ValueError("q_weight, k_weight must be [head_dim] tensors of the inputs' dtype")
+    if cos_sin is None:
+        return None, 0, 0
+    _cuda("cos_sin", cos_sin)
+    if cos_sin.dtype != torch.float32 or cos_sin.dim() != 2:
+        raise ValueError("cos_sin must be a [max_pos, rotary_dim] fp32 tensor")
+    return cos_sin.data_ptr(), *cos_sin.shape
+
+
+def _int32(names, *tensors):
+    _cuda(names, *tensors)
+    for t in tensors:
+        if t is not None and t.dtype != torch.int32:
+            raise ValueError(f"{names.split()[[x is t for x in tensors].index(True)]} must be int32")
+
+
+def qk_norm_rope(q, k, cos_sin, positions, q_weight=None, k_weight=None, interleaved: bool = False, eps: float = 1e-6,
+                 q_out=None, k_out=None, ws=None, stream=None):
+    """Every head of q and k normed (with a weight) and rotated to its token's position; see ``bp_qk_norm_rope``.
+
+    q [T, Hq, D], k [T, Hkv, D] (bf16 or fp32, any stride between tokens; either may be None), cos_sin fp32
+    [max_pos, rotary_dim] or None, positions int32 [T].  q_out / k_out may be q / k.  Returns (q_out, k_out)."""
+    lib = load()
+    x = q if q is not None else k
+    dtype = _DTYPES.get(x.dtype)
+    if dtype is None:
+        raise ValueError("q and k must be bf16 or fp32")
+    t, _, d = x.shape
+    for name, y in (("q", q), ("k", k)):
+        if y is not None and (y.shape[0] != t or y.shape[2] != d):
+            raise ValueError("q and k must have the same tokens and head_dim")
+    table, max_pos, rotary = _rotation(cos_sin, (q_weight, k_weight), x.dtype, d)
+    _int32("positions", positions)
+    if positions.numel() != t:
+        raise ValueError("positions must hold one position for each token")
+    hq = hk = qs = ks = qos = kos = 0
+    if q is not None:
+        hq, qs = q.shape[1], _heads("q", q, x.dtype)
+        if q_out is None:
+            q_out = torch.empty((t, hq, d), dtype=q.dtype, device=q.device)
+        elif q_out.shape != q.shape:
+            raise ValueError("q_out must have q's shape")
+        qos = _heads("q_out", q_out, x.dtype)
+    if k is not None:
+        hk, ks = k.shape[1], _heads("k", k, x.dtype)
+        if k_out is None:
+            k_out = torch.empty((t, hk, d), dtype=k.dtype, device=k.device)
+        elif k_out.shape != k.shape:
+            raise ValueError("k_out must have k's shape")
+        kos = _heads("k_out", k_out, x.dtype)
+    if ws is None:
+        ws = workspace(256, x.device)
+    rc = lib.bp_qk_norm_rope(_ptr(q), qs, _ptr(k), ks, _ptr(q_out), qos, _ptr(k_out), kos, _ptr(q_weight),
+                             _ptr(k_weight), table, _ptr(positions), t, hq, hk, d, rotary, max_pos, int(interleaved),
+                             dtype, eps, _ptr(ws), ws.numel(), _stream(stream))
+    _check(rc, "bp_qk_norm_rope")
+    return q_out, k_out
+
+
+def qkv_append(qkv, k_cache, v_cache, cu_new, cu_kv, block_table, page_size: int, cos_sin, positions=None,
+               q_weight=None, k_weight=None, interleaved: bool = False, eps: float = 1e-6, q_out=None, ws=None,
+               stream=None):
+    """Queries normed and rotated; keys likewise and values into their pages; see ``bp_qkv_append``.
+
+    qkv: a packed projection [T, Hq + 2 Hkv, D] (a token's query heads, then its key and its value heads; any stride
+    between tokens), or a tuple (q or None, k, v) of such tensors of their own.  k_cache / v_cache
+    [num_pages * page_size, Hkv, D]; cu_new / cu_kv int32 [S+1], block_table int32 [S, pages_per_seq] on the device.
+    Returns the queries [T, Hq, D] (None without query heads)."""
+    lib = load()
+    rows, hkv, d = k_cache.shape
+    _cuda("k_cache v_cache", k_cache, v_cache)
+    _int32("cu_new cu_kv block_table positions", cu_new, cu_kv, block_table, positions)
+    dt = k_cache.dtype
+    dtype = _DTYPES.get(dt)
+    if dtype is None or v_cache.dtype != dt or v_cache.shape != k_cache.shape:
+        raise ValueError("the caches must share one shape and dtype (bf16 or fp32)")
+    if torch.is_tensor(qkv):
+        qs = ks = vs = _heads("qkv", qkv, dt)
+        t, heads, dim = qkv.shape
+        hq = heads - 2 * hkv
+        if hq < 0:
+            raise ValueError("qkv holds fewer heads than the caches' keys and values have")
+        qp = qkv.data_ptr()
+        kp = qp + hq * d * qkv.element_size()
+        vp = kp + hkv * d * qkv.element_size()
+    else:
+        q, k, v = qkv
+        ks, vs = _heads("k", k, dt), _heads("v", v, dt)
+        t, heads, dim = k.shape
+        if heads != hkv or v.shape != k.shape or (q is not None and (q.shape[0] != t or q.shape[2] != dim)):
+            raise ValueError("q, k and v must have the same tokens and head_dim, k and v the caches' heads")
+        hq, qs = (0, 0) if q is None else (q.shape[1], _heads("q", q, dt))
+        qp, kp, vp = _ptr(q), k.data_ptr(), v.data_ptr()
+    if dim != d:
+        raise ValueError("the new rows must have the caches' head_dim")
+    if positions is not None and positions.numel() != t:
+        raise ValueError("positions must hold one position for each token")
+    table, max_pos, rotary = _rotation(cos_sin, (q_weight, k_weight), dt, d)
+    qos = 0
+    if hq == 0:
+        qp = q_out = None
+    elif q_out is None:
+        q_out = torch.empty((t, hq, d), dtype=dt, device=k_cache.device)
+    if q_out is not None:
+        if q_out.shape != (t, hq, d):
+            raise ValueError("q_out must be [tokens, query heads, head_dim]")
+        qos = _heads("q_out", q_out, dt)
+    if ws is None:
+        ws = workspace(256, k_cache.device)
+    rc = lib.bp_qkv_append(qp, qs, kp, ks, vp, vs, _ptr(q_out), qos, _ptr(q_weight), _ptr(k_weight), table,
+                           _ptr(positions), _ptr(k_cache), _ptr(v_cache), _ptr(cu_new), _ptr(cu_kv), _ptr(block_table),
+                           block_table.shape[1], int(page_size), rows // int(page_size), cu_new.numel() - 1, t, hq,
+                           hkv, d, rotary, max_pos, int(interleaved), dtype, eps, _ptr(ws), ws.numel(), _stream(stream))
+    _check(rc, "bp_qkv_append")
+    return q_out
+
+
+def chunk_attention_workspace_size(num_seqs, total_q, num_q_heads, num_kv_heads, head_dim) -> int:
+    return int(load().bp_chunk_attention_workspace_size(num_seqs, total_q, num_q_heads, num_kv_heads, head_dim))
+
+
+def chunk_attention_paged(q, k_cache, v_cache, cu_q, cu_kv, block_table, page_size: int, max_q_len: int,
+                          max_kv_len: int, mask: int = MASK_CAUSAL, window: int = 0, softmax_scale: float = 0.0,
+                          out=None, lse=None, ws=None, stream=None):
+    """Attention of chunks of new tokens (a prompt, a chunk of one, or one token) over a paged cache; see
+    ``bp_chunk_attention_paged``.
+
+    q [total_q, Hq, D] bf16 (any stride between tokens), D 64 or 128; k_cache / v_cache [num_pages * page_size, Hkv,
+    D]; cu_q / cu_kv int32 [S+1], block_table int32 [S, pages_per_seq] on the device.  window > 0: a token sees the
+    `window` keys that end with its own.  Returns (o, lse_or_None)."""
+    lib = load()
+    dt = q.dtype
+    stride = _heads("q", q, dt)
+    _cuda("k_cache v_cache out lse", k_cache, v_cache, out, lse)
+    _int32("cu_q cu_kv block_table", cu_q, cu_kv, block_table)
+    dtype = _DTYPES.get(dt)
+    if dtype is None or k_cache.dtype != dt or v_cache.dtype != dt:
+        raise ValueError("q, k_cache, v_cache must share one dtype")
+    t, hq, d = q.shape
+    rows, hkv, dk = k_cache.shape
+    if dk != d or v_cache.shape != k_cache.shape:
+        raise ValueError("q and the caches must share one head_dim, the caches one shape")
+    if out is None:
+        out = torch.empty((t, hq, d), dtype=dt, device=q.device)
+    elif out.shape != q.shape or out.dtype != dt:
+        raise ValueError("out must have q's shape and dtype")
+    if lse is not None and (lse.dtype != torch.float32 or lse.numel() != t * hq):
+        raise ValueError("lse must be fp32 [tokens, query heads]")
+    s = cu_q.numel() - 1
+    if ws is None:
+        ws = workspace(lib.bp_chunk_attention_workspace_size(s, t, hq, hkv, d), q.device)
+    rc = lib.bp_chunk_attention_paged(q.data_ptr(), stride, _ptr(k_cache), _ptr(v_cache), _ptr(out), _ptr(lse),
+                                      _ptr(cu_q), _ptr(cu_kv), _ptr(block_table), block_table.shape[1], int(page_size),
+                                      rows // int(page_size), s, t, int(max_q_len), int(max_kv_len), hq, hkv, d, dtype,
+                                      int(mask), int(window), softmax_scale, _ptr(ws), ws.numel(), _stream(stream))
+    _check(rc, "bp_chunk_attention_paged")
+    return out, lse
 
 
 # --------------------------------------------------------------------------- acceptance

@@ -221,6 +221,138 @@ int bp_kv_append(void* k_cache, void* v_cache, const void* k_new, const void* v_
     return rc;
 }
 
+size_t bp_chunk_attention_workspace_size(int num_seqs, int total_q, int num_q_heads, int num_kv_heads, int head_dim) {
+    (void)num_seqs; (void)total_q; (void)num_q_heads; (void)num_kv_heads;
+    if (head_dim != 64 && head_dim != 128) return sizeof(WorkspaceHeader);
+    return sizeof(WorkspaceHeader) + chunk_attention_scratch_bytes(head_dim);
+}
+
+int bp_chunk_attention_paged(const void* q, int64_t q_stride, const void* k_cache, const void* v_cache, void* o,
+                             float* lse, const int32_t* cu_q, const int32_t* cu_kv, const int32_t* block_table,
+                             int pages_per_seq, int page_size, int num_pages, int num_seqs, int total_q, int max_q_len,
+                             int max_kv_len, int num_q_heads, int num_kv_heads, int head_dim, int dtype, int mask,
+                             int window, float softmax_scale, void* workspace, size_t workspace_bytes, void* stream) {
+    if (num_seqs < 0 || total_q < 0 || max_q_len < 0 || max_kv_len < 0 || window < 0) return BP_ERR_INVALID_ARG;
+    if (num_seqs == 0 || total_q == 0) return BP_OK;  // nothing to compute
+    if (!q || !k_cache || !v_cache || !o || !cu_q || !cu_kv || !block_table) return BP_ERR_INVALID_ARG;
+    if (num_q_heads < 1 || num_kv_heads < 1 || head_dim < 1 || num_q_heads % num_kv_heads != 0)
+        return BP_ERR_INVALID_ARG;
+    if (mask != BP_MASK_CAUSAL_BLOCK && mask != BP_MASK_BIDIR_BLOCK) return BP_ERR_INVALID_ARG;
+    if (dtype != BP_F32 && dtype != BP_BF16) return BP_ERR_INVALID_ARG;
+    if (!(softmax_scale >= 0.f) || isinf(softmax_scale)) return BP_ERR_INVALID_ARG;
+    if (pages_per_seq < 1 || num_pages < 1 || !valid_page_size(page_size)) return BP_ERR_INVALID_ARG;
+    if ((long long)pages_per_seq * page_size < max_kv_len || (long long)num_pages * page_size > INT32_MAX)
+        return BP_ERR_INVALID_ARG;
+    if (q_stride < (int64_t)num_q_heads * head_dim) return BP_ERR_INVALID_ARG;
+    if (dtype != BP_BF16 || (head_dim != 64 && head_dim != 128)) return BP_ERR_UNSUPPORTED;  // tensor-core path only
+    if (num_q_heads / num_kv_heads > 128) return BP_ERR_UNSUPPORTED;  // a token's heads of one KV head fit one tile
+    if (!aligned(q, 16) || q_stride % 8 != 0 || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(o, 16))
+        return BP_ERR_INVALID_ARG;
+    int rc = check_workspace(workspace, workspace_bytes,
+                             bp_chunk_attention_workspace_size(num_seqs, total_q, num_q_heads, num_kv_heads, head_dim));
+    if (rc != BP_OK) return rc;
+    DeviceInfo dev;
+    if ((rc = device_info(&dev)) != BP_OK) return rc;
+    ChunkAttentionArgs a;
+    a.q = q; a.q_stride = q_stride; a.k_cache = k_cache; a.v_cache = v_cache; a.o = o; a.lse = lse;
+    a.cu_q = cu_q; a.cu_kv = cu_kv; a.block_table = block_table;
+    a.pages_per_seq = pages_per_seq; a.page_size = page_size; a.num_pages = num_pages;
+    a.num_seqs = num_seqs; a.total_q = total_q;
+    a.num_q_heads = num_q_heads; a.num_kv_heads = num_kv_heads; a.head_dim = head_dim;
+    a.mask = mask; a.window = window;
+    a.scale = softmax_scale == 0.f ? 1.f / sqrtf((float)head_dim) : softmax_scale;
+    a.scratch = scratch(workspace);
+    a.err_word = err_word(workspace);
+    rc = launch_chunk_attention(a, dev, static_cast<cudaStream_t>(stream));
+    if (rc == BP_ERR_CUDA) cudaGetLastError();
+    return rc;
+}
+
+namespace {
+// What bp_qk_norm_rope and bp_qkv_append check alike; rows: the strides between tokens of what they read and write.
+int check_rope(int head_dim, int rotary_dim, int max_pos, const float* cos_sin, int interleaved, int dtype, float eps,
+               const void* q_weight, const void* k_weight) {
+    if (head_dim < 1 || rotary_dim < 0 || rotary_dim > head_dim || (rotary_dim > 0 && (!cos_sin || max_pos < 1)))
+        return BP_ERR_INVALID_ARG;
+    if (interleaved != 0 && interleaved != 1) return BP_ERR_INVALID_ARG;
+    if (dtype != BP_F32 && dtype != BP_BF16) return BP_ERR_INVALID_ARG;
+    if (!(eps >= 0.f) || isinf(eps)) return BP_ERR_INVALID_ARG;
+    if (head_dim % 8 != 0 || head_dim > 256 || rotary_dim % 16 != 0) return BP_ERR_UNSUPPORTED;
+    if ((rotary_dim > 0 && !aligned(cos_sin, 16)) || !aligned(q_weight, 16) || !aligned(k_weight, 16))
+        return BP_ERR_INVALID_ARG;
+    return BP_OK;
+}
+// A tensor of `heads` heads of `head_dim` a token, `stride` elements from a token to the next; none where heads is 0.
+bool valid_heads(const void* p, int64_t stride, int heads, int head_dim, int dtype) {
+    if (heads == 0) return true;
+    return p && aligned(p, 16) && stride >= (int64_t)heads * head_dim && stride % (dtype == BP_BF16 ? 8 : 4) == 0;
+}
+}  // namespace
+
+int bp_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride, void* q_out, int64_t q_out_stride,
+                    void* k_out, int64_t k_out_stride, const void* q_weight, const void* k_weight, const float* cos_sin,
+                    const int32_t* positions, int num_tokens, int num_q_heads, int num_kv_heads, int head_dim,
+                    int rotary_dim, int max_pos, int interleaved, int dtype, float eps, void* workspace,
+                    size_t workspace_bytes, void* stream) {
+    if (num_tokens < 0 || num_q_heads < 0 || num_kv_heads < 0) return BP_ERR_INVALID_ARG;
+    if (num_tokens == 0 || (num_q_heads == 0 && num_kv_heads == 0)) return BP_OK;  // nothing to compute
+    int rc = check_rope(head_dim, rotary_dim, max_pos, cos_sin, interleaved, dtype, eps, q_weight, k_weight);
+    if (rc != BP_OK) return rc;
+    if (!positions || !valid_heads(q, q_stride, num_q_heads, head_dim, dtype) ||
+        !valid_heads(k, k_stride, num_kv_heads, head_dim, dtype) ||
+        !valid_heads(q_out, q_out_stride, num_q_heads, head_dim, dtype) ||
+        !valid_heads(k_out, k_out_stride, num_kv_heads, head_dim, dtype))
+        return BP_ERR_INVALID_ARG;
+    if ((rc = check_workspace(workspace, workspace_bytes, sizeof(WorkspaceHeader))) != BP_OK) return rc;
+    DeviceInfo dev;
+    if ((rc = device_info(&dev)) != BP_OK) return rc;
+    RopeArgs a = {};
+    a.q = q; a.k = k; a.q_stride = q_stride; a.k_stride = k_stride;
+    a.q_out = q_out; a.k_out = k_out; a.q_out_stride = q_out_stride; a.k_out_stride = k_out_stride;
+    a.q_weight = q_weight; a.k_weight = k_weight; a.cos_sin = cos_sin; a.positions = positions;
+    a.num_tokens = num_tokens; a.num_q_heads = num_q_heads; a.num_kv_heads = num_kv_heads; a.head_dim = head_dim;
+    a.rotary_dim = rotary_dim; a.max_pos = max_pos; a.interleaved = interleaved; a.dtype = dtype; a.eps = eps;
+    a.err_word = err_word(workspace);
+    rc = launch_rope(a, dev, static_cast<cudaStream_t>(stream));
+    if (rc == BP_ERR_CUDA) cudaGetLastError();
+    return rc;
+}
+
+int bp_qkv_append(const void* q, int64_t q_stride, const void* k_new, int64_t k_stride, const void* v_new,
+                  int64_t v_stride, void* q_out, int64_t q_out_stride, const void* q_weight, const void* k_weight,
+                  const float* cos_sin, const int32_t* positions, void* k_cache, void* v_cache, const int32_t* cu_new,
+                  const int32_t* cu_kv, const int32_t* block_table, int pages_per_seq, int page_size, int num_pages,
+                  int num_seqs, int total_new, int num_q_heads, int num_kv_heads, int head_dim, int rotary_dim,
+                  int max_pos, int interleaved, int dtype, float eps, void* workspace, size_t workspace_bytes,
+                  void* stream) {
+    if (num_seqs < 0 || total_new < 0 || num_q_heads < 0) return BP_ERR_INVALID_ARG;
+    if (num_seqs == 0 || total_new == 0) return BP_OK;  // nothing to append
+    int rc = check_rope(head_dim, rotary_dim, max_pos, cos_sin, interleaved, dtype, eps, q_weight, k_weight);
+    if (rc != BP_OK) return rc;
+    if (!k_cache || !v_cache || !cu_new || !cu_kv || !block_table) return BP_ERR_INVALID_ARG;
+    if (num_kv_heads < 1 || pages_per_seq < 1 || num_pages < 1 || !valid_page_size(page_size)) return BP_ERR_INVALID_ARG;
+    if ((long long)num_pages * page_size > INT32_MAX) return BP_ERR_INVALID_ARG;
+    if (!valid_heads(q, q_stride, num_q_heads, head_dim, dtype) || !valid_heads(k_new, k_stride, num_kv_heads, head_dim, dtype) ||
+        !valid_heads(v_new, v_stride, num_kv_heads, head_dim, dtype) ||
+        !valid_heads(q_out, q_out_stride, num_q_heads, head_dim, dtype) || !aligned(k_cache, 16) || !aligned(v_cache, 16))
+        return BP_ERR_INVALID_ARG;
+    if ((rc = check_workspace(workspace, workspace_bytes, sizeof(WorkspaceHeader))) != BP_OK) return rc;
+    DeviceInfo dev;
+    if ((rc = device_info(&dev)) != BP_OK) return rc;
+    RopeArgs a = {};
+    a.q = q; a.k = k_new; a.v = v_new; a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
+    a.q_out = q_out; a.q_out_stride = q_out_stride;
+    a.q_weight = q_weight; a.k_weight = k_weight; a.cos_sin = cos_sin; a.positions = positions;
+    a.num_tokens = total_new; a.num_q_heads = num_q_heads; a.num_kv_heads = num_kv_heads; a.head_dim = head_dim;
+    a.rotary_dim = rotary_dim; a.max_pos = max_pos; a.interleaved = interleaved; a.dtype = dtype; a.eps = eps;
+    a.k_cache = k_cache; a.v_cache = v_cache; a.cu_new = cu_new; a.cu_kv = cu_kv; a.block_table = block_table;
+    a.pages_per_seq = pages_per_seq; a.page_size = page_size; a.num_pages = num_pages; a.num_seqs = num_seqs;
+    a.err_word = err_word(workspace);
+    rc = launch_rope(a, dev, static_cast<cudaStream_t>(stream));
+    if (rc == BP_ERR_CUDA) cudaGetLastError();
+    return rc;
+}
+
 size_t bp_spec_accept_workspace_size(int num_seqs, int total_draft, int vocab) {
     if (num_seqs < 0 || total_draft < 0 || vocab < 1) return 0;
     const size_t s = accept_scratch_bytes(num_seqs, total_draft, vocab);

@@ -1,0 +1,753 @@
+// Attention of chunks of new tokens over a paged KV cache: the prefill of prompts, whole or in chunks, and decoding
+// sequences in the same call.
+//
+//   O_i = sum_j softmax_j(scale <q_i, k_j>) v_j   over lo_i <= j < hi_i
+//
+// with p_i = n - B + i the position of new token i among its sequence's n keys, hi_i = p_i + 1 (causal) or n, lo_i =
+// p_i + 1 - window or 0.  A row that sees no key is 0, its log-sum-exp -inf.
+//
+//   * The G = Hq / Hkv query heads of a KV head are rows of one tile, token-major: floor(128 / G) tokens are an M = 128
+//     tile, two tiles are a work tile that reads every K/V tile once.  Each of the two has a softmax warpgroup (one row
+//     a thread) and its own S, P and O in tensor memory, so that the tensor cores work on one while the other's
+//     weights are formed.  A key tile (128 keys) is S = Q K^T, the online softmax in fp32 (base 2, the accumulator
+//     rescaled only where a row's maximum grew by more than 2^8), P in bf16 over S, O += P V with P from tensor memory.
+//   * The work tiles of all sequences and heads lie on one line, measured in keys; every CTA (one an SM) takes an equal
+//     stretch of it and works through its tiles.  Where a cut falls inside a tile, the two CTAs leave (O, m, l) in the
+//     workspace and a second kernel merges them, in the order of the keys.  So one long context, a ragged batch and a
+//     mix of prompts and decoding sequences all fill the GPU, and no order of arrival enters the result.
+//   * Roles: warps 0-3 and 4-7 softmax, warp 8 TMA producer (its lanes issue the boxes of a tile's pages), warp 9 MMA,
+//     warp 10 clears the rows of V behind a sequence's last key (a page's unused rows may hold anything; their weight
+//     is 0, but 0 times a NaN is none).
+#include <cuda_bf16.h>
+
+#include <algorithm>
+#include <mutex>
+
+#include "common.cuh"
+#include "ptx_sm103.cuh"
+
+namespace bp {
+namespace {
+
+constexpr int kTileM = 128;                      // rows of one stream's query tile
+constexpr int kKeys = 128;                       // keys per K/V tile
+constexpr int kHalfBytes = kKeys * 128;          // 128 rows of 64 columns, 128-byte swizzle
+constexpr int kSoftmaxWarps = 8;
+constexpr int kProducerWarp = 8, kMmaWarp = 9, kTailWarp = 10;
+constexpr int kChunkThreads = 32 * 11;
+constexpr uint32_t kChunkTmem = 512;
+constexpr int kTileCost = 192;                   // a work tile's fixed cost (queries in, output out), in keys
+constexpr int kLeastCost = kTileCost + 2 * kKeys;  // of a CTA's stretch: below it, fewer CTAs take part
+constexpr int kLeastCut = 2;                     // key tiles on either side of a cut
+constexpr int kMaxPages = kKeys / 16;            // pages under a key tile at the smallest page size
+
+template <int D>
+struct Shape {
+    static constexpr int halves = D / 64;
+    static constexpr int tile_bytes = halves * kHalfBytes;      // one K, V or Q tile
+    static constexpr int slots = D == 128 ? 5 : 12;             // ring of K and V tiles
+    static constexpr int smem = (2 + slots) * tile_bytes + 1024;
+    static constexpr uint32_t col_o = 256;                      // O of stream i: columns col_o + i * D
+};
+static_assert(Shape<128>::smem >= tmem_smem_share((int)kChunkTmem, 228 * 1024) &&
+                  Shape<64>::smem >= tmem_smem_share((int)kChunkTmem, 228 * 1024),
+              "leaves no other CTA's tensor memory room");
+
+struct ChunkParams {
+    __nv_bfloat16* o;
+    float* lse;
+    const int32_t* cu_q;
+    const int32_t* cu_kv;
+    const int32_t* block_table;
+    int num_seqs, num_q_heads, num_kv_heads, group;
+    int tokens;  // of one stream's tile: floor(128 / group)
+    int pages_per_seq, page_shift, num_pages;
+    int causal, window;
+    float scale_log2;
+    float* part_o;   // [grid][2][256][D]: the first stretch's part (it began in an earlier CTA) and the last one's
+    float2* part_ml; // [grid][2][256]
+    int4* info;      // [grid]: flags, and the sequence, head and tile that the CTA began and did not end
+    unsigned int* err;
+};
+enum : int { kHasTail = 1, kHasHead = 2, kHeadEnds = 4 };
+
+__device__ __forceinline__ float chunk_exp2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// A sequence of B new tokens that ends n keys; tile t holds the tokens [t * Q, (t + 1) * Q).
+struct Seq {
+    int B, n, Q;
+    int causal, window;
+    __device__ __forceinline__ int tiles() const { return (B + Q - 1) / Q; }
+    __device__ __forceinline__ int hi(int tok_end) const { return causal ? max(0, n - B + tok_end) : n; }  // tok_end <= B
+    __device__ __forceinline__ int lo(int tok) const { return window > 0 ? min(n, max(0, n - B + tok + 1 - window)) : 0; }
+    // sum over t < x of max(0, a + t * Q)
+    __device__ __forceinline__ long long ramp(long long a, int x) const {
+        const int t0 = a >= 0 ? 0 : (int)min((long long)x, (-a + Q - 1) / Q);
+        const long long c = x - t0;
+        return c * a + (long long)Q * (((long long)t0 + x - 1) * c / 2);
+    }
+    // keys (and fixed costs) of the tiles before x, 0 <= x <= tiles(); exact but for a window wider than n at both
+    // ends of a tile, where neighbours agree on the same number all the same
+    __device__ __forceinline__ long long cost(int x) const {
+        long long w = (long long)x * kTileCost;
+        const int T = tiles();
+        if (causal) {
+            w += ramp((long long)n - B + Q, x == T ? x - 1 : x);
+            if (x == T && x > 0) w += n;
+        } else {
+            w += (long long)x * n;
+        }
+        if (window > 0) w -= ramp((long long)n - B + 1 - window, x);
+        return w;
+    }
+};
+
+// A place on the line of all work: key tile j of tile t of head h of sequence s.
+struct Place {
+    int s, h, t, j;
+    __device__ __forceinline__ bool same_tile(const Place& o) const { return s == o.s && h == o.h && t == o.t; }
+};
+
+// One CTA's run of key tiles of one work tile.
+struct Stretch {
+    int s, h, t, q0, B, n;
+    int j0, j1;        // key tiles, counted from key 0
+    bool first, last;  // it holds the work tile's first / last key tile
+};
+
+struct Line {
+    const ChunkParams& p;
+    __device__ __forceinline__ Seq seq(int s) const {
+        Seq q;
+        q.B = __ldg(p.cu_q + s + 1) - __ldg(p.cu_q + s);
+        q.n = __ldg(p.cu_kv + s + 1) - __ldg(p.cu_kv + s);
+        q.Q = 2 * p.tokens;
+        q.causal = p.causal;
+        q.window = p.window;
+        return q;
+    }
+    // key tiles [first, first + count) under tile t
+    __device__ __forceinline__ static void span(const Seq& q, int t, int& first, int& count) {
+        const int lo = q.lo(t * q.Q), hi = q.hi(min(q.B, (t + 1) * q.Q));
+        first = lo / kKeys;
+        count = hi > lo ? (hi + kKeys - 1) / kKeys - first : 0;
+    }
+    // the place at `rem` of sequence s's own part of the line
+    __device__ __forceinline__ Place within(int s, long long rem) const {
+        const Seq q = seq(s);
+        const int T = q.tiles();
+        const long long all = q.cost(T);
+        Place at;
+        at.s = s;
+        at.h = (int)(rem / all);
+        rem -= at.h * all;
+        int lo = 0, hi = T;  // the largest t with cost(t) <= rem
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (q.cost(mid) <= rem) lo = mid; else hi = mid;
+        }
+        at.t = lo;
+        const long long off = rem - q.cost(lo), w = q.cost(lo + 1) - q.cost(lo);
+        int first, count;
+        span(q, lo, first, count);
+        const long long x = off - kTileCost;
+        at.j = x <= 0 ? 0 : (int)min((long long)count, (x + kKeys / 2) / kKeys);
+        if (at.j < kLeastCut || count - at.j < kLeastCut) {
+            at.j = 0;
+            if (2 * off >= w) ++at.t;  // the next tile's start
+        }
+        if (at.t == T) at.t = 0, ++at.h;
+        if (at.h == p.num_kv_heads) at.h = 0, ++at.s;
+        return at;
+    }
+};
+
+// Works through the stretches between two places; every role of the CTA does so by itself.
+struct Walk {
+    const ChunkParams& p;
+    Place at, end;
+    __device__ __forceinline__ bool next(Stretch& g) {
+        const Line line{p};
+        while (at.s < end.s || (at.s == end.s && (at.h < end.h || (at.h == end.h && (at.t < end.t || (at.t == end.t && at.j < end.j)))))) {
+            const Seq q = line.seq(at.s);
+            const int T = q.tiles();
+            if (T <= 0) {
+                at = Place{at.s + 1, 0, 0, 0};
+                continue;
+            }
+            int first, count;
+            Line::span(q, at.t, first, count);
+            const bool cut = at.same_tile(end);
+            g.s = at.s; g.h = at.h; g.t = at.t; g.q0 = __ldg(p.cu_q + at.s); g.B = q.B; g.n = q.n;
+            g.j0 = first + at.j;
+            g.j1 = first + (cut ? end.j : count);
+            g.first = at.j == 0;
+            g.last = !cut;
+            if (cut) {
+                at = end;
+            } else {
+                at.j = 0;
+                if (++at.t == T) {
+                    at.t = 0;
+                    if (++at.h == p.num_kv_heads) at.h = 0, ++at.s;
+                }
+            }
+            return true;
+        }
+        return false;
+    }
+};
+
+// Stream i's key tiles of a stretch: those that some row of its tile sees.
+__device__ __forceinline__ void stream_range(const ChunkParams& p, const Stretch& g, int i, int& a, int& b) {
+    const Seq q{g.B, g.n, 2 * p.tokens, p.causal, p.window};
+    const int tok = g.t * q.Q + i * p.tokens, end = min(g.B, tok + p.tokens);
+    a = b = g.j0;
+    if (tok >= g.B) return;
+    const int lo = q.lo(tok), hi = q.hi(end);
+    if (hi <= lo) return;
+    a = max(g.j0, lo / kKeys);
+    b = min(g.j1, (hi + kKeys - 1) / kKeys);
+    if (b <= a) a = b = g.j0;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kChunkThreads, 1)
+chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap qmap,
+                       const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
+    using S = Shape<D>;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t bar_full[S::slots], bar_empty[S::slots], bar_raw[S::slots];
+    __shared__ uint64_t bar_q_full, bar_q_empty, bar_s[2], bar_p[2], bar_o[2], bar_drain;
+    __shared__ uint32_t tmem_sh;
+    __shared__ Place ends[2];
+    uint8_t* const smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
+    uint8_t* const sQ = smem;                           // two tiles
+    uint8_t* const sKV = smem + 2 * S::tile_bytes;      // the ring
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int G = p.group;
+
+    if (tid == 0) {
+        for (int i = 0; i < S::slots; ++i) {
+            mbar_init(&bar_full[i], 1);
+            mbar_init(&bar_empty[i], 1);
+            mbar_init(&bar_raw[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&bar_s[i], 1);
+            mbar_init(&bar_p[i], 128);
+            mbar_init(&bar_o[i], 1);
+        }
+        mbar_init(&bar_q_full, 1);
+        mbar_init(&bar_q_empty, 1);
+        mbar_init(&bar_drain, 1);
+        fence_mbar_init();
+    }
+    if (warp == kMmaWarp) {
+        tmem_alloc(&tmem_sh, kChunkTmem);
+        tmem_relinquish();
+    }
+    griddep_wait();
+    if (warp == kProducerWarp) {  // this CTA's stretch of the line
+        const Line line{p};
+        auto whole = [&](int s) -> long long {
+            if (s >= p.num_seqs) return 0;
+            const Seq q = line.seq(s);
+            return q.B > 0 ? q.cost(q.tiles()) * p.num_kv_heads : 0;
+        };
+        long long total = 0;
+        for (int base = 0; base < p.num_seqs; base += 32) {
+            long long w = whole(base + lane);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
+            total += w;
+        }
+        const long long parts = min((long long)gridDim.x, max(1ll, total / kLeastCost));
+        const long long c = blockIdx.x;
+        // cuts at total * c / parts
+        const long long step = total / parts, rest = total % parts;
+        const long long cut[2] = {c * step + c * rest / parts, (c + 1) * step + (c + 1) * rest / parts};
+        Place place[2] = {Place{p.num_seqs, 0, 0, 0}, Place{p.num_seqs, 0, 0, 0}};
+        long long before = 0;
+        if (c < parts) {
+            for (int base = 0; base < p.num_seqs; base += 32) {
+                const long long w = whole(base + lane);
+                long long incl = w;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const long long y = __shfl_up_sync(0xffffffffu, incl, o);
+                    if (lane >= o) incl += y;
+                }
+                incl += before;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const unsigned hit = __ballot_sync(0xffffffffu, w > 0 && incl - w <= cut[e] && cut[e] < incl);
+                    if (hit) {
+                        const int l = __ffs(hit) - 1;
+                        place[e] = line.within(base + l, cut[e] - __shfl_sync(0xffffffffu, incl - w, l));
+                    }
+                }
+                before = __shfl_sync(0xffffffffu, incl, 31);
+            }
+        }
+        if (lane < 2) ends[lane] = place[lane];
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    griddep_launch_dependents();
+    const uint32_t tmem = tmem_sh;
+    Walk walk{p, ends[0], ends[1]};
+    Stretch g;
+
+    if (warp == kProducerWarp) {
+        // ================= TMA producer: queries, then K and V tiles through the ring, K first
+        const int rows = min(kKeys, 1 << p.page_shift);  // of a box
+        const int nbox = kKeys / rows;
+        const int box = lane / S::halves, half = lane % S::halves;
+        unsigned x = 0;  // ring position
+        int nq = 0;
+        bool ok = true;
+        unsigned on_raw = 0, raw_phase = 0;  // per slot: whether its last use is on bar_raw; that barrier's uses, mod 2
+        while (ok && walk.next(g)) {
+            const int tok = g.t * 2 * p.tokens;
+            int a0, b0, a1, b1;
+            stream_range(p, g, 0, a0, b0);
+            stream_range(p, g, 1, a1, b1);
+            if (g.j1 <= g.j0) continue;
+            if (nq > 0 && !__all_sync(0xffffffffu, mbar_wait(&bar_q_empty, (nq - 1) & 1, kWaitBudget))) {
+                ok = false;
+                break;
+            }
+            const bool two = tok + p.tokens < g.B;
+            if (lane == 0) {
+                const uint32_t bytes = (uint32_t)(p.tokens * G) * 128 * S::halves;
+                mbar_arrive_expect_tx(&bar_q_full, two ? 2 * bytes : bytes);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (i == 0 || two)
+#pragma unroll
+                        for (int hh = 0; hh < S::halves; ++hh)
+                            tma_load_3d(sQ + i * S::tile_bytes + hh * kHalfBytes, &qmap, &bar_q_full, 64 * hh, g.h * G,
+                                        g.q0 + tok + i * p.tokens);
+            }
+            ++nq;
+            const int32_t* table = p.block_table + (size_t)g.s * p.pages_per_seq;
+            const int last_page = (g.n - 1) >> p.page_shift;
+            // the pool row of this lane's box of key tile j (-1: past the sequence's last page)
+            auto pool_row = [&](int j) {
+                const int key = j * kKeys + box * rows, pg = key >> p.page_shift;
+                if (box >= nbox || pg > last_page) return -1;
+                int id = pg < p.pages_per_seq ? __ldg(table + pg) : -1;
+                if ((unsigned)id >= (unsigned)p.num_pages) {
+                    raise_error(p.err, kErrDeviceArg);
+                    id = 0;
+                }
+                return (id << p.page_shift) + (key & ((1 << p.page_shift) - 1));
+            };
+            int row = pool_row(g.j0);
+            for (int j = g.j0; j < g.j1 && ok; ++j) {
+                const int row_next = j + 1 < g.j1 ? pool_row(j + 1) : -1;
+                const int boxes = min(nbox, ((g.n - j * kKeys) + rows - 1) / rows);
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv, ++x) {
+                    const int slot = x % S::slots;
+                    const unsigned use = x / S::slots;
+                    if (use > 0 && !__all_sync(0xffffffffu, mbar_wait(&bar_empty[slot], (use - 1) & 1, kWaitBudget))) {
+                        ok = false;
+                        break;
+                    }
+                    // a V tile with rows past the last key goes through the tail warp
+                    const bool raw = kv == 1 && (j + 1) * kKeys > g.n;
+                    uint64_t* bar = raw ? &bar_raw[slot] : &bar_full[slot];
+                    on_raw = raw ? on_raw | 1u << slot : on_raw & ~(1u << slot);
+                    if (raw) raw_phase ^= 1u << slot;
+                    if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(boxes * rows) * 128 * S::halves);
+                    __syncwarp();
+                    if (row >= 0)
+                        tma_load_3d(sKV + slot * S::tile_bytes + half * kHalfBytes + box * rows * 128, kv ? &vmap : &kmap,
+                                    bar, 64 * half, g.h, row);
+                }
+                row = row_next;
+            }
+        }
+        if (!ok && lane == 0) raise_error(p.err, kErrTimeout);
+        // no copy may still be in flight when the CTA leaves
+        for (unsigned y = x > (unsigned)S::slots ? x - S::slots : 0; y < x; ++y) {
+            const int slot = y % S::slots;
+            const bool raw = on_raw >> slot & 1;
+            if (!mbar_wait(raw ? &bar_raw[slot] : &bar_full[slot], raw ? ~raw_phase >> slot & 1 : (y / S::slots) & 1, kDrainBudget) && lane == 0)
+                raise_error(p.err, kErrTimeout);
+        }
+        if (nq > 0 && !mbar_wait(&bar_q_full, (nq - 1) & 1, kDrainBudget) && lane == 0) raise_error(p.err, kErrTimeout);
+    } else if (warp == kMmaWarp) {
+        // ================= MMA issuer
+        if (lane == 0) {
+            const uint32_t id_s = idesc_bf16_f32(kTileM, kKeys, false, false);
+            const uint32_t id_o = idesc_bf16_f32(kTileM, D, false, true);
+            const uint32_t q_addr = smem_addr(sQ), kv_addr = smem_addr(sKV);
+            unsigned x0 = 0;  // ring position of the stretch's first K tile
+            unsigned np[2] = {0, 0};
+            int nq = 0;
+            bool ok = true, any = false;
+            while (ok && walk.next(g)) {
+                if (g.j1 <= g.j0) continue;
+                int a[2], b[2];
+                stream_range(p, g, 0, a[0], b[0]);
+                stream_range(p, g, 1, a[1], b[1]);
+                if (!mbar_wait(&bar_q_full, nq & 1, kWaitBudget)) { ok = false; break; }
+                ++nq;
+                any = true;
+                for (int j = g.j0; j <= g.j1 && ok; ++j) {
+                    const unsigned xk = x0 + 2 * (j - g.j0), xv = xk - 1;  // K of tile j, V of tile j - 1
+                    if (j < g.j1 && !mbar_wait(&bar_full[xk % S::slots], (xk / S::slots) & 1, kWaitBudget)) { ok = false; break; }
+                    if (j > g.j0 && !mbar_wait(&bar_full[xv % S::slots], (xv / S::slots) & 1, kWaitBudget)) { ok = false; break; }
+                    tc_fence_after();
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        if (j > a[i] && j <= b[i]) {  // O += P V of tile j - 1
+                            if (!mbar_wait(&bar_p[i], np[i] & 1, kWaitBudget)) { ok = false; break; }
+                            ++np[i];
+                            tc_fence_after();
+                            const uint32_t v_addr = kv_addr + (xv % S::slots) * S::tile_bytes;
+                            // keys past the sequence's last in steps of 16: the tail warp has cleared the rest of a step
+                            const int steps = min(kKeys / 16, (g.n - (j - 1) * kKeys + 15) / 16);
+                            for (int kk = 0; kk < steps; ++kk)
+                                umma_ts(tmem + S::col_o + i * D, tmem + i * 128 + kk * 8,
+                                        smem_desc(v_addr + kk * 2048, kHalfBytes, 1024, kSwizzle128B), id_o,
+                                        (j - 1 > a[i] || kk > 0) ? 1u : 0u);
+                            if (j == b[i]) umma_commit(&bar_o[i]);
+                        }
+                        if (i == 1 && j > g.j0) umma_commit(&bar_empty[xv % S::slots]);
+                        if (j >= a[i] && j < b[i]) {  // S = Q K^T of tile j
+                            const uint32_t k_addr = kv_addr + (xk % S::slots) * S::tile_bytes;
+#pragma unroll
+                            for (int kk = 0; kk < D / 16; ++kk) {
+                                const uint32_t off = (kk >> 2) * kHalfBytes + (kk & 3) * 32;
+                                umma_ss(tmem + i * 128, smem_desc(q_addr + i * S::tile_bytes + off, 16, 1024, kSwizzle128B),
+                                        smem_desc(k_addr + off, 16, 1024, kSwizzle128B), id_s, kk > 0 ? 1u : 0u);
+                            }
+                            umma_commit(&bar_s[i]);
+                        }
+                    }
+                    if (!ok) break;
+                    if (j < g.j1) umma_commit(&bar_empty[xk % S::slots]);
+                    if (j == g.j1 - 1) umma_commit(&bar_q_empty);
+                }
+                x0 += 2 * (g.j1 - g.j0);
+            }
+            if (!ok) raise_error(p.err, kErrTimeout);
+            if (any) {
+                umma_commit(&bar_drain);
+                if (!mbar_wait(&bar_drain, 0, kDrainBudget)) raise_error(p.err, kErrTimeout);
+            }
+        }
+        __syncwarp();
+    } else if (warp == kTailWarp) {
+        // ================= V rows past a sequence's last key; what this CTA leaves to the merge
+        unsigned x0 = 0, phase = 0;
+        int4 left = make_int4(0, 0, 0, 0);
+        bool ok = true;
+        while (walk.next(g)) {
+            if (!g.first) left.x |= kHasHead | (g.last ? kHeadEnds : 0);
+            if (g.first && !g.last) left = make_int4(left.x | kHasTail, g.s, g.h, g.t);
+            if (g.j1 <= g.j0) continue;
+            if (ok && g.j1 * kKeys > g.n) {
+                const unsigned x = x0 + 2 * (g.j1 - 1 - g.j0) + 1;
+                const int slot = x % S::slots;
+                if (!__all_sync(0xffffffffu, mbar_wait(&bar_raw[slot], (phase >> slot) & 1, kWaitBudget))) {
+                    ok = false;
+                } else {
+                    phase ^= 1u << slot;
+                    const int from = g.n - (g.j1 - 1) * kKeys, to = (from + 15) & ~15;  // the rest of a step of 16 keys
+                    for (int c = lane; c < (to - from) * 8 * S::halves; c += 32) {
+                        const int r = c % (8 * S::halves);
+                        *reinterpret_cast<uint4*>(sKV + slot * S::tile_bytes + (r >> 3) * kHalfBytes +
+                                                  (from + c / (8 * S::halves)) * 128 + (r & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bar_full[slot]);
+                }
+            }
+            x0 += 2 * (g.j1 - g.j0);
+        }
+        if (!ok && lane == 0) raise_error(p.err, kErrTimeout);
+        if (lane == 0) p.info[blockIdx.x] = left;
+    } else {
+        // ================= softmax of stream i: one row a thread
+        const int i = warp >> 2, quad = warp & 3;
+        const int r = quad * 32 + lane;
+        const uint32_t s_addr = tmem + (static_cast<uint32_t>(quad * 32) << 16) + i * 128;
+        const uint32_t o_addr = tmem + (static_cast<uint32_t>(quad * 32) << 16) + S::col_o + i * D;
+        const int my_tok = r / G, my_head = r - my_tok * G;
+        unsigned ns = 0, no = 0;
+        bool failed = false;
+        while (!failed && walk.next(g)) {
+            int a, b;
+            stream_range(p, g, i, a, b);
+            const int tok = g.t * 2 * p.tokens + i * p.tokens + my_tok;
+            const bool active = my_tok < p.tokens && tok < g.B;
+            const int pos = g.n - g.B + tok;
+            const int hi = !active ? 0 : p.causal ? max(0, pos + 1) : g.n;
+            const int lo = p.window > 0 ? max(0, pos + 1 - p.window) : 0;
+            float m = -INFINITY, l = 0.f;
+            for (int j = a; j < b; ++j, ++ns) {
+                if (!__all_sync(0xffffffffu, mbar_wait(&bar_s[i], ns & 1, kWaitBudget))) {
+                    failed = true;
+                    break;
+                }
+                tc_fence_after();
+                uint32_t x[4][32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + c * 32, x[c]);
+                tmem_ld_wait();
+                const int from = lo - j * kKeys, to = hi - j * kKeys;  // visible columns
+                if (!__all_sync(0xffffffffu, from <= 0 && to >= kKeys)) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (c * 32 + e < from || c * 32 + e >= to) x[c][e] = 0xff800000u;  // -inf
+                }
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2)
+                        mx[(e >> 1) & 3] = fmaxf(mx[(e >> 1) & 3], fmaxf(__uint_as_float(x[c][e]), __uint_as_float(x[c][e + 1])));
+                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
+                const bool grew = top > m + 8.f;
+                const float alpha = grew ? chunk_exp2(m - top) : 1.f;
+                // (this tile's scores are complete, so the MMAs before them, the last P V among them, are too)
+                if (j > a && __any_sync(0xffffffffu, grew && m != -INFINITY)) {
+#pragma unroll
+                    for (int c = 0; c < D / 16; ++c) {
+                        uint32_t v[16];
+                        tmem_ld16(o_addr + c * 16, v);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * alpha);
+                        tmem_st16(o_addr + c * 16, v);
+                    }
+                }
+                if (grew) {
+                    l *= alpha;
+                    m = top;
+                }
+                const float negm = m == -INFINITY ? 0.f : -m;
+                const uint64_t scale2 = pack_f32x2(p.scale_log2, p.scale_log2), negm2 = pack_f32x2(negm, negm);
+                uint64_t sum2[2] = {0ull, 0ull};
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        float u, w;
+                        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[c][2 * e]), __uint_as_float(x[c][2 * e + 1])), scale2, negm2), u, w);
+                        u = chunk_exp2(u);
+                        w = chunk_exp2(w);
+                        sum2[e & 1] = add_f32x2(sum2[e & 1], pack_f32x2(u, w));
+                        pk[e] = pack_bf16x2(u, w);  // bf16: the type of V, which P multiplies
+                    }
+                    tmem_st16(s_addr + c * 16, pk);
+                }
+                float s0, s1, s2, s3;
+                unpack_f32x2(sum2[0], s0, s1);
+                unpack_f32x2(sum2[1], s2, s3);
+                l += (s0 + s1) + (s2 + s3);
+                tmem_st_wait();
+                tc_fence_before();
+                mbar_arrive(&bar_p[i]);
+            }
+            if (failed) break;
+            if (b > a) {
+                if (!__all_sync(0xffffffffu, mbar_wait(&bar_o[i], no & 1, kWaitBudget))) {
+                    failed = true;
+                    break;
+                }
+                ++no;
+                tc_fence_after();
+            }
+            const bool whole = g.first && g.last;
+            const float inv = whole ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
+            const size_t orow = (size_t)(g.q0 + tok) * p.num_q_heads + g.h * G + my_head;
+            const size_t prow = ((size_t)blockIdx.x * 2 + (g.first ? 1 : 0)) * (2 * kTileM) + i * kTileM + r;
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t v[32];
+                if (b > a) {
+                    tmem_ld32(o_addr + c * 32, v);
+                    tmem_ld_wait();
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] = 0u;
+                }
+                if (active && whole) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) {
+                        uint4 w;
+                        w.x = pack_bf16x2(__uint_as_float(v[e]) * inv, __uint_as_float(v[e + 1]) * inv);
+                        w.y = pack_bf16x2(__uint_as_float(v[e + 2]) * inv, __uint_as_float(v[e + 3]) * inv);
+                        w.z = pack_bf16x2(__uint_as_float(v[e + 4]) * inv, __uint_as_float(v[e + 5]) * inv);
+                        w.w = pack_bf16x2(__uint_as_float(v[e + 6]) * inv, __uint_as_float(v[e + 7]) * inv);
+                        *reinterpret_cast<uint4*>(p.o + orow * D + c * 32 + e) = w;
+                    }
+                } else if (active) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) st_global_f32x8(p.part_o + prow * D + c * 32 + e, reinterpret_cast<const float*>(&v[e]));
+                }
+                __syncwarp();
+            }
+            if (active) {
+                if (!whole) p.part_ml[prow] = make_float2(m, l);
+                else if (p.lse) p.lse[orow] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+            }
+            tc_fence_before();
+        }
+        if (failed && lane == 0) raise_error(p.err, kErrTimeout);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        tc_fence_after();
+        tmem_dealloc(tmem, kChunkTmem);
+    }
+}
+
+// Merges the parts of every work tile that was cut: block (c, y) the rows [32 y, 32 y + 32) of the tile that CTA c
+// began and did not end.  Its parts are c's last and the first ones of the CTAs behind it, up to the one that ends it.
+// A row is one warp's: 4 rows a warp.
+constexpr int kMergeRows = 32, kMergeThreads = 256;
+template <int D>
+__global__ void __launch_bounds__(kMergeThreads) chunk_merge_kernel(const ChunkParams p, int grid) {
+    griddep_launch_dependents();
+    griddep_wait();
+    const int c = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int4 mine = p.info[c];
+    if (!(mine.x & kHasTail)) return;
+    const int q0 = p.cu_q[mine.y], B = p.cu_q[mine.y + 1] - q0;
+    int last = c + 1;  // the CTA that ends the tile
+    for (int base = c + 1; base < grid; base += 32) {
+        const unsigned hit = __ballot_sync(0xffffffffu, base + lane < grid && (p.info[base + lane].x & kHeadEnds));
+        if (hit) {
+            last = base + __ffs(hit) - 1;
+            break;
+        }
+    }
+    constexpr int kPer = D / 32;
+    for (int k = 0; k < kMergeRows / 8; ++k) {
+        const int row = blockIdx.y * kMergeRows + k * 8 + warp;
+        const int i = row / kTileM, r = row % kTileM, tok = mine.w * 2 * p.tokens + i * p.tokens + r / p.group;
+        if (r / p.group >= p.tokens || tok >= B) continue;
+        float acc[kPer] = {}, m = -INFINITY, l = 0.f;
+        for (int e = c; e <= last; ++e) {
+            const size_t prow = ((size_t)e * 2 + (e == c ? 1 : 0)) * (2 * kTileM) + row;
+            if (e > c && !(p.info[e].x & kHasHead)) continue;
+            const float2 ml = p.part_ml[prow];
+            if (!(ml.y > 0.f)) continue;
+            const float m_new = fmaxf(m, ml.x), w_old = chunk_exp2(m - m_new), w = chunk_exp2(ml.x - m_new);
+            l = l * w_old + ml.y * w;
+#pragma unroll
+            for (int d = 0; d < kPer; ++d) acc[d] = acc[d] * w_old + p.part_o[prow * D + lane * kPer + d] * w;
+            m = m_new;
+        }
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const size_t orow = (size_t)(q0 + tok) * p.num_q_heads + mine.z * p.group + r % p.group;
+#pragma unroll
+        for (int d = 0; d < kPer; d += 2)
+            *reinterpret_cast<uint32_t*>(p.o + orow * D + lane * kPer + d) = pack_bf16x2(acc[d] * inv, acc[d + 1] * inv);
+        if (p.lse && lane == 0) p.lse[orow] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    }
+}
+
+template <int D>
+int run(const ChunkAttentionArgs& a, const DeviceInfo& dev, cudaStream_t stream) {
+    using S = Shape<D>;
+    ChunkParams p;
+    p.o = static_cast<__nv_bfloat16*>(a.o);
+    p.lse = a.lse;
+    p.cu_q = a.cu_q;
+    p.cu_kv = a.cu_kv;
+    p.block_table = a.block_table;
+    p.num_seqs = a.num_seqs;
+    p.num_q_heads = a.num_q_heads;
+    p.num_kv_heads = a.num_kv_heads;
+    p.group = a.num_q_heads / a.num_kv_heads;
+    p.tokens = kTileM / p.group;
+    p.pages_per_seq = a.pages_per_seq;
+    p.page_shift = 0;
+    while ((1 << p.page_shift) < a.page_size) ++p.page_shift;
+    p.num_pages = a.num_pages;
+    p.causal = a.mask == BP_MASK_CAUSAL_BLOCK;
+    p.window = a.window;
+    p.scale_log2 = a.scale * 1.4426950408889634f;
+    p.err = a.err_word;
+    const int grid = std::min(dev.sm_count, kChunkMaxGrid);
+    uint8_t* at = static_cast<uint8_t*>(a.scratch);
+    p.part_o = reinterpret_cast<float*>(at);
+    at += (size_t)kChunkMaxGrid * 2 * 2 * kTileM * D * sizeof(float);
+    p.part_ml = reinterpret_cast<float2*>(at);
+    at += (size_t)kChunkMaxGrid * 2 * 2 * kTileM * sizeof(float2);
+    p.info = reinterpret_cast<int4*>(at);
+
+    CUtensorMap qmap, kmap, vmap;
+    const cuuint64_t qdims[3] = {(cuuint64_t)D, (cuuint64_t)a.num_q_heads, (cuuint64_t)a.total_q};
+    const cuuint64_t qstrides[2] = {(cuuint64_t)D * 2, (cuuint64_t)a.q_stride * 2};
+    const cuuint32_t qbox[3] = {64, (cuuint32_t)p.group, (cuuint32_t)p.tokens};
+    int rc = encode_tensor_map(&qmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(a.q), qdims, qstrides, qbox,
+                               CU_TENSOR_MAP_SWIZZLE_128B);
+    if (rc != BP_OK) return rc;
+    const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)a.num_kv_heads, (cuuint64_t)a.num_pages * a.page_size};
+    const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)a.num_kv_heads * D * 2};
+    const cuuint32_t box[3] = {64, 1, (cuuint32_t)std::min(a.page_size, kKeys)};
+    rc = encode_tensor_map(&kmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(a.k_cache), dims, strides, box,
+                           CU_TENSOR_MAP_SWIZZLE_128B);
+    if (rc != BP_OK) return rc;
+    rc = encode_tensor_map(&vmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(a.v_cache), dims, strides, box,
+                           CU_TENSOR_MAP_SWIZZLE_128B);
+    if (rc != BP_OK) return rc;
+
+    static std::mutex mu;
+    static bool configured[64] = {};
+    if (dev.device < 0 || dev.device >= 64) return BP_ERR_UNSUPPORTED;
+    {
+        std::lock_guard<std::mutex> lock(mu);
+        if (!configured[dev.device]) {
+            if (cudaFuncSetAttribute(chunk_attention_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::smem) != cudaSuccess)
+                return BP_ERR_CUDA;
+            configured[dev.device] = true;
+        }
+    }
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3((unsigned)grid, 1, 1);
+    cfg.blockDim = dim3(kChunkThreads, 1, 1);
+    cfg.dynamicSmemBytes = S::smem;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, chunk_attention_kernel<D>, p, qmap, kmap, vmap) != cudaSuccess) return BP_ERR_CUDA;
+    cfg.gridDim = dim3((unsigned)grid, 2 * kTileM / kMergeRows, 1);
+    cfg.blockDim = dim3(kMergeThreads, 1, 1);
+    cfg.dynamicSmemBytes = 0;
+    return cudaLaunchKernelEx(&cfg, chunk_merge_kernel<D>, p, grid) == cudaSuccess ? BP_OK : BP_ERR_CUDA;
+}
+
+}  // namespace
+
+size_t chunk_attention_scratch_bytes(int head_dim) {
+    return (size_t)kChunkMaxGrid * (2 * 2 * kTileM * ((size_t)head_dim * sizeof(float) + sizeof(float2)) + sizeof(int4));
+}
+
+int launch_chunk_attention(const ChunkAttentionArgs& a, const DeviceInfo& dev, cudaStream_t stream) {
+    return a.head_dim == 128 ? run<128>(a, dev, stream) : run<64>(a, dev, stream);
+}
+
+}  // namespace bp

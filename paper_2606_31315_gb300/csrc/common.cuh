@@ -99,6 +99,52 @@ struct KvAppendArgs {
 int launch_kv_append(const KvAppendArgs& a, cudaStream_t stream);
 int launch_attention_f32(const AttentionArgs& a, const DeviceInfo& dev, cudaStream_t stream);
 
+struct ChunkAttentionArgs {
+    const void* q;
+    int64_t q_stride;  // elements from a token's queries to the next one's
+    const void* k_cache;
+    const void* v_cache;
+    void* o;
+    float* lse;
+    const int32_t* cu_q;
+    const int32_t* cu_kv;
+    const int32_t* block_table;
+    int pages_per_seq, page_size, num_pages, num_seqs, total_q;
+    int num_q_heads, num_kv_heads, head_dim;
+    int mask, window;
+    float scale;
+    void* scratch;  // chunk_attention_scratch_bytes(head_dim)
+    unsigned int* err_word;
+};
+constexpr int kChunkMaxGrid = 192;  // CTAs at most, one an SM; each has its parts' place in the workspace
+size_t chunk_attention_scratch_bytes(int head_dim);
+int launch_chunk_attention(const ChunkAttentionArgs& a, const DeviceInfo& dev, cudaStream_t stream);
+
+// Norms and rotation of queries and keys; with a cache, the keys and values go to their pages.
+struct RopeArgs {
+    const void* q;
+    const void* k;
+    const void* v;  // NULL without a cache
+    int64_t q_stride, k_stride, v_stride;  // elements from a token to the next
+    void* q_out;
+    void* k_out;    // without a cache
+    int64_t q_out_stride, k_out_stride;
+    const void* q_weight;
+    const void* k_weight;
+    const float* cos_sin;
+    const int32_t* positions;
+    int num_tokens, num_q_heads, num_kv_heads, head_dim, rotary_dim, max_pos, interleaved, dtype;
+    float eps;
+    void* k_cache;
+    void* v_cache;
+    const int32_t* cu_new;
+    const int32_t* cu_kv;
+    const int32_t* block_table;
+    int pages_per_seq, page_size, num_pages, num_seqs;
+    unsigned int* err_word;
+};
+int launch_rope(const RopeArgs& a, const DeviceInfo& dev, cudaStream_t stream);
+
 struct AcceptArgs {
     const float* target;
     const float* draft;

@@ -1,0 +1,349 @@
+"""The prefill operators against plain forms in 64 bits: norms and rotation of queries and keys, the same on the way into
+a paged cache, and attention of chunks of new tokens over it.
+
+Tolerances are per element and derived from what the kernels round (u = 2^-8, the unit roundoff of bf16's 8 bits,
+e = 2^-24 that of fp32):
+  norm and rotation   fp32 throughout: the mean of squares, its root, two products and a rotation of two products and a
+                      sum stay within 16 e of |a| + |b|, the pair's sizes after the norm; a bf16 output adds u of itself
+  attention           a weight is rounded to bf16 (u), its exponent carries the fp32 error of a product of 128 terms
+                      (below 5e-4 for these inputs: 128 e times |q| |k| scale < 35, doubled for weight and sum), and
+                      the output is rounded (u): (u + 1e-3) sum_j p_j |v_j| + u |o|; log-sum-exp within 5e-4
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2606_31315_gb300 as bp
+
+pytestmark = pytest.mark.gpu
+
+U, E = 2.0 ** -8, 2.0 ** -24
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    bp.build()
+    bp.load()
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _offsets(lengths):
+    return torch.tensor(np.concatenate([[0], np.cumsum(lengths)]), dtype=torch.int32, device="cuda")
+
+
+def _table(positions, rotary):
+    angle = torch.arange(positions, dtype=torch.float64)[:, None] * 1e4 ** (
+        -torch.arange(rotary // 2, dtype=torch.float64) / max(1, rotary // 2))
+    return torch.cat([angle.cos(), angle.sin()], 1).float().cuda()
+
+
+def _turned(x, weight, table, pos, interleaved, eps):
+    """(the exact result, |a| + |b| of every element's pair) in 64 bits."""
+    x = x.double()
+    if weight is not None:
+        x = x / torch.sqrt((x * x).mean(-1, keepdim=True) + eps) * weight.double()
+    r = 0 if table is None else table.shape[1]
+    if r == 0:
+        return x, x.abs()
+    row = table[pos.long()].double()[:, None]
+    c, s = row[..., :r // 2], row[..., r // 2:]
+    i = torch.arange(r // 2, device="cuda")
+    ia, ib = (2 * i, 2 * i + 1) if interleaved else (i, i + r // 2)
+    a, b = x[..., ia], x[..., ib]
+    out, size = x.clone(), x.abs()
+    out[..., ia], out[..., ib] = a * c - b * s, b * c + a * s
+    size[..., ia] = size[..., ib] = a.abs() + b.abs()
+    return out, size
+
+
+def _near_turned(got, ref):
+    out, size = ref
+    tol = 16 * E * size + (U * out.abs() * 1.001 if got.dtype == torch.bfloat16 else 0.0)
+    err = (got.double() - out).abs()
+    assert torch.all(err <= tol + 1e-37), float((err - tol).max())
+
+
+TURNS = [  # head_dim, rotary_dim, interleaved, norm
+    (128, 128, False, True), (128, 64, False, True), (128, 128, True, True), (64, 64, False, True), (64, 32, True, False),
+    (96, 96, False, True), (80, 16, False, True), (256, 128, False, True), (16, 16, True, True), (128, 0, False, True),
+    (8, 0, False, False)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dim,rotary,interleaved,norm", TURNS)
+@pytest.mark.parametrize("tokens,hq,hkv", [(1, 32, 8), (7, 5, 1), (1500, 6, 2)])
+def test_norm_and_rotation(dtype, dim, rotary, interleaved, norm, tokens, hq, hkv):
+    g = _gen(tokens + dim)
+    q = torch.randn(tokens, hq, dim, device="cuda", generator=g).to(dtype)
+    k = (3 * torch.randn(tokens, hkv, dim, device="cuda", generator=g)).to(dtype)
+    q[0, 0] = 0  # a head of zeros: eps keeps its norm finite
+    qw, kw = [(1 + torch.randn(dim, device="cuda", generator=g)).to(dtype) if norm else None for _ in range(2)]
+    table = _table(500, rotary) if rotary else None
+    pos = torch.randint(0, 500, (tokens,), device="cuda", generator=g).to(torch.int32)
+    ws = bp.workspace(256, "cuda")
+    qo, ko = bp.qk_norm_rope(q, k, table, pos, q_weight=qw, k_weight=kw, interleaved=interleaved, eps=1e-5, ws=ws)
+    assert bp.get_status(ws) == 0
+    _near_turned(qo, _turned(q, qw, table, pos, interleaved, 1e-5))
+    _near_turned(ko, _turned(k, kw, table, pos, interleaved, 1e-5))
+
+
+def test_norm_and_rotation_of_views_and_in_place():
+    """Views of a packed projection, queries alone, keys alone, and outputs over the inputs."""
+    g = _gen(1)
+    packed = torch.randn(37, 12, 128, device="cuda", generator=g).to(torch.bfloat16)
+    q, k = packed[:, :8], packed[:, 8:10]
+    w = (1 + 0.1 * torch.randn(128, device="cuda", generator=g)).to(torch.bfloat16)
+    table, pos = _table(64, 128), torch.arange(37, device="cuda", dtype=torch.int32)
+    rq, rk = _turned(q, w, table, pos, False, 1e-6), _turned(k, w, table, pos, False, 1e-6)
+    ws = bp.workspace(256, "cuda")
+    qo, none = bp.qk_norm_rope(q, None, table, pos, q_weight=w, ws=ws)
+    assert none is None
+    _near_turned(qo, rq)
+    none, ko = bp.qk_norm_rope(None, k, table, pos, k_weight=w, ws=ws)
+    assert none is None
+    _near_turned(ko, rk)
+    rest = packed[:, 10:].clone()
+    bp.qk_norm_rope(q, k, table, pos, q_weight=w, k_weight=w, q_out=q, k_out=k, ws=ws)
+    _near_turned(packed[:, :8], rq)
+    _near_turned(packed[:, 8:10], rk)
+    assert torch.equal(packed[:, 10:], rest) and bp.get_status(ws) == 0
+
+
+def test_a_position_outside_the_table_is_reported():
+    x = torch.ones(3, 2, 64, device="cuda")
+    out = torch.full_like(x, 7.0)
+    ws = bp.workspace(256, "cuda")
+    table = _table(10, 64)
+    bp.qk_norm_rope(x, None, table, torch.tensor([0, 10, -1], dtype=torch.int32, device="cuda"), q_out=out, ws=ws)
+    assert bp.get_status(ws) == bp._binding.BP_ERR_DEVICE_FLAG
+    assert torch.all(out[1:] == 7.0) and torch.all(out[0] != 7.0)
+
+
+def _paged(lens, page, hkv, dim, dtype, g, held):
+    """A pool whose rows are not numbers, but for the first held[s] keys of every sequence; a table of shuffled pages."""
+    need = [-(-n // page) for n in lens]
+    order = torch.randperm(sum(need) + 2, generator=torch.Generator().manual_seed(page)).to(torch.int32)
+    table = torch.full((len(lens), max(1, max(need))), -5, dtype=torch.int32)  # entries no sequence uses
+    at = 0
+    for s, n in enumerate(need):
+        table[s, :n] = order[at:at + n]
+        at += n
+    table = table.cuda()
+    rows = (sum(need) + 2) * page
+    caches = [torch.full((rows, hkv, dim), math.nan, device="cuda", dtype=dtype) for _ in range(2)]
+    keys = []
+    for s, n in enumerate(lens):
+        j = torch.arange(n, device="cuda")
+        r = table[s].long()[j // page] * page + j % page
+        keys.append(r)
+        for c in caches:
+            c[r[:held[s]]] = torch.randn(held[s], hkv, dim, device="cuda", generator=g).to(dtype)
+    return caches, table, keys
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("ctx,new", [((0,), (1,)), ((5, 100, 0, 33, 63), (3, 1, 70, 0, 1)), ((40,) * 45, (2, 0, 1) * 15),
+                                     ((1000, 7), (600, 400))])
+@pytest.mark.parametrize("page,packed", [(16, True), (64, False)])
+def test_append(dtype, ctx, new, page, packed):
+    """Keys normed and rotated, values as they are, each at its key's place and nothing else touched; the queries; rows of
+    padding behind the last sequence left out."""
+    g = _gen(len(ctx))
+    hq, hkv, dim, pad = 4, 2, 64, 3
+    total = sum(new)
+    (kc, vc), table, keys = _paged([c + n for c, n in zip(ctx, new)], page, hkv, dim, dtype, g, ctx)
+    qkv = torch.randn(total + pad, hq + 2 * hkv, dim, device="cuda", generator=g).to(dtype)
+    kw = (1 + 0.1 * torch.randn(dim, device="cuda", generator=g)).to(dtype)
+    tab = _table(max(c + n for c, n in zip(ctx, new)), 32)
+    q, k, v = qkv.split([hq, hkv, hkv], 1)
+    rows = torch.cat([r[c:] for r, c in zip(keys, ctx)])
+    pos = torch.cat([torch.arange(c, c + n, device="cuda") for c, n in zip(ctx, new)])
+    want_k, want_v = kc.clone(), vc.clone()
+    want_v[rows] = v[:total]
+    ws = bp.workspace(256, "cuda")
+    qo = torch.full((total + pad, hq, dim), 7.0, device="cuda", dtype=dtype)
+    given = qkv if packed else (q.contiguous(), k.contiguous(), v.contiguous())
+    got = bp.qkv_append(given, kc, vc, _offsets(new), _offsets([c + n for c, n in zip(ctx, new)]), table, page, tab,
+                        k_weight=kw, q_out=qo, ws=ws)
+    assert bp.get_status(ws) == 0 and got is qo
+    _near_turned(qo[:total], _turned(q[:total], None, tab, pos, False, 1e-6))
+    assert torch.all(qo[total:] == 7.0)
+    _near_turned(kc[rows], _turned(k[:total], kw, tab, pos, False, 1e-6))
+    want_k[rows] = kc[rows]
+    bits = torch.int16 if dtype == torch.bfloat16 else torch.int32
+    assert torch.equal(kc.view(bits), want_k.view(bits)) and torch.equal(vc.view(bits), want_v.view(bits))
+
+
+def test_append_of_keys_alone_at_given_positions():
+    g = _gen(2)
+    (kc, vc), table, keys = _paged([20], 16, 2, 128, torch.bfloat16, g, [15])
+    k, v = [torch.randn(5, 2, 128, device="cuda", generator=g).to(torch.bfloat16) for _ in range(2)]
+    pos = torch.tensor([9, 3, 0, 4, 7], dtype=torch.int32, device="cuda")
+    tab = _table(10, 128)
+    ws = bp.workspace(256, "cuda")
+    assert bp.qkv_append((None, k, v), kc, vc, _offsets([5]), _offsets([20]), table, 16, tab, positions=pos, interleaved=True,
+                         ws=ws) is None
+    assert bp.get_status(ws) == 0
+    _near_turned(kc[keys[0][15:]], _turned(k, None, tab, pos, True, 1e-6))
+    assert torch.equal(vc[keys[0][15:]], v)
+
+
+def test_append_without_a_place_is_reported():
+    """A page id outside the pool and a key past the table: reported, not written; the other sequence's tokens are."""
+    g = _gen(3)
+    (kc, vc), table, keys = _paged([16, 32], 16, 1, 64, torch.float32, g, [15, 30])
+    table[0, 0] = 99
+    k, v = [torch.randn(4, 1, 64, device="cuda", generator=g) for _ in range(2)]
+    before = kc.clone()
+    ws = bp.workspace(256, "cuda")
+    # sequence 0: one token on page 99; sequence 1: key 31 has a place, keys 32 and 33 lie past its two pages
+    bp.qkv_append((None, k, v), kc, vc, _offsets([1, 3]), _offsets([16, 34]), table, 16, None, ws=ws)
+    assert bp.get_status(ws) == bp._binding.BP_ERR_DEVICE_FLAG
+    before[keys[1][31]] = k[1]
+    assert torch.equal(kc.view(torch.int32), before.view(torch.int32))
+
+
+def _attend(q, kc, vc, rows, causal, window, scale):
+    """One sequence in 64 bits: o, the sums of p |v|, the log-sum-exp; rows without a key give 0 and -inf."""
+    b, hq, d = q.shape
+    n, hkv = len(rows), kc.shape[1]
+    k, v = [c[rows].double().repeat_interleave(hq // hkv, 1) for c in (kc, vc)]
+    x = torch.einsum("ihd,jhd->hij", q.double(), k) * scale
+    p, j = torch.arange(n - b, n, device="cuda")[:, None], torch.arange(n, device="cuda")[None]
+    hidden = torch.zeros(b, n, dtype=torch.bool, device="cuda")
+    if causal:
+        hidden |= j > p
+    if window:
+        hidden |= j <= p - window
+    x.masked_fill_(hidden, -math.inf)
+    z = torch.logsumexp(x, 2) if n else torch.full((hq, b), -math.inf, dtype=torch.float64, device="cuda")
+    w = torch.exp(x - z[..., None].nan_to_num(neginf=0.0))
+    return torch.einsum("hij,jhd->ihd", w, v), torch.einsum("hij,jhd->ihd", w, v.abs()), z.T
+
+
+def _check_chunk(ctx, new, hq=8, hkv=2, dim=128, page=16, causal=True, window=0, scale=0.0, seed=0, stride=None):
+    g = _gen(seed)
+    lens = [c + n for c, n in zip(ctx, new)]
+    (kc, vc), table, keys = _paged(lens, page, hkv, dim, torch.bfloat16, g, lens)
+    total = sum(new)
+    wide = torch.randn(total, stride or hq, dim, device="cuda", generator=g).mul_(1.5).to(torch.bfloat16)
+    q = wide[:, :hq]
+    lse = torch.full((total, hq), 7.0, device="cuda")
+    out = torch.full((total, hq, dim), 7.0, device="cuda", dtype=torch.bfloat16)
+    ws = bp.workspace(bp.chunk_attention_workspace_size(len(new), total, hq, hkv, dim), "cuda")
+    bp.chunk_attention_paged(q, kc, vc, _offsets(new), _offsets(lens), table, page, max(new), max(1, max(lens)),
+                             mask=bp.MASK_CAUSAL if causal else bp.MASK_BIDIR, window=window, softmax_scale=scale, out=out,
+                             lse=lse, ws=ws)
+    assert bp.get_status(ws) == 0
+    at = 0
+    for c, n, r in zip(ctx, new, keys):
+        if n:
+            o, size, z = _attend(q[at:at + n], kc, vc, r, causal, window, scale or dim ** -0.5)
+            err = (out[at:at + n].double() - o).abs()
+            tol = (U + 1e-3) * size + U * o.abs()
+            assert torch.all(err <= tol + 1e-30), (c, n, float((err - tol).max()))
+            got = lse[at:at + n].double()
+            assert torch.equal(torch.isinf(z), torch.isinf(got))
+            assert float((got - z).nan_to_num(0.0, 0.0, 0.0).abs().max()) <= 5e-4
+        at += n
+    return out
+
+
+@pytest.mark.parametrize("dim", [128, 64])
+@pytest.mark.parametrize("ctx,new", [
+    ((0,), (1,)), ((0,), (2,)), ((15,), (1,)), ((127,), (1,)), ((128,), (1,)), ((2047,), (1,)), ((0,), (63,)),
+    ((0,), (128,)), ((0,), (129,)), ((700,), (300,)), ((5, 0, 1000, 31, 64), (1, 200, 33, 0, 17)), ((3000,), (70,)),
+    ((0,) * 40, (1, 2, 3, 50) * 10)])
+def test_chunk_lengths(dim, ctx, new):
+    _check_chunk(ctx, new, dim=dim)
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (8, 8), (6, 2), (10, 2), (7, 1), (32, 8), (16, 1), (128, 1), (100, 1)])
+@pytest.mark.parametrize("dim,page", [(128, 64), (64, 16)])
+def test_chunk_heads(hq, hkv, dim, page):
+    _check_chunk((130, 17, 4), (70, 1, 140), hq=hq, hkv=hkv, dim=dim, page=page, seed=hq)
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256, 1024])
+def test_chunk_pages(page):
+    _check_chunk((200, 0, 511), (77, 300, 1), page=page, seed=page)
+
+
+@pytest.mark.parametrize("window", [1, 2, 100, 128, 129, 700, 5000])
+@pytest.mark.parametrize("causal", [True, False])
+def test_chunk_windows(window, causal):
+    _check_chunk((900, 0, 300), (200, 500, 1), causal=causal, window=window, seed=window)
+
+
+@pytest.mark.parametrize("dim", [128, 64])
+def test_chunk_sees_everything(dim):
+    _check_chunk((0, 100, 1000), (130, 1, 64), causal=False, dim=dim)
+
+
+def test_chunk_scale_and_stride():
+    _check_chunk((300, 0), (90, 40), scale=0.3, stride=13)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_rows_without_keys(causal):
+    """More new tokens than keys: the first rows see nothing and are 0, with a log-sum-exp of -inf."""
+    _check_chunk((-50, 0, -3, -200, 100), (80, 5, 3, 500, 2), causal=causal)
+    _check_chunk((-50, 10), (80, 70), causal=causal, window=20)
+
+
+def test_long_split_and_repeats():
+    """A context cut over all CTAs; the same call gives the same bits again, and once more on another stream."""
+    ctx, new = (20000, 3, 9000), (40, 5, 1)
+    a = _check_chunk(ctx, new, hq=4, hkv=1, page=64)
+    b = _check_chunk(ctx, new, hq=4, hkv=1, page=64)
+    assert torch.equal(a, b)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        c = _check_chunk(ctx, new, hq=4, hkv=1, page=64)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(a, c)
+
+
+def test_scores_of_any_size():
+    """Rows whose maxima grow from tile to tile, and scores far below 0: the running maximum is followed."""
+    g = _gen(9)
+    n, hkv, dim = 1200, 1, 128
+    (kc, vc), table, keys = _paged([n], 64, hkv, dim, torch.bfloat16, g, [n])
+    ramp = torch.linspace(-60, 60, n, device="cuda")
+    kc[keys[0]] = 0
+    kc[keys[0], 0, 0] = ramp.to(torch.bfloat16)
+    q = torch.zeros(64, 2, dim, device="cuda", dtype=torch.bfloat16)
+    q[:, 0, 0], q[:, 1, 0] = 30.0, -30.0
+    ws = bp.workspace(bp.chunk_attention_workspace_size(1, 64, 2, 1, dim), "cuda")
+    out, _ = bp.chunk_attention_paged(q, kc, vc, _offsets([64]), _offsets([n]), table, 64, 64, n, softmax_scale=1.0, ws=ws)
+    assert bp.get_status(ws) == 0
+    o, size, _ = _attend(q, kc, vc, keys[0], True, 0, 1.0)
+    assert torch.all((out.double() - o).abs() <= (U + 1e-3) * size + U * o.abs() + 1e-30)
+
+
+def test_a_bad_page_is_reported():
+    g = _gen(4)
+    (kc, vc), table, _ = _paged([300], 16, 1, 64, torch.bfloat16, g, [300])
+    table[0, 3] = 10 ** 6
+    q = torch.randn(4, 2, 64, device="cuda", generator=g).to(torch.bfloat16)
+    ws = bp.workspace(bp.chunk_attention_workspace_size(1, 4, 2, 1, 64), "cuda")
+    bp.chunk_attention_paged(q, kc, vc, _offsets([4]), _offsets([300]), table, 16, 4, 300, ws=ws)
+    assert bp.get_status(ws) == bp._binding.BP_ERR_DEVICE_FLAG
+
+
+def test_empty_calls():
+    z = lambda *s: torch.zeros(*s, device="cuda", dtype=torch.bfloat16)  # noqa: E731
+    ws = bp.workspace(bp.chunk_attention_workspace_size(1, 0, 2, 1, 64), "cuda")
+    table = torch.zeros(1, 1, dtype=torch.int32, device="cuda")
+    o, _ = bp.chunk_attention_paged(z(0, 2, 64), z(16, 1, 64), z(16, 1, 64), _offsets([0]), _offsets([5]), table, 16, 0, 5, ws=ws)
+    assert o.shape == (0, 2, 64)
+    assert bp.qk_norm_rope(z(0, 2, 64), z(0, 1, 64), _table(4, 64), torch.zeros(0, dtype=torch.int32, device="cuda"))[0].shape == (0, 2, 64)
+    assert bp.qkv_append(z(0, 4, 64), z(16, 1, 64), z(16, 1, 64), _offsets([0]), _offsets([5]), table, 16, None).shape == (0, 2, 64)
