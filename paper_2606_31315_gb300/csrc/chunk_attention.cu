@@ -15,8 +15,8 @@
 //     stretch of it and works through its tiles.  Where a cut falls inside a tile, the two CTAs leave (O, m, l) in the
 //     workspace and a second kernel merges them, in the order of the keys.  So one long context, a ragged batch and a
 //     mix of prompts and decoding sequences all fill the GPU, and no order of arrival enters the result.
-//   * Roles: warps 0-3 and 4-7 softmax, warp 8 TMA producer (its lanes issue the boxes of a tile's pages), warp 9 MMA,
-//     warp 10 clears the rows of V behind a sequence's last key (a page's unused rows may hold anything; their weight
+//   * Roles: warps 0-7 and 8-15 softmax of stream 0 and 1, warp 16 lays out the CTA's jobs and issues the TMA copies (its
+//     lanes the boxes of a tile's pages), warps 17 and 18 issue the streams' MMAs, warp 19 clears the rows of V behind a sequence's last key (a page's unused rows may hold anything; their weight
 //     is 0, but 0 times a NaN is none).
 #include <cuda_bf16.h>
 
@@ -32,25 +32,28 @@ namespace {
 constexpr int kTileM = 128;                      // rows of one stream's query tile
 constexpr int kKeys = 128;                       // keys per K/V tile
 constexpr int kHalfBytes = kKeys * 128;          // 128 rows of 64 columns, 128-byte swizzle
-constexpr int kSoftmaxWarps = 8;
-constexpr int kProducerWarp = 8, kMmaWarp = 9, kTailWarp = 10;
-constexpr int kChunkThreads = 32 * 11;
+constexpr int kSoftmaxWarps = 16;                // two threads a row, 64 keys each
+constexpr int kProducerWarp = 16, kMmaWarp = 17, kTailWarp = 19;  // (a stream's MMA warp: kMmaWarp + stream)
+constexpr int kChunkThreads = 32 * 20;
+// Registers: 96 a thread at launch; the softmax warps take 104, the other warpgroup keeps 64 (512 x 104 + 128 x 64 =
+// 640 x 96).
+constexpr int kSoftmaxRegs = 104, kOtherRegs = 64;
 constexpr uint32_t kChunkTmem = 512;
 constexpr int kTileCost = 192;                   // a work tile's fixed cost (queries in, output out), in keys
 constexpr int kLeastCost = kTileCost + 2 * kKeys;  // of a CTA's stretch: below it, fewer CTAs take part
+constexpr int kJobs = 4;                         // jobs laid out ahead
 constexpr int kLeastCut = 2;                     // key tiles on either side of a cut
-constexpr int kMaxPages = kKeys / 16;            // pages under a key tile at the smallest page size
 
 template <int D>
 struct Shape {
     static constexpr int halves = D / 64;
     static constexpr int tile_bytes = halves * kHalfBytes;      // one K, V or Q tile
     static constexpr int slots = D == 128 ? 5 : 12;             // ring of K and V tiles
-    static constexpr int smem = (2 + slots) * tile_bytes + 1024;
+    static constexpr int tiles = (2 + slots) * tile_bytes;      // the two Q tiles, the ring
     static constexpr uint32_t col_o = 256;                      // O of stream i: columns col_o + i * D
 };
-static_assert(Shape<128>::smem >= tmem_smem_share((int)kChunkTmem, 228 * 1024) &&
-                  Shape<64>::smem >= tmem_smem_share((int)kChunkTmem, 228 * 1024),
+static_assert(Shape<128>::tiles >= tmem_smem_share((int)kChunkTmem, 228 * 1024) &&
+                  Shape<64>::tiles >= tmem_smem_share((int)kChunkTmem, 228 * 1024),
               "leaves no other CTA's tensor memory room");
 
 struct ChunkParams {
@@ -113,10 +116,12 @@ struct Place {
 };
 
 // One CTA's run of key tiles of one work tile.
-struct Stretch {
-    int s, h, t, q0, B, n;
+struct Job {
+    int s, h, t;       // sequence (-1: no more jobs), KV head, work tile
+    int q0, B, n;      // the sequence's first query row, its new tokens and keys
     int j0, j1;        // key tiles, counted from key 0
-    bool first, last;  // it holds the work tile's first / last key tile
+    int a[2], b[2];    // those that some row of stream 0's / 1's tile sees (a = b: none)
+    int first, last;   // it holds the work tile's first / last key tile
 };
 
 struct Line {
@@ -166,14 +171,21 @@ struct Line {
     }
 };
 
-// Works through the stretches between two places; every role of the CTA does so by itself.
+// Works through the jobs between two places.
 struct Walk {
     const ChunkParams& p;
     Place at, end;
-    __device__ __forceinline__ bool next(Stretch& g) {
+    int known;  // the sequence that `q` and `q0` are of
+    Seq q;
+    int q0;
+    __device__ __forceinline__ bool next(Job& g) {
         const Line line{p};
         while (at.s < end.s || (at.s == end.s && (at.h < end.h || (at.h == end.h && (at.t < end.t || (at.t == end.t && at.j < end.j)))))) {
-            const Seq q = line.seq(at.s);
+            if (at.s != known) {
+                q = line.seq(at.s);
+                q0 = __ldg(p.cu_q + at.s);
+                known = at.s;
+            }
             const int T = q.tiles();
             if (T <= 0) {
                 at = Place{at.s + 1, 0, 0, 0};
@@ -182,11 +194,20 @@ struct Walk {
             int first, count;
             Line::span(q, at.t, first, count);
             const bool cut = at.same_tile(end);
-            g.s = at.s; g.h = at.h; g.t = at.t; g.q0 = __ldg(p.cu_q + at.s); g.B = q.B; g.n = q.n;
+            g.s = at.s; g.h = at.h; g.t = at.t; g.q0 = q0; g.B = q.B; g.n = q.n;
             g.j0 = first + at.j;
             g.j1 = first + (cut ? end.j : count);
             g.first = at.j == 0;
             g.last = !cut;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int tok = g.t * q.Q + i * p.tokens, tok_end = min(g.B, tok + p.tokens);
+                const int lo = q.lo(tok), hi = q.hi(max(tok_end, 0));
+                const int a = max(g.j0, lo / kKeys), b = min(g.j1, (hi + kKeys - 1) / kKeys);
+                const bool some = tok < g.B && hi > lo && a < b;
+                g.a[i] = some ? a : g.j0;
+                g.b[i] = some ? b : g.j0;
+            }
             if (cut) {
                 at = end;
             } else {
@@ -202,294 +223,109 @@ struct Walk {
     }
 };
 
-// Stream i's key tiles of a stretch: those that some row of its tile sees.
-__device__ __forceinline__ void stream_range(const ChunkParams& p, const Stretch& g, int i, int& a, int& b) {
-    const Seq q{g.B, g.n, 2 * p.tokens, p.causal, p.window};
-    const int tok = g.t * q.Q + i * p.tokens, end = min(g.B, tok + p.tokens);
-    a = b = g.j0;
-    if (tok >= g.B) return;
-    const int lo = q.lo(tok), hi = q.hi(end);
-    if (hi <= lo) return;
-    a = max(g.j0, lo / kKeys);
-    b = min(g.j1, (hi + kKeys - 1) / kKeys);
-    if (b <= a) a = b = g.j0;
-}
+// Shared memory behind the tiles.
+template <int SLOTS>
+struct Shared {
+    uint64_t full[SLOTS], empty[SLOTS], raw[SLOTS];  // the ring; raw: a V tile that the tail warp hands on
+    uint64_t q_full, q_empty, drain[2], turn[2];
+    uint64_t s[2], p[2], o[2];                       // of a stream: scores, weights, the accumulator
+    uint64_t job_full[kJobs], job_empty[kJobs];
+    Job job[kJobs];                                  // what the producer warp has laid out for the others
+    uint32_t tmem;
+    int pair_failed[8];
+    float row[2][2][kTileM];                         // [stream][half]: row maxima, at the end row sums
+};
+template <int D>
+constexpr int chunk_smem() { return Shape<D>::tiles + (int)sizeof(Shared<Shape<D>::slots>); }
+static_assert(chunk_smem<128>() <= 227 * 1024 && chunk_smem<64>() <= 227 * 1024, "a block's shared memory");
 
 template <int D>
 __global__ void __launch_bounds__(kChunkThreads, 1)
 chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap qmap,
                        const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
     using S = Shape<D>;
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bar_full[S::slots], bar_empty[S::slots], bar_raw[S::slots];
-    __shared__ uint64_t bar_q_full, bar_q_empty, bar_s[2], bar_p[2], bar_o[2], bar_drain;
-    __shared__ uint32_t tmem_sh;
-    __shared__ Place ends[2];
-    uint8_t* const smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
+    extern __shared__ __align__(1024) uint8_t smem[];
     uint8_t* const sQ = smem;                           // two tiles
     uint8_t* const sKV = smem + 2 * S::tile_bytes;      // the ring
+    Shared<S::slots>& sh = *reinterpret_cast<Shared<S::slots>*>(smem + S::tiles);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int G = p.group;
+    if (smem_addr(smem) & 1023) {  // (the swizzled tiles' alignment: dynamic shared memory starts on such a boundary)
+        if (tid == 0) raise_error(p.err, kErrDeviceArg);
+        return;
+    }
 
+    if (tid < 8) sh.pair_failed[tid] = 0;
     if (tid == 0) {
         for (int i = 0; i < S::slots; ++i) {
-            mbar_init(&bar_full[i], 1);
-            mbar_init(&bar_empty[i], 1);
-            mbar_init(&bar_raw[i], 1);
+            mbar_init(&sh.full[i], 1);
+            mbar_init(&sh.empty[i], 2);
+            mbar_init(&sh.raw[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&bar_s[i], 1);
-            mbar_init(&bar_p[i], 128);
-            mbar_init(&bar_o[i], 1);
+            mbar_init(&sh.s[i], 1);
+            mbar_init(&sh.p[i], 256);
+            mbar_init(&sh.o[i], 1);
+            mbar_init(&sh.drain[i], 1);
+            mbar_init(&sh.turn[i], 1);
         }
-        mbar_init(&bar_q_full, 1);
-        mbar_init(&bar_q_empty, 1);
-        mbar_init(&bar_drain, 1);
+        for (int i = 0; i < kJobs; ++i) {
+            mbar_init(&sh.job_full[i], 1);
+            mbar_init(&sh.job_empty[i], kSoftmaxWarps + 3);
+        }
+        mbar_init(&sh.q_full, 1);
+        mbar_init(&sh.q_empty, 2);
         fence_mbar_init();
     }
     if (warp == kMmaWarp) {
-        tmem_alloc(&tmem_sh, kChunkTmem);
+        tmem_alloc(&sh.tmem, kChunkTmem);
         tmem_relinquish();
     }
     griddep_wait();
-    if (warp == kProducerWarp) {  // this CTA's stretch of the line
-        const Line line{p};
-        auto whole = [&](int s) -> long long {
-            if (s >= p.num_seqs) return 0;
-            const Seq q = line.seq(s);
-            return q.B > 0 ? q.cost(q.tiles()) * p.num_kv_heads : 0;
-        };
-        long long total = 0;
-        for (int base = 0; base < p.num_seqs; base += 32) {
-            long long w = whole(base + lane);
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
-            total += w;
-        }
-        const long long parts = min((long long)gridDim.x, max(1ll, total / kLeastCost));
-        const long long c = blockIdx.x;
-        // cuts at total * c / parts
-        const long long step = total / parts, rest = total % parts;
-        const long long cut[2] = {c * step + c * rest / parts, (c + 1) * step + (c + 1) * rest / parts};
-        Place place[2] = {Place{p.num_seqs, 0, 0, 0}, Place{p.num_seqs, 0, 0, 0}};
-        long long before = 0;
-        if (c < parts) {
-            for (int base = 0; base < p.num_seqs; base += 32) {
-                const long long w = whole(base + lane);
-                long long incl = w;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const long long y = __shfl_up_sync(0xffffffffu, incl, o);
-                    if (lane >= o) incl += y;
-                }
-                incl += before;
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const unsigned hit = __ballot_sync(0xffffffffu, w > 0 && incl - w <= cut[e] && cut[e] < incl);
-                    if (hit) {
-                        const int l = __ffs(hit) - 1;
-                        place[e] = line.within(base + l, cut[e] - __shfl_sync(0xffffffffu, incl - w, l));
-                    }
-                }
-                before = __shfl_sync(0xffffffffu, incl, 31);
-            }
-        }
-        if (lane < 2) ends[lane] = place[lane];
-    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     griddep_launch_dependents();
-    const uint32_t tmem = tmem_sh;
-    Walk walk{p, ends[0], ends[1]};
-    Stretch g;
-
-    if (warp == kProducerWarp) {
-        // ================= TMA producer: queries, then K and V tiles through the ring, K first
-        const int rows = min(kKeys, 1 << p.page_shift);  // of a box
-        const int nbox = kKeys / rows;
-        const int box = lane / S::halves, half = lane % S::halves;
-        unsigned x = 0;  // ring position
-        int nq = 0;
-        bool ok = true;
-        unsigned on_raw = 0, raw_phase = 0;  // per slot: whether its last use is on bar_raw; that barrier's uses, mod 2
-        while (ok && walk.next(g)) {
-            const int tok = g.t * 2 * p.tokens;
-            int a0, b0, a1, b1;
-            stream_range(p, g, 0, a0, b0);
-            stream_range(p, g, 1, a1, b1);
-            if (g.j1 <= g.j0) continue;
-            if (nq > 0 && !__all_sync(0xffffffffu, mbar_wait(&bar_q_empty, (nq - 1) & 1, kWaitBudget))) {
-                ok = false;
-                break;
-            }
-            const bool two = tok + p.tokens < g.B;
-            if (lane == 0) {
-                const uint32_t bytes = (uint32_t)(p.tokens * G) * 128 * S::halves;
-                mbar_arrive_expect_tx(&bar_q_full, two ? 2 * bytes : bytes);
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    if (i == 0 || two)
-#pragma unroll
-                        for (int hh = 0; hh < S::halves; ++hh)
-                            tma_load_3d(sQ + i * S::tile_bytes + hh * kHalfBytes, &qmap, &bar_q_full, 64 * hh, g.h * G,
-                                        g.q0 + tok + i * p.tokens);
-            }
-            ++nq;
-            const int32_t* table = p.block_table + (size_t)g.s * p.pages_per_seq;
-            const int last_page = (g.n - 1) >> p.page_shift;
-            // the pool row of this lane's box of key tile j (-1: past the sequence's last page)
-            auto pool_row = [&](int j) {
-                const int key = j * kKeys + box * rows, pg = key >> p.page_shift;
-                if (box >= nbox || pg > last_page) return -1;
-                int id = pg < p.pages_per_seq ? __ldg(table + pg) : -1;
-                if ((unsigned)id >= (unsigned)p.num_pages) {
-                    raise_error(p.err, kErrDeviceArg);
-                    id = 0;
-                }
-                return (id << p.page_shift) + (key & ((1 << p.page_shift) - 1));
-            };
-            int row = pool_row(g.j0);
-            for (int j = g.j0; j < g.j1 && ok; ++j) {
-                const int row_next = j + 1 < g.j1 ? pool_row(j + 1) : -1;
-                const int boxes = min(nbox, ((g.n - j * kKeys) + rows - 1) / rows);
-#pragma unroll
-                for (int kv = 0; kv < 2; ++kv, ++x) {
-                    const int slot = x % S::slots;
-                    const unsigned use = x / S::slots;
-                    if (use > 0 && !__all_sync(0xffffffffu, mbar_wait(&bar_empty[slot], (use - 1) & 1, kWaitBudget))) {
-                        ok = false;
-                        break;
-                    }
-                    // a V tile with rows past the last key goes through the tail warp
-                    const bool raw = kv == 1 && (j + 1) * kKeys > g.n;
-                    uint64_t* bar = raw ? &bar_raw[slot] : &bar_full[slot];
-                    on_raw = raw ? on_raw | 1u << slot : on_raw & ~(1u << slot);
-                    if (raw) raw_phase ^= 1u << slot;
-                    if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(boxes * rows) * 128 * S::halves);
-                    __syncwarp();
-                    if (row >= 0)
-                        tma_load_3d(sKV + slot * S::tile_bytes + half * kHalfBytes + box * rows * 128, kv ? &vmap : &kmap,
-                                    bar, 64 * half, g.h, row);
-                }
-                row = row_next;
-            }
-        }
-        if (!ok && lane == 0) raise_error(p.err, kErrTimeout);
-        // no copy may still be in flight when the CTA leaves
-        for (unsigned y = x > (unsigned)S::slots ? x - S::slots : 0; y < x; ++y) {
-            const int slot = y % S::slots;
-            const bool raw = on_raw >> slot & 1;
-            if (!mbar_wait(raw ? &bar_raw[slot] : &bar_full[slot], raw ? ~raw_phase >> slot & 1 : (y / S::slots) & 1, kDrainBudget) && lane == 0)
-                raise_error(p.err, kErrTimeout);
-        }
-        if (nq > 0 && !mbar_wait(&bar_q_full, (nq - 1) & 1, kDrainBudget) && lane == 0) raise_error(p.err, kErrTimeout);
-    } else if (warp == kMmaWarp) {
-        // ================= MMA issuer
-        if (lane == 0) {
-            const uint32_t id_s = idesc_bf16_f32(kTileM, kKeys, false, false);
-            const uint32_t id_o = idesc_bf16_f32(kTileM, D, false, true);
-            const uint32_t q_addr = smem_addr(sQ), kv_addr = smem_addr(sKV);
-            unsigned x0 = 0;  // ring position of the stretch's first K tile
-            unsigned np[2] = {0, 0};
-            int nq = 0;
-            bool ok = true, any = false;
-            while (ok && walk.next(g)) {
-                if (g.j1 <= g.j0) continue;
-                int a[2], b[2];
-                stream_range(p, g, 0, a[0], b[0]);
-                stream_range(p, g, 1, a[1], b[1]);
-                if (!mbar_wait(&bar_q_full, nq & 1, kWaitBudget)) { ok = false; break; }
-                ++nq;
-                any = true;
-                for (int j = g.j0; j <= g.j1 && ok; ++j) {
-                    const unsigned xk = x0 + 2 * (j - g.j0), xv = xk - 1;  // K of tile j, V of tile j - 1
-                    if (j < g.j1 && !mbar_wait(&bar_full[xk % S::slots], (xk / S::slots) & 1, kWaitBudget)) { ok = false; break; }
-                    if (j > g.j0 && !mbar_wait(&bar_full[xv % S::slots], (xv / S::slots) & 1, kWaitBudget)) { ok = false; break; }
-                    tc_fence_after();
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        if (j > a[i] && j <= b[i]) {  // O += P V of tile j - 1
-                            if (!mbar_wait(&bar_p[i], np[i] & 1, kWaitBudget)) { ok = false; break; }
-                            ++np[i];
-                            tc_fence_after();
-                            const uint32_t v_addr = kv_addr + (xv % S::slots) * S::tile_bytes;
-                            // keys past the sequence's last in steps of 16: the tail warp has cleared the rest of a step
-                            const int steps = min(kKeys / 16, (g.n - (j - 1) * kKeys + 15) / 16);
-                            for (int kk = 0; kk < steps; ++kk)
-                                umma_ts(tmem + S::col_o + i * D, tmem + i * 128 + kk * 8,
-                                        smem_desc(v_addr + kk * 2048, kHalfBytes, 1024, kSwizzle128B), id_o,
-                                        (j - 1 > a[i] || kk > 0) ? 1u : 0u);
-                            if (j == b[i]) umma_commit(&bar_o[i]);
-                        }
-                        if (i == 1 && j > g.j0) umma_commit(&bar_empty[xv % S::slots]);
-                        if (j >= a[i] && j < b[i]) {  // S = Q K^T of tile j
-                            const uint32_t k_addr = kv_addr + (xk % S::slots) * S::tile_bytes;
-#pragma unroll
-                            for (int kk = 0; kk < D / 16; ++kk) {
-                                const uint32_t off = (kk >> 2) * kHalfBytes + (kk & 3) * 32;
-                                umma_ss(tmem + i * 128, smem_desc(q_addr + i * S::tile_bytes + off, 16, 1024, kSwizzle128B),
-                                        smem_desc(k_addr + off, 16, 1024, kSwizzle128B), id_s, kk > 0 ? 1u : 0u);
-                            }
-                            umma_commit(&bar_s[i]);
-                        }
-                    }
-                    if (!ok) break;
-                    if (j < g.j1) umma_commit(&bar_empty[xk % S::slots]);
-                    if (j == g.j1 - 1) umma_commit(&bar_q_empty);
-                }
-                x0 += 2 * (g.j1 - g.j0);
-            }
-            if (!ok) raise_error(p.err, kErrTimeout);
-            if (any) {
-                umma_commit(&bar_drain);
-                if (!mbar_wait(&bar_drain, 0, kDrainBudget)) raise_error(p.err, kErrTimeout);
-            }
-        }
+    const uint32_t tmem = sh.tmem;
+    // the next job, for a warp that has had `nj` of them; false: no more (or a wait given up: ok is false then)
+    auto next_job = [&](unsigned& nj, Job& g, bool& ok) {
+        const int e = nj % kJobs;
+        ok = __all_sync(0xffffffffu, mbar_wait(&sh.job_full[e], (nj / kJobs) & 1, kWaitBudget));
+        if (!ok) return false;
+        g = sh.job[e];
         __syncwarp();
-    } else if (warp == kTailWarp) {
-        // ================= V rows past a sequence's last key; what this CTA leaves to the merge
-        unsigned x0 = 0, phase = 0;
-        int4 left = make_int4(0, 0, 0, 0);
-        bool ok = true;
-        while (walk.next(g)) {
-            if (!g.first) left.x |= kHasHead | (g.last ? kHeadEnds : 0);
-            if (g.first && !g.last) left = make_int4(left.x | kHasTail, g.s, g.h, g.t);
-            if (g.j1 <= g.j0) continue;
-            if (ok && g.j1 * kKeys > g.n) {
-                const unsigned x = x0 + 2 * (g.j1 - 1 - g.j0) + 1;
-                const int slot = x % S::slots;
-                if (!__all_sync(0xffffffffu, mbar_wait(&bar_raw[slot], (phase >> slot) & 1, kWaitBudget))) {
-                    ok = false;
-                } else {
-                    phase ^= 1u << slot;
-                    const int from = g.n - (g.j1 - 1) * kKeys, to = (from + 15) & ~15;  // the rest of a step of 16 keys
-                    for (int c = lane; c < (to - from) * 8 * S::halves; c += 32) {
-                        const int r = c % (8 * S::halves);
-                        *reinterpret_cast<uint4*>(sKV + slot * S::tile_bytes + (r >> 3) * kHalfBytes +
-                                                  (from + c / (8 * S::halves)) * 128 + (r & 7) * 16) = make_uint4(0, 0, 0, 0);
-                    }
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&bar_full[slot]);
-                }
-            }
-            x0 += 2 * (g.j1 - g.j0);
-        }
-        if (!ok && lane == 0) raise_error(p.err, kErrTimeout);
-        if (lane == 0) p.info[blockIdx.x] = left;
-    } else {
-        // ================= softmax of stream i: one row a thread
-        const int i = warp >> 2, quad = warp & 3;
-        const int r = quad * 32 + lane;
-        const uint32_t s_addr = tmem + (static_cast<uint32_t>(quad * 32) << 16) + i * 128;
-        const uint32_t o_addr = tmem + (static_cast<uint32_t>(quad * 32) << 16) + S::col_o + i * D;
+        if (lane == 0) mbar_arrive(&sh.job_empty[e]);
+        ++nj;
+        return g.s >= 0;
+    };
+
+    if (warp < kSoftmaxWarps) {
+        regs_inc<kSoftmaxRegs>();
+        // ================= softmax of stream i: two threads a row, each 64 of a tile's keys and half of O's columns.  The
+        // two warps that share 32 rows meet once a tile, with their halves' maxima (which also keeps one from writing P
+        // over scores that the other has yet to read), and go on with the same numbers.
+        const int i = warp >> 3, half = (warp >> 2) & 1, quad = warp & 3;
+        const int r = quad * 32 + lane, pair = i * 4 + quad;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+        const uint32_t s_addr = lanes + i * 128 + half * 64, p_addr = lanes + i * 128 + half * 32;
+        const uint32_t o_addr = lanes + S::col_o + i * D + half * (D / 2);
         const int my_tok = r / G, my_head = r - my_tok * G;
         unsigned ns = 0, no = 0;
         bool failed = false;
-        while (!failed && walk.next(g)) {
-            int a, b;
-            stream_range(p, g, i, a, b);
+        // what the other half has for this row, given what this one has; false: one of the two warps gave up a wait
+        // (the other warp has read the last tile's before this one writes: its weights were waited for since)
+        auto meet = [&](float mine, float& theirs) {
+            sh.row[i][half][r] = mine;
+            if (failed) sh.pair_failed[pair] = 1;
+            named_barrier(1 + pair, 64);
+            theirs = sh.row[i][half ^ 1][r];
+            return *const_cast<volatile int*>(&sh.pair_failed[pair]) == 0;
+        };
+        unsigned nj = 0;
+        Job g;
+        bool ok;
+        while (next_job(nj, g, ok)) {
+            const int a = g.a[i], b = g.b[i];
             const int tok = g.t * 2 * p.tokens + i * p.tokens + my_tok;
             const bool active = my_tok < p.tokens && tok < g.B;
             const int pos = g.n - g.B + tok;
@@ -497,36 +333,39 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
             const int lo = p.window > 0 ? max(0, pos + 1 - p.window) : 0;
             float m = -INFINITY, l = 0.f;
             for (int j = a; j < b; ++j, ++ns) {
-                if (!__all_sync(0xffffffffu, mbar_wait(&bar_s[i], ns & 1, kWaitBudget))) {
-                    failed = true;
-                    break;
-                }
+                failed = !__all_sync(0xffffffffu, mbar_wait(&sh.s[i], ns & 1, kWaitBudget));
                 tc_fence_after();
-                uint32_t x[4][32];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + c * 32, x[c]);
+                uint32_t x[2][32];
+                tmem_ld32(s_addr, x[0]);
+                tmem_ld32(s_addr + 32, x[1]);
                 tmem_ld_wait();
-                const int from = lo - j * kKeys, to = hi - j * kKeys;  // visible columns
-                if (!__all_sync(0xffffffffu, from <= 0 && to >= kKeys)) {
+                const int from = lo - j * kKeys - half * 64, to = hi - j * kKeys - half * 64;  // visible columns
+                if (!__all_sync(0xffffffffu, from <= 0 && to >= 64)) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
+                    for (int c = 0; c < 2; ++c)
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
                             if (c * 32 + e < from || c * 32 + e >= to) x[c][e] = 0xff800000u;  // -inf
                 }
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
+                for (int c = 0; c < 2; ++c)
 #pragma unroll
                     for (int e = 0; e < 32; e += 2)
                         mx[(e >> 1) & 3] = fmaxf(mx[(e >> 1) & 3], fmaxf(__uint_as_float(x[c][e]), __uint_as_float(x[c][e + 1])));
-                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
+                const float mine = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                float theirs;
+                if (!meet(mine, theirs)) {
+                    failed = true;
+                    break;
+                }
+                const float top = fmaxf(mine, theirs) * p.scale_log2;
                 const bool grew = top > m + 8.f;
                 const float alpha = grew ? chunk_exp2(m - top) : 1.f;
                 // (this tile's scores are complete, so the MMAs before them, the last P V among them, are too)
                 if (j > a && __any_sync(0xffffffffu, grew && m != -INFINITY)) {
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) {
+                    for (int c = 0; c < D / 32; ++c) {
                         uint32_t v[16];
                         tmem_ld16(o_addr + c * 16, v);
                         tmem_ld_wait();
@@ -543,7 +382,7 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
                 const uint64_t scale2 = pack_f32x2(p.scale_log2, p.scale_log2), negm2 = pack_f32x2(negm, negm);
                 uint64_t sum2[2] = {0ull, 0ull};
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
+                for (int c = 0; c < 2; ++c) {
                     uint32_t pk[16];
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
@@ -554,7 +393,7 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
                         sum2[e & 1] = add_f32x2(sum2[e & 1], pack_f32x2(u, w));
                         pk[e] = pack_bf16x2(u, w);  // bf16: the type of V, which P multiplies
                     }
-                    tmem_st16(s_addr + c * 16, pk);
+                    tmem_st16(p_addr + c * 16, pk);
                 }
                 float s0, s1, s2, s3;
                 unpack_f32x2(sum2[0], s0, s1);
@@ -562,23 +401,27 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
                 l += (s0 + s1) + (s2 + s3);
                 tmem_st_wait();
                 tc_fence_before();
-                mbar_arrive(&bar_p[i]);
+                mbar_arrive(&sh.p[i]);
             }
             if (failed) break;
             if (b > a) {
-                if (!__all_sync(0xffffffffu, mbar_wait(&bar_o[i], no & 1, kWaitBudget))) {
-                    failed = true;
-                    break;
-                }
+                failed = !__all_sync(0xffffffffu, mbar_wait(&sh.o[i], no & 1, kWaitBudget));
                 ++no;
                 tc_fence_after();
             }
+            float others;
+            if (!meet(l, others)) {
+                failed = true;
+                break;
+            }
+            named_barrier(1 + pair, 64);  // both have read it before the next job's first tile writes there
+            l = half ? others + l : l + others;
             const bool whole = g.first && g.last;
             const float inv = whole ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
             const size_t orow = (size_t)(g.q0 + tok) * p.num_q_heads + g.h * G + my_head;
             const size_t prow = ((size_t)blockIdx.x * 2 + (g.first ? 1 : 0)) * (2 * kTileM) + i * kTileM + r;
 #pragma unroll
-            for (int c = 0; c < D / 32; ++c) {
+            for (int c = 0; c < D / 64; ++c) {
                 uint32_t v[32];
                 if (b > a) {
                     tmem_ld32(o_addr + c * 32, v);
@@ -587,29 +430,274 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[e] = 0u;
                 }
+                const int col = half * (D / 2) + c * 32;
                 if (active && whole) {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8) {
-                        uint4 w;
-                        w.x = pack_bf16x2(__uint_as_float(v[e]) * inv, __uint_as_float(v[e + 1]) * inv);
-                        w.y = pack_bf16x2(__uint_as_float(v[e + 2]) * inv, __uint_as_float(v[e + 3]) * inv);
-                        w.z = pack_bf16x2(__uint_as_float(v[e + 4]) * inv, __uint_as_float(v[e + 5]) * inv);
-                        w.w = pack_bf16x2(__uint_as_float(v[e + 6]) * inv, __uint_as_float(v[e + 7]) * inv);
-                        *reinterpret_cast<uint4*>(p.o + orow * D + c * 32 + e) = w;
+                    for (int e = 0; e < 32; e += 16) {  // whole 32-byte sectors
+                        float w[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            w[k] = __uint_as_float(pack_bf16x2(__uint_as_float(v[e + 2 * k]) * inv, __uint_as_float(v[e + 2 * k + 1]) * inv));
+                        st_global_f32x8(reinterpret_cast<float*>(p.o + orow * D + col + e), w);
                     }
                 } else if (active) {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8) st_global_f32x8(p.part_o + prow * D + c * 32 + e, reinterpret_cast<const float*>(&v[e]));
+                    for (int e = 0; e < 32; e += 8) st_global_f32x8(p.part_o + prow * D + col + e, reinterpret_cast<const float*>(&v[e]));
                 }
                 __syncwarp();
             }
-            if (active) {
+            if (active && half == 0) {
                 if (!whole) p.part_ml[prow] = make_float2(m, l);
                 else if (p.lse) p.lse[orow] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
             }
             tc_fence_before();
         }
-        if (failed && lane == 0) raise_error(p.err, kErrTimeout);
+        if ((failed || !ok) && lane == 0) raise_error(p.err, kErrTimeout);
+    } else {
+        regs_dec<kOtherRegs>();
+        if (warp == kProducerWarp) {
+            // ================= this CTA's part of the line, laid out in jobs; their queries, then K and V tiles through
+            // the ring, K first
+            const Line line{p};
+            auto whole = [&](int s) -> long long {
+                if (s >= p.num_seqs) return 0;
+                const Seq q = line.seq(s);
+                return q.B > 0 ? q.cost(q.tiles()) * p.num_kv_heads : 0;
+            };
+            long long total = 0;
+            for (int base = 0; base < p.num_seqs; base += 32) {
+                long long w = whole(base + lane);
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
+                total += w;
+            }
+            const long long parts = min((long long)gridDim.x, max(1ll, total / kLeastCost));
+            const long long c = blockIdx.x;
+            // cuts at total * c / parts
+            const long long step = total / parts, rest = total % parts;
+            const long long cut[2] = {c * step + c * rest / parts, (c + 1) * step + (c + 1) * rest / parts};
+            Place place[2] = {Place{p.num_seqs, 0, 0, 0}, Place{p.num_seqs, 0, 0, 0}};
+            long long before = 0;
+            if (c < parts) {
+                for (int base = 0; base < p.num_seqs; base += 32) {
+                    const long long w = whole(base + lane);
+                    long long incl = w;
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) {
+                        const long long y = __shfl_up_sync(0xffffffffu, incl, o);
+                        if (lane >= o) incl += y;
+                    }
+                    incl += before;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const unsigned hit = __ballot_sync(0xffffffffu, w > 0 && incl - w <= cut[e] && cut[e] < incl);
+                        if (hit) {
+                            const int l = __ffs(hit) - 1;
+                            place[e] = line.within(base + l, cut[e] - __shfl_sync(0xffffffffu, incl - w, l));
+                        }
+                    }
+                    before = __shfl_sync(0xffffffffu, incl, 31);
+                }
+            }
+            Walk walk{p, place[0], place[1], -1, Seq{}, 0};
+            unsigned nj = 0;
+            bool ok = true;
+            // lays out the next job, or the end of them
+            auto lay_out = [&](Job& g) {
+                if (!walk.next(g)) g.s = -1;
+                const int e = nj % kJobs;
+                if (nj >= kJobs && !__all_sync(0xffffffffu, mbar_wait(&sh.job_empty[e], ((nj / kJobs) - 1) & 1, kWaitBudget))) {
+                    ok = false;
+                    return;
+                }
+                if (lane == 0) {
+                    sh.job[e] = g;
+                    mbar_arrive(&sh.job_full[e]);
+                }
+                ++nj;
+            };
+            const int rows = min(kKeys, 1 << p.page_shift);  // of a box
+            const int nbox = kKeys / rows;
+            const int box = lane / S::halves, half = lane % S::halves;
+            unsigned x = 0;  // ring position
+            int nq = 0;
+            unsigned on_raw = 0, raw_phase = 0;  // per slot: whether its last use is on raw; that barrier's uses, mod 2
+            Job g, after;
+            lay_out(g);
+            while (ok && g.s >= 0) {
+                lay_out(after);
+                if (!ok) break;
+                if (g.j1 > g.j0) {
+                    const int tok = g.t * 2 * p.tokens;
+                    if (nq > 0 && !__all_sync(0xffffffffu, mbar_wait(&sh.q_empty, (nq - 1) & 1, kWaitBudget))) {
+                        ok = false;
+                        break;
+                    }
+                    const bool two = tok + p.tokens < g.B;
+                    if (lane == 0) {
+                        const uint32_t bytes = (uint32_t)(p.tokens * G) * 128 * S::halves;
+                        mbar_arrive_expect_tx(&sh.q_full, two ? 2 * bytes : bytes);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            if (i == 0 || two)
+#pragma unroll
+                                for (int hh = 0; hh < S::halves; ++hh)
+                                    tma_load_3d(sQ + i * S::tile_bytes + hh * kHalfBytes, &qmap, &sh.q_full, 64 * hh, g.h * G,
+                                                g.q0 + tok + i * p.tokens);
+                    }
+                    ++nq;
+                    const int32_t* table = p.block_table + (size_t)g.s * p.pages_per_seq;
+                    const int last_page = (g.n - 1) >> p.page_shift;
+                    // the pool row of this lane's box of key tile j (-1: past the sequence's last page)
+                    auto pool_row = [&](int j) {
+                        const int key = j * kKeys + box * rows, pg = key >> p.page_shift;
+                        if (box >= nbox || pg > last_page) return -1;
+                        int id = pg < p.pages_per_seq ? __ldg(table + pg) : -1;
+                        if ((unsigned)id >= (unsigned)p.num_pages) {
+                            raise_error(p.err, kErrDeviceArg);
+                            id = 0;
+                        }
+                        return (id << p.page_shift) + (key & ((1 << p.page_shift) - 1));
+                    };
+                    int row = pool_row(g.j0);
+                    for (int j = g.j0; j < g.j1 && ok; ++j) {
+                        const int row_next = j + 1 < g.j1 ? pool_row(j + 1) : -1;
+                        const int boxes = min(nbox, ((g.n - j * kKeys) + rows - 1) / rows);
+#pragma unroll
+                        for (int kv = 0; kv < 2; ++kv, ++x) {
+                            const int slot = x % S::slots;
+                            const unsigned use = x / S::slots;
+                            if (use > 0 && !__all_sync(0xffffffffu, mbar_wait(&sh.empty[slot], (use - 1) & 1, kWaitBudget))) {
+                                ok = false;
+                                break;
+                            }
+                            // a V tile with rows past the last key goes through the tail warp
+                            const bool raw = kv == 1 && (j + 1) * kKeys > g.n;
+                            uint64_t* bar = raw ? &sh.raw[slot] : &sh.full[slot];
+                            on_raw = raw ? on_raw | 1u << slot : on_raw & ~(1u << slot);
+                            if (raw) raw_phase ^= 1u << slot;
+                            if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(boxes * rows) * 128 * S::halves);
+                            __syncwarp();
+                            if (row >= 0)
+                                tma_load_3d(sKV + slot * S::tile_bytes + half * kHalfBytes + box * rows * 128, kv ? &vmap : &kmap,
+                                            bar, 64 * half, g.h, row);
+                        }
+                        row = row_next;
+                    }
+                }
+                g = after;
+            }
+            if (!ok && lane == 0) raise_error(p.err, kErrTimeout);
+            // no copy may still be in flight when the CTA leaves
+            for (unsigned y = x > (unsigned)S::slots ? x - S::slots : 0; y < x; ++y) {
+                const int slot = y % S::slots;
+                const bool raw = on_raw >> slot & 1;
+                if (!mbar_wait(raw ? &sh.raw[slot] : &sh.full[slot], raw ? ~raw_phase >> slot & 1 : (y / S::slots) & 1, kDrainBudget) && lane == 0)
+                    raise_error(p.err, kErrTimeout);
+            }
+            if (nq > 0 && !mbar_wait(&sh.q_full, (nq - 1) & 1, kDrainBudget) && lane == 0) raise_error(p.err, kErrTimeout);
+        } else if (warp != kTailWarp) {
+            // ================= MMA issuer of stream i.  The streams take turns, a P V and a Q K^T at a time, each from a
+            // thread of its own: one waits for its operands and commits while the other's MMAs are issued
+            const int i = warp - kMmaWarp;
+            const uint32_t id_s = idesc_bf16_f32(kTileM, kKeys, false, false);
+            const uint32_t id_o = idesc_bf16_f32(kTileM, D, false, true);
+            // descriptors of this stream's Q tile, of the ring's first slot as K and as V; an offset adds its 16-byte units
+            const uint64_t q_desc = smem_desc(smem_addr(sQ) + i * S::tile_bytes, 16, 1024, kSwizzle128B);
+            const uint64_t k_desc = smem_desc(smem_addr(sKV), 16, 1024, kSwizzle128B);
+            const uint64_t v_desc = smem_desc(smem_addr(sKV), kHalfBytes, 1024, kSwizzle128B);
+            unsigned x = 0;  // ring position
+            unsigned nj = 0, np = 0, turn = 0;
+            int nq = 0;
+            bool ok, fine = true, any = false;
+            Job g;
+            while (next_job(nj, g, ok)) {
+                if (g.j1 <= g.j0) continue;
+                const int a = g.a[i], b = g.b[i];
+                if (lane == 0) {
+                    // this stream's arrival on `bar`: when its MMAs so far are done, or at once if it had none there
+                    auto release = [&](uint64_t* bar, bool used) {
+                        if (used) umma_commit(bar); else mbar_arrive(bar);
+                    };
+                    fine = mbar_wait(&sh.q_full, nq & 1, kWaitBudget);
+                    for (int j = g.j0; j <= g.j1 && fine; ++j, ++turn, x += 2) {  // x: K of tile j
+                        const int kslot = x % S::slots, vslot = (x - 1) % S::slots;
+                        const bool pv = j > a && j <= b, qk = j >= a && j < b;
+                        if (j < g.j1) fine = mbar_wait(&sh.full[kslot], (x / S::slots) & 1, kWaitBudget);
+                        if (fine && j > g.j0) fine = mbar_wait(&sh.full[vslot], ((x - 1) / S::slots) & 1, kWaitBudget);
+                        if (fine && pv) fine = mbar_wait(&sh.p[i], np++ & 1, kWaitBudget);
+                        if (fine) fine = mbar_wait(&sh.turn[i], (turn & 1) ^ (i ^ 1), kWaitBudget);
+                        if (!fine) break;
+                        tc_fence_after();
+                        if (pv) {  // O += P V of tile j - 1
+                            const uint64_t desc = v_desc + vslot * (S::tile_bytes >> 4);
+                            // keys past the sequence's last in steps of 16: the tail warp has cleared the rest of a step
+                            const int steps = min(kKeys / 16, (g.n - (j - 1) * kKeys + 15) / 16);
+#pragma unroll
+                            for (int kk = 0; kk < kKeys / 16; ++kk)
+                                if (kk < steps)
+                                    umma_ts(tmem + S::col_o + i * D, tmem + i * 128 + kk * 8, desc + kk * (2048 >> 4), id_o,
+                                            (j - 1 > a || kk > 0) ? 1u : 0u);
+                        }
+                        if (qk) {  // S = Q K^T of tile j
+                            const uint64_t desc = k_desc + kslot * (S::tile_bytes >> 4);
+#pragma unroll
+                            for (int kk = 0; kk < D / 16; ++kk) {
+                                const uint32_t off = (kk >> 2) * kHalfBytes + (kk & 3) * 32;
+                                umma_ss(tmem + i * 128, q_desc + (off >> 4), desc + (off >> 4), id_s, kk > 0 ? 1u : 0u);
+                            }
+                            any = true;
+                        }
+                        mbar_arrive(&sh.turn[i ^ 1]);
+                        if (qk) umma_commit(&sh.s[i]);
+                        if (pv && j == b) umma_commit(&sh.o[i]);
+                        if (j > g.j0) release(&sh.empty[vslot], pv);
+                        if (j < g.j1) release(&sh.empty[kslot], qk);
+                        if (j == g.j1 - 1) release(&sh.q_empty, any);
+                    }
+                    x -= 2;  // (the step behind the last tile has no K)
+                }
+                ++nq;
+                fine = __shfl_sync(0xffffffffu, fine ? 1 : 0, 0) != 0;
+                if (!fine) break;
+            }
+            if ((!fine || !ok) && lane == 0) raise_error(p.err, kErrTimeout);
+            if (lane == 0 && any) {
+                umma_commit(&sh.drain[i]);
+                if (!mbar_wait(&sh.drain[i], 0, kDrainBudget)) raise_error(p.err, kErrTimeout);
+            }
+            __syncwarp();
+        } else {
+            // ================= V rows past a sequence's last key; what this CTA leaves to the merge
+            unsigned x0 = 0, phase = 0, nj = 0;
+            int4 left = make_int4(0, 0, 0, 0);
+            bool ok, fine = true;
+            Job g;
+            while (next_job(nj, g, ok)) {
+                if (!g.first) left.x |= kHasHead | (g.last ? kHeadEnds : 0);
+                if (g.first && !g.last) left = make_int4(left.x | kHasTail, g.s, g.h, g.t);
+                if (g.j1 <= g.j0) continue;
+                if (g.j1 * kKeys > g.n) {
+                    const unsigned x = x0 + 2 * (g.j1 - 1 - g.j0) + 1;
+                    const int slot = x % S::slots;
+                    fine = __all_sync(0xffffffffu, mbar_wait(&sh.raw[slot], (phase >> slot) & 1, kWaitBudget));
+                    if (!fine) break;
+                    phase ^= 1u << slot;
+                    const int from = g.n - (g.j1 - 1) * kKeys, to = (from + 15) & ~15;  // the rest of a step of 16 keys
+                    for (int c = lane; c < (to - from) * 8 * S::halves; c += 32) {
+                        const int r = c % (8 * S::halves);
+                        *reinterpret_cast<uint4*>(sKV + slot * S::tile_bytes + (r >> 3) * kHalfBytes +
+                                                  (from + c / (8 * S::halves)) * 128 + (r & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.full[slot]);
+                }
+                x0 += 2 * (g.j1 - g.j0);
+            }
+            if ((!fine || !ok) && lane == 0) raise_error(p.err, kErrTimeout);
+            if (lane == 0) p.info[blockIdx.x] = left;
+        }
     }
     tc_fence_before();
     __syncthreads();
@@ -718,7 +806,7 @@ int run(const ChunkAttentionArgs& a, const DeviceInfo& dev, cudaStream_t stream)
     {
         std::lock_guard<std::mutex> lock(mu);
         if (!configured[dev.device]) {
-            if (cudaFuncSetAttribute(chunk_attention_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::smem) != cudaSuccess)
+            if (cudaFuncSetAttribute(chunk_attention_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, chunk_smem<D>()) != cudaSuccess)
                 return BP_ERR_CUDA;
             configured[dev.device] = true;
         }
@@ -729,7 +817,7 @@ int run(const ChunkAttentionArgs& a, const DeviceInfo& dev, cudaStream_t stream)
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.gridDim = dim3((unsigned)grid, 1, 1);
     cfg.blockDim = dim3(kChunkThreads, 1, 1);
-    cfg.dynamicSmemBytes = S::smem;
+    cfg.dynamicSmemBytes = chunk_smem<D>();
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
