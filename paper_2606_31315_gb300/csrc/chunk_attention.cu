@@ -67,12 +67,19 @@ struct ChunkParams {
     int pages_per_seq, page_shift, num_pages;
     int causal, window;
     float scale_log2;
-    float* part_o;   // [grid][2][256][D]: the first stretch's part (it began in an earlier CTA) and the last one's
+    float* part_o;   // [grid][2][D / 8][256][8] (part_at): the first stretch's part (it began in an earlier CTA) and the last one's
     float2* part_ml; // [grid][2][256]
     int4* info;      // [grid]: flags, and the sequence, head and tile that the CTA began and did not end
     unsigned int* err;
 };
 enum : int { kHasTail = 1, kHasHead = 2, kHeadEnds = 4 };
+
+// Where column `col` (a multiple of 8) of row `row` of a part lies: 8 columns of all rows together, so that the threads of
+// a warp, a row each, write whole lines.
+template <int D>
+__device__ __forceinline__ size_t part_at(size_t slot, int row, int col) {
+    return ((slot * (D / 8) + col / 8) * (2 * kTileM) + row) * 8;
+}
 
 __device__ __forceinline__ float chunk_exp2(float x) {
     float y;
@@ -228,7 +235,7 @@ template <int SLOTS>
 struct Shared {
     uint64_t full[SLOTS], empty[SLOTS], raw[SLOTS];  // the ring; raw: a V tile that the tail warp hands on
     uint64_t q_full, q_empty, drain[2], turn[2];
-    uint64_t s[2], p[2], o[2];                       // of a stream: scores, weights, the accumulator
+    uint64_t s[2], p[2][2], o[2];                    // of a stream: scores, weights (two parts), the accumulator
     uint64_t job_full[kJobs], job_empty[kJobs];
     Job job[kJobs];                                  // what the producer warp has laid out for the others
     uint32_t tmem;
@@ -264,7 +271,8 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.s[i], 1);
-            mbar_init(&sh.p[i], 256);
+            mbar_init(&sh.p[i][0], 256);
+            mbar_init(&sh.p[i][1], 256);
             mbar_init(&sh.o[i], 1);
             mbar_init(&sh.drain[i], 1);
             mbar_init(&sh.turn[i], 1);
@@ -302,12 +310,12 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
     if (warp < kSoftmaxWarps) {
         regs_inc<kSoftmaxRegs>();
         // ================= softmax of stream i: two threads a row, each 64 of a tile's keys and half of O's columns.  The
-        // two warps that share 32 rows meet once a tile, with their halves' maxima (which also keeps one from writing P
-        // over scores that the other has yet to read), and go on with the same numbers.
+        // two warps that share 32 rows ask each other once a tile whether a row of theirs has outgrown its maximum; where
+        // one has, they exchange their halves' maxima and go on with the same numbers.
         const int i = warp >> 3, half = (warp >> 2) & 1, quad = warp & 3;
         const int r = quad * 32 + lane, pair = i * 4 + quad;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
-        const uint32_t s_addr = lanes + i * 128 + half * 64, p_addr = lanes + i * 128 + half * 32;
+        const uint32_t s_addr = lanes + i * 128 + half * 64;  // P comes over this half's own scores
         const uint32_t o_addr = lanes + S::col_o + i * D + half * (D / 2);
         const int my_tok = r / G, my_head = r - my_tok * G;
         unsigned ns = 0, no = 0;
@@ -323,8 +331,8 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
         };
         unsigned nj = 0;
         Job g;
-        bool ok;
-        while (next_job(nj, g, ok)) {
+        bool ok, more = next_job(nj, g, ok);
+        while (more) {
             const int a = g.a[i], b = g.b[i];
             const int tok = g.t * 2 * p.tokens + i * p.tokens + my_tok;
             const bool active = my_tok < p.tokens && tok < g.B;
@@ -333,50 +341,58 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
             const int lo = p.window > 0 ? max(0, pos + 1 - p.window) : 0;
             float m = -INFINITY, l = 0.f;
             for (int j = a; j < b; ++j, ++ns) {
+                const int from = lo - j * kKeys - half * 64, to = hi - j * kKeys - half * 64;  // visible columns
+                const bool full = __all_sync(0xffffffffu, from <= 0 && to >= 64);
                 failed = !__all_sync(0xffffffffu, mbar_wait(&sh.s[i], ns & 1, kWaitBudget));
                 tc_fence_after();
                 uint32_t x[2][32];
-                tmem_ld32(s_addr, x[0]);
-                tmem_ld32(s_addr + 32, x[1]);
-                tmem_ld_wait();
-                const int from = lo - j * kKeys - half * 64, to = hi - j * kKeys - half * 64;  // visible columns
-                if (!__all_sync(0xffffffffu, from <= 0 && to >= 64)) {
+                float mine;
+                if (full) {
+                    float m0, m1;
+                    tmem_ld32_max(s_addr, x[0], m0);
+                    tmem_ld32_max(s_addr + 32, x[1], m1);
+                    tmem_ld_wait();
+                    mine = fmaxf(m0, m1);
+                } else {
+                    tmem_ld32(s_addr, x[0]);
+                    tmem_ld32(s_addr + 32, x[1]);
+                    tmem_ld_wait();
+                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
+                        for (int e = 0; e < 32; ++e) {
                             if (c * 32 + e < from || c * 32 + e >= to) x[c][e] = 0xff800000u;  // -inf
+                            mx[e & 3] = fmaxf(mx[e & 3], __uint_as_float(x[c][e]));
+                        }
+                    mine = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                 }
-                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                for (int c = 0; c < 2; ++c)
-#pragma unroll
-                    for (int e = 0; e < 32; e += 2)
-                        mx[(e >> 1) & 3] = fmaxf(mx[(e >> 1) & 3], fmaxf(__uint_as_float(x[c][e]), __uint_as_float(x[c][e + 1])));
-                const float mine = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-                float theirs;
-                if (!meet(mine, theirs)) {
-                    failed = true;
-                    break;
-                }
-                const float top = fmaxf(mine, theirs) * p.scale_log2;
-                const bool grew = top > m + 8.f;
-                const float alpha = grew ? chunk_exp2(m - top) : 1.f;
-                // (this tile's scores are complete, so the MMAs before them, the last P V among them, are too)
-                if (j > a && __any_sync(0xffffffffu, grew && m != -INFINITY)) {
-#pragma unroll
-                    for (int c = 0; c < D / 32; ++c) {
-                        uint32_t v[16];
-                        tmem_ld16(o_addr + c * 16, v);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * alpha);
-                        tmem_st16(o_addr + c * 16, v);
+                // (m is the same in both warps; with it 2^(score - m) stays below 2^8)
+                if (named_barrier_or(1 + pair, 64, failed || mine * p.scale_log2 > m + 8.f)) {
+                    float theirs;
+                    if (!meet(mine, theirs)) {
+                        failed = true;
+                        break;
                     }
-                }
-                if (grew) {
-                    l *= alpha;
-                    m = top;
+                    const float top = fmaxf(mine, theirs) * p.scale_log2;
+                    const bool grew = top > m + 8.f;
+                    const float alpha = grew ? chunk_exp2(m - top) : 1.f;
+                    // (this tile's scores are complete, so the MMAs before them, the last P V among them, are too)
+                    if (j > a && __any_sync(0xffffffffu, grew && m != -INFINITY)) {
+#pragma unroll
+                        for (int c = 0; c < D / 32; ++c) {
+                            uint32_t v[16];
+                            tmem_ld16(o_addr + c * 16, v);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * alpha);
+                            tmem_st16(o_addr + c * 16, v);
+                        }
+                    }
+                    if (grew) {
+                        l *= alpha;
+                        m = top;
+                    }
                 }
                 const float negm = m == -INFINITY ? 0.f : -m;
                 const uint64_t scale2 = pack_f32x2(p.scale_log2, p.scale_log2), negm2 = pack_f32x2(negm, negm);
@@ -393,17 +409,20 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
                         sum2[e & 1] = add_f32x2(sum2[e & 1], pack_f32x2(u, w));
                         pk[e] = pack_bf16x2(u, w);  // bf16: the type of V, which P multiplies
                     }
-                    tmem_st16(p_addr + c * 16, pk);
+                    tmem_st16(s_addr + c * 16, pk);
+                    // the MMAs of the first 32 keys of both halves begin while the weights of the others are formed
+                    tmem_st_wait();
+                    tc_fence_before();
+                    mbar_arrive(&sh.p[i][c]);
                 }
                 float s0, s1, s2, s3;
                 unpack_f32x2(sum2[0], s0, s1);
                 unpack_f32x2(sum2[1], s2, s3);
                 l += (s0 + s1) + (s2 + s3);
-                tmem_st_wait();
-                tc_fence_before();
-                mbar_arrive(&sh.p[i]);
             }
             if (failed) break;
+            const Job done = g;
+            more = next_job(nj, g, ok);  // while the last P V runs
             if (b > a) {
                 failed = !__all_sync(0xffffffffu, mbar_wait(&sh.o[i], no & 1, kWaitBudget));
                 ++no;
@@ -416,10 +435,12 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
             }
             named_barrier(1 + pair, 64);  // both have read it before the next job's first tile writes there
             l = half ? others + l : l + others;
-            const bool whole = g.first && g.last;
+            const bool whole = done.first && done.last;
             const float inv = whole ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
-            const size_t orow = (size_t)(g.q0 + tok) * p.num_q_heads + g.h * G + my_head;
-            const size_t prow = ((size_t)blockIdx.x * 2 + (g.first ? 1 : 0)) * (2 * kTileM) + i * kTileM + r;
+            const size_t orow = (size_t)(done.q0 + tok) * p.num_q_heads + done.h * G + my_head;
+            const size_t slot = (size_t)blockIdx.x * 2 + (done.first ? 1 : 0);
+            // the row's address for the lanes of this group of four that store a piece of it
+            const unsigned long long out = active ? reinterpret_cast<unsigned long long>(p.o + orow * D + half * (D / 2)) : 0ull;
 #pragma unroll
             for (int c = 0; c < D / 64; ++c) {
                 uint32_t v[32];
@@ -430,24 +451,39 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[e] = 0u;
                 }
-                const int col = half * (D / 2) + c * 32;
-                if (active && whole) {
+                if (whole) {
+                    // 4 lanes' 4 pieces of 8 columns (16 bytes) transposed among them, so that a store's 4 lanes write 64
+                    // consecutive bytes of one row: 8 lines a store instead of 32
+                    uint32_t w[4][4];
 #pragma unroll
-                    for (int e = 0; e < 32; e += 16) {  // whole 32-byte sectors
-                        float w[8];
+                    for (int k = 0; k < 16; ++k)
+                        w[k >> 2][k & 3] = pack_bf16x2(__uint_as_float(v[2 * k]) * inv, __uint_as_float(v[2 * k + 1]) * inv);
 #pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            w[k] = __uint_as_float(pack_bf16x2(__uint_as_float(v[e + 2 * k]) * inv, __uint_as_float(v[e + 2 * k + 1]) * inv));
-                        st_global_f32x8(reinterpret_cast<float*>(p.o + orow * D + col + e), w);
+                    for (int o = 1; o < 4; o <<= 1)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (!(k & o)) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const bool up = lane & o;
+                                    const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? w[k][e] : w[k | o][e], o);
+                                    if (up) w[k][e] = got; else w[k | o][e] = got;
+                                }
+                            }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {  // piece lane & 3 of the row of lane (lane & ~3) + k
+                        const unsigned long long at = __shfl_sync(0xffffffffu, out, (lane & ~3) + k);
+                        if (at) *reinterpret_cast<uint4*>(at + c * 64 + (lane & 3) * 16) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
                     }
                 } else if (active) {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8) st_global_f32x8(p.part_o + prow * D + col + e, reinterpret_cast<const float*>(&v[e]));
+                    for (int e = 0; e < 32; e += 8)
+                        st_global_f32x8(p.part_o + part_at<D>(slot, i * kTileM + r, half * (D / 2) + c * 32 + e), reinterpret_cast<const float*>(&v[e]));
                 }
                 __syncwarp();
             }
             if (active && half == 0) {
-                if (!whole) p.part_ml[prow] = make_float2(m, l);
+                if (!whole) p.part_ml[slot * (2 * kTileM) + i * kTileM + r] = make_float2(m, l);
                 else if (p.lse) p.lse[orow] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
             }
             tc_fence_before();
@@ -625,7 +661,7 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
                         const bool pv = j > a && j <= b, qk = j >= a && j < b;
                         if (j < g.j1) fine = mbar_wait(&sh.full[kslot], (x / S::slots) & 1, kWaitBudget);
                         if (fine && j > g.j0) fine = mbar_wait(&sh.full[vslot], ((x - 1) / S::slots) & 1, kWaitBudget);
-                        if (fine && pv) fine = mbar_wait(&sh.p[i], np++ & 1, kWaitBudget);
+                        if (fine && pv) fine = mbar_wait(&sh.p[i][0], np & 1, kWaitBudget);
                         if (fine) fine = mbar_wait(&sh.turn[i], (turn & 1) ^ (i ^ 1), kWaitBudget);
                         if (!fine) break;
                         tc_fence_after();
@@ -633,11 +669,24 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
                             const uint64_t desc = v_desc + vslot * (S::tile_bytes >> 4);
                             // keys past the sequence's last in steps of 16: the tail warp has cleared the rest of a step
                             const int steps = min(kKeys / 16, (g.n - (j - 1) * kKeys + 15) / 16);
+                            // (P: the first 32 keys of either half, then the others; key step kk at column 8 kk of its half)
 #pragma unroll
-                            for (int kk = 0; kk < kKeys / 16; ++kk)
-                                if (kk < steps)
-                                    umma_ts(tmem + S::col_o + i * D, tmem + i * 128 + kk * 8, desc + kk * (2048 >> 4), id_o,
-                                            (j - 1 > a || kk > 0) ? 1u : 0u);
+                            for (int part = 0; part < 2; ++part) {
+                                if (part == 1) {
+                                    fine = mbar_wait(&sh.p[i][1], np & 1, kWaitBudget);
+                                    if (!fine) break;
+                                    tc_fence_after();
+                                }
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) {
+                                    const int kk = (k >> 1) * 4 + part * 2 + (k & 1);
+                                    if (kk < steps)
+                                        umma_ts(tmem + S::col_o + i * D, tmem + i * 128 + (kk >> 2) * 64 + (kk & 3) * 8,
+                                                desc + kk * (2048 >> 4), id_o, (j - 1 > a || kk > 0) ? 1u : 0u);
+                                }
+                            }
+                            ++np;
+                            if (!fine) break;
                         }
                         if (qk) {  // S = Q K^T of tile j
                             const uint64_t desc = k_desc + kslot * (S::tile_bytes >> 4);
@@ -707,15 +756,15 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
     }
 }
 
-// Merges the parts of every work tile that was cut: block (c, y) the rows [32 y, 32 y + 32) of the tile that CTA c
-// began and did not end.  Its parts are c's last and the first ones of the CTAs behind it, up to the one that ends it.
-// A row is one warp's: 4 rows a warp.
-constexpr int kMergeRows = 32, kMergeThreads = 256;
+// Merges the parts of every work tile that was cut: block (c, y) 32 rows of the tile that CTA c began and did not end.
+// Its parts are c's last and the first ones of the CTAs behind it, up to the one that ends it.  A thread has 8 columns of
+// a row; a warp 32 rows' (a part's lines are read whole).
+constexpr int kMergeRows = 32;
 template <int D>
-__global__ void __launch_bounds__(kMergeThreads) chunk_merge_kernel(const ChunkParams p, int grid) {
+__global__ void __launch_bounds__(kMergeRows * D / 8) chunk_merge_kernel(const ChunkParams p, int grid) {
     griddep_launch_dependents();
     griddep_wait();
-    const int c = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int c = blockIdx.x, lane = threadIdx.x & 31, col = (threadIdx.x >> 5) * 8;
     const int4 mine = p.info[c];
     if (!(mine.x & kHasTail)) return;
     const int q0 = p.cu_q[mine.y], B = p.cu_q[mine.y + 1] - q0;
@@ -727,30 +776,30 @@ __global__ void __launch_bounds__(kMergeThreads) chunk_merge_kernel(const ChunkP
             break;
         }
     }
-    constexpr int kPer = D / 32;
-    for (int k = 0; k < kMergeRows / 8; ++k) {
-        const int row = blockIdx.y * kMergeRows + k * 8 + warp;
-        const int i = row / kTileM, r = row % kTileM, tok = mine.w * 2 * p.tokens + i * p.tokens + r / p.group;
-        if (r / p.group >= p.tokens || tok >= B) continue;
-        float acc[kPer] = {}, m = -INFINITY, l = 0.f;
-        for (int e = c; e <= last; ++e) {
-            const size_t prow = ((size_t)e * 2 + (e == c ? 1 : 0)) * (2 * kTileM) + row;
-            if (e > c && !(p.info[e].x & kHasHead)) continue;
-            const float2 ml = p.part_ml[prow];
-            if (!(ml.y > 0.f)) continue;
-            const float m_new = fmaxf(m, ml.x), w_old = chunk_exp2(m - m_new), w = chunk_exp2(ml.x - m_new);
-            l = l * w_old + ml.y * w;
+    const int row = blockIdx.y * kMergeRows + lane;
+    const int i = row / kTileM, r = row % kTileM, tok = mine.w * 2 * p.tokens + i * p.tokens + r / p.group;
+    if (r / p.group >= p.tokens || tok >= B) return;
+    float acc[8] = {}, m = -INFINITY, l = 0.f;
+    for (int e = c; e <= last; ++e) {
+        const size_t slot = (size_t)e * 2 + (e == c ? 1 : 0);
+        if (e > c && !(p.info[e].x & kHasHead)) continue;
+        const float2 ml = p.part_ml[slot * (2 * kTileM) + row];
+        if (!(ml.y > 0.f)) continue;
+        const float4* o = reinterpret_cast<const float4*>(p.part_o + part_at<D>(slot, row, col));
+        const float4 o0 = o[0], o1 = o[1];
+        const float v[8] = {o0.x, o0.y, o0.z, o0.w, o1.x, o1.y, o1.z, o1.w};
+        const float m_new = fmaxf(m, ml.x), w_old = chunk_exp2(m - m_new), w = chunk_exp2(ml.x - m_new);
+        l = l * w_old + ml.y * w;
 #pragma unroll
-            for (int d = 0; d < kPer; ++d) acc[d] = acc[d] * w_old + p.part_o[prow * D + lane * kPer + d] * w;
-            m = m_new;
-        }
-        const float inv = l > 0.f ? 1.f / l : 0.f;
-        const size_t orow = (size_t)(q0 + tok) * p.num_q_heads + mine.z * p.group + r % p.group;
-#pragma unroll
-        for (int d = 0; d < kPer; d += 2)
-            *reinterpret_cast<uint32_t*>(p.o + orow * D + lane * kPer + d) = pack_bf16x2(acc[d] * inv, acc[d + 1] * inv);
-        if (p.lse && lane == 0) p.lse[orow] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        for (int d = 0; d < 8; ++d) acc[d] = acc[d] * w_old + v[d] * w;
+        m = m_new;
     }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const size_t orow = (size_t)(q0 + tok) * p.num_q_heads + mine.z * p.group + r % p.group;
+    *reinterpret_cast<uint4*>(p.o + orow * D + col) =
+        make_uint4(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv),
+                   pack_bf16x2(acc[4] * inv, acc[5] * inv), pack_bf16x2(acc[6] * inv, acc[7] * inv));
+    if (p.lse && col == 0) p.lse[orow] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
 template <int D>
@@ -823,7 +872,7 @@ int run(const ChunkAttentionArgs& a, const DeviceInfo& dev, cudaStream_t stream)
     cfg.numAttrs = 1;
     if (cudaLaunchKernelEx(&cfg, chunk_attention_kernel<D>, p, qmap, kmap, vmap) != cudaSuccess) return BP_ERR_CUDA;
     cfg.gridDim = dim3((unsigned)grid, 2 * kTileM / kMergeRows, 1);
-    cfg.blockDim = dim3(kMergeThreads, 1, 1);
+    cfg.blockDim = dim3(kMergeRows * D / 8, 1, 1);
     cfg.dynamicSmemBytes = 0;
     return cudaLaunchKernelEx(&cfg, chunk_merge_kernel<D>, p, grid) == cudaSuccess ? BP_OK : BP_ERR_CUDA;
 }
