@@ -235,7 +235,7 @@ template <int SLOTS>
 struct Shared {
     uint64_t full[SLOTS], empty[SLOTS], raw[SLOTS];  // the ring; raw: a V tile that the tail warp hands on
     uint64_t q_full, q_empty, drain[2], turn[2];
-    uint64_t s[2], p[2][2], o[2];                    // of a stream: scores, weights (two parts), the accumulator
+    uint64_t s[2], p[2], o[2];                       // of a stream: scores, weights, the accumulator
     uint64_t job_full[kJobs], job_empty[kJobs];
     Job job[kJobs];                                  // what the producer warp has laid out for the others
     uint32_t tmem;
@@ -271,8 +271,7 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sh.s[i], 1);
-            mbar_init(&sh.p[i][0], 256);
-            mbar_init(&sh.p[i][1], 256);
+            mbar_init(&sh.p[i], 256);
             mbar_init(&sh.o[i], 1);
             mbar_init(&sh.drain[i], 1);
             mbar_init(&sh.turn[i], 1);
@@ -410,11 +409,10 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
                         pk[e] = pack_bf16x2(u, w);  // bf16: the type of V, which P multiplies
                     }
                     tmem_st16(s_addr + c * 16, pk);
-                    // the MMAs of the first 32 keys of both halves begin while the weights of the others are formed
-                    tmem_st_wait();
-                    tc_fence_before();
-                    mbar_arrive(&sh.p[i][c]);
                 }
+                tmem_st_wait();
+                tc_fence_before();
+                mbar_arrive(&sh.p[i]);
                 float s0, s1, s2, s3;
                 unpack_f32x2(sum2[0], s0, s1);
                 unpack_f32x2(sum2[1], s2, s3);
@@ -634,14 +632,22 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
             if (nq > 0 && !mbar_wait(&sh.q_full, (nq - 1) & 1, kDrainBudget) && lane == 0) raise_error(p.err, kErrTimeout);
         } else if (warp != kTailWarp) {
             // ================= MMA issuer of stream i.  The streams take turns, a P V and a Q K^T at a time, each from a
-            // thread of its own: one waits for its operands and commits while the other's MMAs are issued
+            // warp of its own: one waits for its operands and commits while the other's MMAs are issued
             const int i = warp - kMmaWarp;
             const uint32_t id_s = idesc_bf16_f32(kTileM, kKeys, false, false);
             const uint32_t id_o = idesc_bf16_f32(kTileM, D, false, true);
-            // descriptors of this stream's Q tile, of the ring's first slot as K and as V; an offset adds its 16-byte units
-            const uint64_t q_desc = smem_desc(smem_addr(sQ) + i * S::tile_bytes, 16, 1024, kSwizzle128B);
-            const uint64_t k_desc = smem_desc(smem_addr(sKV), 16, 1024, kSwizzle128B);
-            const uint64_t v_desc = smem_desc(smem_addr(sKV), kHalfBytes, 1024, kSwizzle128B);
+            // descriptors of this stream's Q tile, of the ring's first slot as K and as V: their upper halves are constant,
+            // an offset adds its 16-byte units to the lower ones
+            const uint64_t upper = smem_desc(0, 0, 1024, kSwizzle128B);
+            const uint32_t q_lo = (uint32_t)smem_desc(smem_addr(sQ) + i * S::tile_bytes, 16, 0, 0);
+            const uint32_t k_lo = (uint32_t)smem_desc(smem_addr(sKV), 16, 0, 0);
+            const uint32_t v_lo = (uint32_t)smem_desc(smem_addr(sKV), kHalfBytes, 0, 0);
+            const uint32_t t_s = tmem + i * 128, t_o = tmem + S::col_o + i * D;
+            auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, kWaitBudget)) != 0; };
+            // this stream's arrival on `bar`: when its MMAs so far are done, or at once if it had none there
+            auto release = [&](uint64_t* bar, bool used) {
+                if (used) umma_commit(bar); else mbar_arrive(bar);
+            };
             unsigned x = 0;  // ring position
             unsigned nj = 0, np = 0, turn = 0;
             int nq = 0;
@@ -650,68 +656,54 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
             while (next_job(nj, g, ok)) {
                 if (g.j1 <= g.j0) continue;
                 const int a = g.a[i], b = g.b[i];
-                if (lane == 0) {
-                    // this stream's arrival on `bar`: when its MMAs so far are done, or at once if it had none there
-                    auto release = [&](uint64_t* bar, bool used) {
-                        if (used) umma_commit(bar); else mbar_arrive(bar);
-                    };
-                    fine = mbar_wait(&sh.q_full, nq & 1, kWaitBudget);
-                    for (int j = g.j0; j <= g.j1 && fine; ++j, ++turn, x += 2) {  // x: K of tile j
-                        const int kslot = x % S::slots, vslot = (x - 1) % S::slots;
-                        const bool pv = j > a && j <= b, qk = j >= a && j < b;
-                        if (j < g.j1) fine = mbar_wait(&sh.full[kslot], (x / S::slots) & 1, kWaitBudget);
-                        if (fine && j > g.j0) fine = mbar_wait(&sh.full[vslot], ((x - 1) / S::slots) & 1, kWaitBudget);
-                        if (fine && pv) fine = mbar_wait(&sh.p[i][0], np & 1, kWaitBudget);
-                        if (fine) fine = mbar_wait(&sh.turn[i], (turn & 1) ^ (i ^ 1), kWaitBudget);
-                        if (!fine) break;
-                        tc_fence_after();
-                        if (pv) {  // O += P V of tile j - 1
-                            const uint64_t desc = v_desc + vslot * (S::tile_bytes >> 4);
-                            // keys past the sequence's last in steps of 16: the tail warp has cleared the rest of a step
-                            const int steps = min(kKeys / 16, (g.n - (j - 1) * kKeys + 15) / 16);
-                            // (P: the first 32 keys of either half, then the others; key step kk at column 8 kk of its half)
+                fine = wait(&sh.q_full, nq & 1);
+                for (int j = g.j0; j <= g.j1 && fine; ++j, ++turn, x += 2) {  // x: K of tile j
+                    const int kslot = x % S::slots, vslot = (x - 1) % S::slots;
+                    const bool pv = j > a && j <= b, qk = j >= a && j < b;
+                    if (j < g.j1) fine = wait(&sh.full[kslot], (x / S::slots) & 1);
+                    if (fine && j > g.j0) fine = wait(&sh.full[vslot], ((x - 1) / S::slots) & 1);
+                    if (fine && pv) fine = wait(&sh.p[i], np++ & 1);
+                    if (fine) fine = wait(&sh.turn[i], (turn & 1) ^ (i ^ 1));
+                    if (!fine) break;
+                    tc_fence_after();
+                    // keys past the sequence's last in steps of 16: the tail warp has cleared the rest of a step
+                    const int steps = pv ? min(kKeys / 16, (g.n - (j - 1) * kKeys + 15) / 16) : 0;
+                    const uint32_t vl = v_lo + vslot * (S::tile_bytes >> 4), kl = k_lo + kslot * (S::tile_bytes >> 4);
+                    uint32_t on = j - 1 > a ? 1u : 0u;
+                    if (elect_one()) {
+                        if (pv) {  // O += P V of tile j - 1 (P's 64-key halves lie 64 columns apart)
 #pragma unroll
-                            for (int part = 0; part < 2; ++part) {
-                                if (part == 1) {
-                                    fine = mbar_wait(&sh.p[i][1], np & 1, kWaitBudget);
-                                    if (!fine) break;
-                                    tc_fence_after();
-                                }
-#pragma unroll
-                                for (int k = 0; k < 4; ++k) {
-                                    const int kk = (k >> 1) * 4 + part * 2 + (k & 1);
-                                    if (kk < steps)
-                                        umma_ts(tmem + S::col_o + i * D, tmem + i * 128 + (kk >> 2) * 64 + (kk & 3) * 8,
-                                                desc + kk * (2048 >> 4), id_o, (j - 1 > a || kk > 0) ? 1u : 0u);
-                                }
+                            for (int kk = 0; kk < kKeys / 16; ++kk) {
+                                if (kk < steps)
+                                    umma_ts(t_o, t_s + (kk >> 2) * 64 + (kk & 3) * 8, upper | (vl + kk * (2048 >> 4)), id_o, on);
+                                on = 1;
                             }
-                            ++np;
-                            if (!fine) break;
                         }
                         if (qk) {  // S = Q K^T of tile j
-                            const uint64_t desc = k_desc + kslot * (S::tile_bytes >> 4);
+                            on = 0;
 #pragma unroll
                             for (int kk = 0; kk < D / 16; ++kk) {
-                                const uint32_t off = (kk >> 2) * kHalfBytes + (kk & 3) * 32;
-                                umma_ss(tmem + i * 128, q_desc + (off >> 4), desc + (off >> 4), id_s, kk > 0 ? 1u : 0u);
+                                const uint32_t off = ((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4;
+                                umma_ss(t_s, upper | (q_lo + off), upper | (kl + off), id_s, on);
+                                on = 1;
                             }
-                            any = true;
                         }
                         mbar_arrive(&sh.turn[i ^ 1]);
                         if (qk) umma_commit(&sh.s[i]);
                         if (pv && j == b) umma_commit(&sh.o[i]);
                         if (j > g.j0) release(&sh.empty[vslot], pv);
                         if (j < g.j1) release(&sh.empty[kslot], qk);
-                        if (j == g.j1 - 1) release(&sh.q_empty, any);
+                        if (j == g.j1 - 1) release(&sh.q_empty, any || qk);
                     }
-                    x -= 2;  // (the step behind the last tile has no K)
+                    __syncwarp();
+                    any = any || qk;
                 }
+                x -= 2;  // (the step behind the last tile has no K)
                 ++nq;
-                fine = __shfl_sync(0xffffffffu, fine ? 1 : 0, 0) != 0;
                 if (!fine) break;
             }
             if ((!fine || !ok) && lane == 0) raise_error(p.err, kErrTimeout);
-            if (lane == 0 && any) {
+            if (any && elect_one()) {
                 umma_commit(&sh.drain[i]);
                 if (!mbar_wait(&sh.drain[i], 0, kDrainBudget)) raise_error(p.err, kErrTimeout);
             }
