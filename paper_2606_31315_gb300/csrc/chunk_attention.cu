@@ -671,11 +671,17 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
                     const uint32_t vl = v_lo + vslot * (S::tile_bytes >> 4), kl = k_lo + kslot * (S::tile_bytes >> 4);
                     uint32_t on = j - 1 > a ? 1u : 0u;
                     if (elect_one()) {
-                        if (pv) {  // O += P V of tile j - 1 (P's 64-key halves lie 64 columns apart)
+                        // O += P V of tile j - 1 (P's 64-key halves lie 64 columns apart)
+                        if (steps == kKeys / 16) {
 #pragma unroll
                             for (int kk = 0; kk < kKeys / 16; ++kk) {
-                                if (kk < steps)
-                                    umma_ts(t_o, t_s + (kk >> 2) * 64 + (kk & 3) * 8, upper | (vl + kk * (2048 >> 4)), id_o, on);
+                                umma_ts(t_o, t_s + (kk >> 2) * 64 + (kk & 3) * 8, upper | (vl + kk * (2048 >> 4)), id_o, on);
+                                on = 1;
+                            }
+                        } else {
+#pragma unroll 1
+                            for (int kk = 0; kk < steps; ++kk) {
+                                umma_ts(t_o, t_s + (kk >> 2) * 64 + (kk & 3) * 8, upper | (vl + kk * (2048 >> 4)), id_o, on);
                                 on = 1;
                             }
                         }
