@@ -366,8 +366,35 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
                         }
                     mine = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                 }
-                // (m is the same in both warps; with it 2^(score - m) stays below 2^8)
-                if (named_barrier_or(1 + pair, 64, failed || mine * p.scale_log2 > m + 8.f)) {
+                // weights 2^(scale * score - m) of columns [32 c, 32 c + 32), as packed pairs; their sum
+                const uint64_t scale2 = pack_f32x2(p.scale_log2, p.scale_log2);
+                uint32_t pk[16];
+                auto weigh = [&](int c) {
+                    const float negm = m == -INFINITY ? 0.f : -m;
+                    const uint64_t negm2 = pack_f32x2(negm, negm);
+                    uint64_t sum2[2] = {0ull, 0ull};
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        float u, w;
+                        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[c][2 * e]), __uint_as_float(x[c][2 * e + 1])), scale2, negm2), u, w);
+                        u = chunk_exp2(u);
+                        w = chunk_exp2(w);
+                        sum2[e & 1] = add_f32x2(sum2[e & 1], pack_f32x2(u, w));
+                        pk[e] = pack_bf16x2(u, w);  // bf16: the type of V, which P multiplies
+                    }
+                    float u, w;
+                    unpack_f32x2(add_f32x2(sum2[0], sum2[1]), u, w);
+                    return u + w;
+                };
+                // the first half of them with the maximum so far, which is rarely outgrown; then again if it was
+                float sum = 0.f;
+#pragma unroll 1
+                for (bool first = true, again = true; again; first = false) {
+                    sum = weigh(0);
+                    again = false;
+                    if (!first) break;
+                    // (m is the same in both warps; with it 2^(score - m) stays below 2^8)
+                    if (!named_barrier_or(1 + pair, 64, failed || mine * p.scale_log2 > m + 8.f)) break;
                     float theirs;
                     if (!meet(mine, theirs)) {
                         failed = true;
@@ -392,31 +419,16 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
                         l *= alpha;
                         m = top;
                     }
+                    again = true;
                 }
-                const float negm = m == -INFINITY ? 0.f : -m;
-                const uint64_t scale2 = pack_f32x2(p.scale_log2, p.scale_log2), negm2 = pack_f32x2(negm, negm);
-                uint64_t sum2[2] = {0ull, 0ull};
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t pk[16];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        float u, w;
-                        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[c][2 * e]), __uint_as_float(x[c][2 * e + 1])), scale2, negm2), u, w);
-                        u = chunk_exp2(u);
-                        w = chunk_exp2(w);
-                        sum2[e & 1] = add_f32x2(sum2[e & 1], pack_f32x2(u, w));
-                        pk[e] = pack_bf16x2(u, w);  // bf16: the type of V, which P multiplies
-                    }
-                    tmem_st16(s_addr + c * 16, pk);
-                }
+                if (failed) break;
+                tmem_st16(s_addr, pk);
+                sum += weigh(1);
+                tmem_st16(s_addr + 16, pk);
+                l += sum;
                 tmem_st_wait();
                 tc_fence_before();
                 mbar_arrive(&sh.p[i]);
-                float s0, s1, s2, s3;
-                unpack_f32x2(sum2[0], s0, s1);
-                unpack_f32x2(sum2[1], s2, s3);
-                l += (s0 + s1) + (s2 + s3);
             }
             if (failed) break;
             const Job done = g;
