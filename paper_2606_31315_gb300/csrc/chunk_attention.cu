@@ -294,16 +294,18 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
     tc_fence_after();
     griddep_launch_dependents();
     const uint32_t tmem = sh.tmem;
-    // the next job, for a warp that has had `nj` of them; false: no more (or a wait given up: ok is false then)
-    auto next_job = [&](unsigned& nj, Job& g, bool& ok) {
-        const int e = nj % kJobs;
-        ok = __all_sync(0xffffffffu, mbar_wait(&sh.job_full[e], (nj / kJobs) & 1, kWaitBudget));
-        if (!ok) return false;
-        g = sh.job[e];
+    // The next job, for a warp that has had `nj` of them; none if there are no more (or a wait was given up: ok is false).
+    // The warp reads what it needs and calls had_job.
+    auto next_job = [&](unsigned nj, bool& ok) -> const Job* {
+        ok = __all_sync(0xffffffffu, mbar_wait(&sh.job_full[nj % kJobs], (nj / kJobs) & 1, kWaitBudget));
+        if (!ok) return nullptr;
+        const Job* g = &sh.job[nj % kJobs];
+        return g->s >= 0 ? g : nullptr;
+    };
+    auto had_job = [&](unsigned& nj) {
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.job_empty[e]);
+        if (lane == 0) mbar_arrive(&sh.job_empty[nj % kJobs]);
         ++nj;
-        return g.s >= 0;
     };
 
     if (warp < kSoftmaxWarps) {
@@ -329,15 +331,18 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
             return *const_cast<volatile int*>(&sh.pair_failed[pair]) == 0;
         };
         unsigned nj = 0;
-        Job g;
-        bool ok, more = next_job(nj, g, ok);
-        while (more) {
-            const int a = g.a[i], b = g.b[i];
-            const int tok = g.t * 2 * p.tokens + i * p.tokens + my_tok;
-            const bool active = my_tok < p.tokens && tok < g.B;
-            const int pos = g.n - g.B + tok;
-            const int hi = !active ? 0 : p.causal ? max(0, pos + 1) : g.n;
+        bool ok;
+        while (const Job* g = next_job(nj, ok)) {
+            const int a = g->a[i], b = g->b[i];
+            const int tok = g->t * 2 * p.tokens + i * p.tokens + my_tok;
+            const bool active = my_tok < p.tokens && tok < g->B;
+            const int pos = g->n - g->B + tok;
+            const int hi = !active ? 0 : p.causal ? max(0, pos + 1) : g->n;
             const int lo = p.window > 0 ? max(0, pos + 1 - p.window) : 0;
+            const bool first = g->first, whole = first && g->last;
+            // the query row's number among all, in the output (-1: none)
+            const long long orow = active ? (long long)(g->q0 + tok) * p.num_q_heads + g->h * G + my_head : -1;
+            had_job(nj);
             float m = -INFINITY, l = 0.f;
             for (int j = a; j < b; ++j, ++ns) {
                 const int from = lo - j * kKeys - half * 64, to = hi - j * kKeys - half * 64;  // visible columns
@@ -389,10 +394,10 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
                 // the first half of them with the maximum so far, which is rarely outgrown; then again if it was
                 float sum = 0.f;
 #pragma unroll 1
-                for (bool first = true, again = true; again; first = false) {
+                for (bool once = true, again = true; again; once = false) {
                     sum = weigh(0);
                     again = false;
-                    if (!first) break;
+                    if (!once) break;
                     // (m is the same in both warps; with it 2^(score - m) stays below 2^8)
                     if (!named_barrier_or(1 + pair, 64, failed || mine * p.scale_log2 > m + 8.f)) break;
                     float theirs;
@@ -431,8 +436,6 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
                 mbar_arrive(&sh.p[i]);
             }
             if (failed) break;
-            const Job done = g;
-            more = next_job(nj, g, ok);  // while the last P V runs
             if (b > a) {
                 failed = !__all_sync(0xffffffffu, mbar_wait(&sh.o[i], no & 1, kWaitBudget));
                 ++no;
@@ -445,12 +448,12 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
             }
             named_barrier(1 + pair, 64);  // both have read it before the next job's first tile writes there
             l = half ? others + l : l + others;
-            const bool whole = done.first && done.last;
             const float inv = whole ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
-            const size_t orow = (size_t)(done.q0 + tok) * p.num_q_heads + done.h * G + my_head;
-            const size_t slot = (size_t)blockIdx.x * 2 + (done.first ? 1 : 0);
-            // the row's address for the lanes of this group of four that store a piece of it
-            const unsigned long long out = active ? reinterpret_cast<unsigned long long>(p.o + orow * D + half * (D / 2)) : 0ull;
+            const size_t slot = (size_t)blockIdx.x * 2 + (first ? 1 : 0);
+            // the rows of this lane's group of four, each of which the four store together
+            long long rows[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) rows[k] = __shfl_sync(0xffffffffu, orow, (lane & ~3) + k);
 #pragma unroll
             for (int c = 0; c < D / 64; ++c) {
                 uint32_t v[32];
@@ -481,10 +484,10 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
                                 }
                             }
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {  // piece lane & 3 of the row of lane (lane & ~3) + k
-                        const unsigned long long at = __shfl_sync(0xffffffffu, out, (lane & ~3) + k);
-                        if (at) *reinterpret_cast<uint4*>(at + c * 64 + (lane & 3) * 16) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
-                    }
+                    for (int k = 0; k < 4; ++k)  // piece lane & 3 of the row of lane (lane & ~3) + k
+                        if (rows[k] >= 0)
+                            *reinterpret_cast<uint4*>(p.o + rows[k] * D + half * (D / 2) + c * 32 + (lane & 3) * 8) =
+                                make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
                 } else if (active) {
 #pragma unroll
                     for (int e = 0; e < 32; e += 8)
@@ -664,22 +667,22 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
             unsigned nj = 0, np = 0, turn = 0;
             int nq = 0;
             bool ok, fine = true, any = false;
-            Job g;
-            while (next_job(nj, g, ok)) {
-                if (g.j1 <= g.j0) continue;
-                const int a = g.a[i], b = g.b[i];
+            while (const Job* g = next_job(nj, ok)) {
+                const int a = g->a[i], b = g->b[i], j0 = g->j0, j1 = g->j1, n = g->n;
+                had_job(nj);
+                if (j1 <= j0) continue;
                 fine = wait(&sh.q_full, nq & 1);
-                for (int j = g.j0; j <= g.j1 && fine; ++j, ++turn, x += 2) {  // x: K of tile j
+                for (int j = j0; j <= j1 && fine; ++j, ++turn, x += 2) {  // x: K of tile j
                     const int kslot = x % S::slots, vslot = (x - 1) % S::slots;
                     const bool pv = j > a && j <= b, qk = j >= a && j < b;
-                    if (j < g.j1) fine = wait(&sh.full[kslot], (x / S::slots) & 1);
-                    if (fine && j > g.j0) fine = wait(&sh.full[vslot], ((x - 1) / S::slots) & 1);
+                    if (j < j1) fine = wait(&sh.full[kslot], (x / S::slots) & 1);
+                    if (fine && j > j0) fine = wait(&sh.full[vslot], ((x - 1) / S::slots) & 1);
                     if (fine && pv) fine = wait(&sh.p[i], np++ & 1);
                     if (fine) fine = wait(&sh.turn[i], (turn & 1) ^ (i ^ 1));
                     if (!fine) break;
                     tc_fence_after();
                     // keys past the sequence's last in steps of 16: the tail warp has cleared the rest of a step
-                    const int steps = pv ? min(kKeys / 16, (g.n - (j - 1) * kKeys + 15) / 16) : 0;
+                    const int steps = pv ? min(kKeys / 16, (n - (j - 1) * kKeys + 15) / 16) : 0;
                     const uint32_t vl = v_lo + vslot * (S::tile_bytes >> 4), kl = k_lo + kslot * (S::tile_bytes >> 4);
                     uint32_t on = j - 1 > a ? 1u : 0u;
                     if (elect_one()) {
@@ -709,9 +712,9 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
                         mbar_arrive(&sh.turn[i ^ 1]);
                         if (qk) umma_commit(&sh.s[i]);
                         if (pv && j == b) umma_commit(&sh.o[i]);
-                        if (j > g.j0) release(&sh.empty[vslot], pv);
-                        if (j < g.j1) release(&sh.empty[kslot], qk);
-                        if (j == g.j1 - 1) release(&sh.q_empty, any || qk);
+                        if (j > j0) release(&sh.empty[vslot], pv);
+                        if (j < j1) release(&sh.empty[kslot], qk);
+                        if (j == j1 - 1) release(&sh.q_empty, any || qk);
                     }
                     __syncwarp();
                     any = any || qk;
@@ -731,8 +734,9 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
             unsigned x0 = 0, phase = 0, nj = 0;
             int4 left = make_int4(0, 0, 0, 0);
             bool ok, fine = true;
-            Job g;
-            while (next_job(nj, g, ok)) {
+            while (const Job* job = next_job(nj, ok)) {
+                const Job g = *job;
+                had_job(nj);
                 if (!g.first) left.x |= kHasHead | (g.last ? kHeadEnds : 0);
                 if (g.first && !g.last) left = make_int4(left.x | kHasTail, g.s, g.h, g.t);
                 if (g.j1 <= g.j0) continue;
