@@ -39,10 +39,9 @@ constexpr int kChunkThreads = 32 * 20;
 // 640 x 96).
 constexpr int kSoftmaxRegs = 104, kOtherRegs = 64;
 constexpr uint32_t kChunkTmem = 512;
-constexpr int kTileCost = 192;                   // a work tile's fixed cost (queries in, output out), in keys
-constexpr int kLeastCost = kTileCost + 2 * kKeys;  // of a CTA's stretch: below it, fewer CTAs take part
+constexpr int kTileCost = 400;                   // a work tile's fixed cost (queries in, output out), in keys
+constexpr int kLeastCost = 2 * kKeys;                // of a CTA's stretch: below it, fewer CTAs take part
 constexpr int kJobs = 4;                         // jobs laid out ahead
-constexpr int kLeastCut = 2;                     // key tiles on either side of a cut
 
 template <int D>
 struct Shape {
@@ -69,6 +68,7 @@ struct ChunkParams {
     float scale_log2;
     float* part_o;   // [grid][2][D / 8][256][8] (part_at): the first stretch's part (it began in an earlier CTA) and the last one's
     float2* part_ml; // [grid][2][256]
+    unsigned long long grid_inverse;  // 2^64 / the grid, rounded down
     int4* info;      // [grid]: flags, and the sequence, head and tile that the CTA began and did not end
     unsigned int* err;
 };
@@ -94,11 +94,12 @@ struct Seq {
     __device__ __forceinline__ int tiles() const { return (B + Q - 1) / Q; }
     __device__ __forceinline__ int hi(int tok_end) const { return causal ? max(0, n - B + tok_end) : n; }  // tok_end <= B
     __device__ __forceinline__ int lo(int tok) const { return window > 0 ? min(n, max(0, n - B + tok + 1 - window)) : 0; }
+    __device__ __forceinline__ int keys(int t) const { return max(0, hi(min(B, (t + 1) * Q)) - lo(t * Q)); }
     // sum over t < x of max(0, a + t * Q)
-    __device__ __forceinline__ long long ramp(long long a, int x) const {
-        const int t0 = a >= 0 ? 0 : (int)min((long long)x, (-a + Q - 1) / Q);
+    __device__ __forceinline__ long long ramp(int a, int x) const {
+        const int t0 = a >= 0 ? 0 : min(x, (-a + Q - 1) / Q);
         const long long c = x - t0;
-        return c * a + (long long)Q * (((long long)t0 + x - 1) * c / 2);
+        return c * a + Q * ((c * (t0 + x - 1)) >> 1);
     }
     // keys (and fixed costs) of the tiles before x, 0 <= x <= tiles(); exact but for a window wider than n at both
     // ends of a tile, where neighbours agree on the same number all the same
@@ -106,12 +107,12 @@ struct Seq {
         long long w = (long long)x * kTileCost;
         const int T = tiles();
         if (causal) {
-            w += ramp((long long)n - B + Q, x == T ? x - 1 : x);
+            w += ramp(n - B + Q, x == T ? x - 1 : x);
             if (x == T && x > 0) w += n;
         } else {
             w += (long long)x * n;
         }
-        if (window > 0) w -= ramp((long long)n - B + 1 - window, x);
+        if (window > 0) w -= ramp(max(n - B + 1 - window, -(1 << 30)), x);
         return w;
     }
 };
@@ -131,52 +132,49 @@ struct Job {
     int first, last;   // it holds the work tile's first / last key tile
 };
 
-struct Line {
-    const ChunkParams& p;
-    __device__ __forceinline__ Seq seq(int s) const {
-        Seq q;
-        q.B = __ldg(p.cu_q + s + 1) - __ldg(p.cu_q + s);
-        q.n = __ldg(p.cu_kv + s + 1) - __ldg(p.cu_kv + s);
-        q.Q = 2 * p.tokens;
-        q.causal = p.causal;
-        q.window = p.window;
-        return q;
+__device__ __forceinline__ Seq load_seq(const ChunkParams& p, int s) {
+    const int q0 = __ldg(p.cu_q + s), q1 = __ldg(p.cu_q + s + 1), k0 = __ldg(p.cu_kv + s), k1 = __ldg(p.cu_kv + s + 1);
+    return Seq{q1 - q0, k1 - k0, 2 * p.tokens, p.causal, p.window};
+}
+// Key tiles [first, first + count) under tile t.
+__device__ __forceinline__ void tile_span(const Seq& q, int t, int& first, int& count) {
+    const int lo = q.lo(t * q.Q), hi = q.hi(min(q.B, (t + 1) * q.Q));
+    first = lo / kKeys;
+    count = hi > lo ? (hi + kKeys - 1) / kKeys - first : 0;
+}
+// A sequence's whole part of the line.
+__device__ __forceinline__ long long seq_cost(const ChunkParams& p, const Seq& q) {
+    if (q.B <= 0) return 0;
+    return (q.B <= q.Q ? kTileCost + q.keys(0) : q.cost(q.tiles())) * p.num_kv_heads;
+}
+// The place at `rem` of that part.
+__device__ __forceinline__ Place place_in(const ChunkParams& p, int s, const Seq& q, long long rem) {
+    const int T = q.B <= q.Q ? 1 : q.tiles();
+    const long long all = T == 1 ? kTileCost + q.keys(0) : q.cost(T);
+    Place at;
+    at.s = s;
+    at.h = min((int)__fdividef((float)rem, (float)all), p.num_kv_heads - 1);  // rem / all, put right below
+    rem -= at.h * all;
+    while (rem < 0) rem += all, --at.h;
+    while (rem >= all) rem -= all, ++at.h;
+    at.t = 0;
+    for (int hi = T; hi - at.t > 1;) {  // the largest t with cost(t) <= rem
+        const int mid = (at.t + hi) >> 1;
+        if (q.cost(mid) <= rem) at.t = mid; else hi = mid;
     }
-    // key tiles [first, first + count) under tile t
-    __device__ __forceinline__ static void span(const Seq& q, int t, int& first, int& count) {
-        const int lo = q.lo(t * q.Q), hi = q.hi(min(q.B, (t + 1) * q.Q));
-        first = lo / kKeys;
-        count = hi > lo ? (hi + kKeys - 1) / kKeys - first : 0;
-    }
-    // the place at `rem` of sequence s's own part of the line
-    __device__ __forceinline__ Place within(int s, long long rem) const {
-        const Seq q = seq(s);
-        const int T = q.tiles();
-        const long long all = q.cost(T);
-        Place at;
-        at.s = s;
-        at.h = (int)(rem / all);
-        rem -= at.h * all;
-        int lo = 0, hi = T;  // the largest t with cost(t) <= rem
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (q.cost(mid) <= rem) lo = mid; else hi = mid;
-        }
-        at.t = lo;
-        const long long off = rem - q.cost(lo), w = q.cost(lo + 1) - q.cost(lo);
-        int first, count;
-        span(q, lo, first, count);
-        const long long x = off - kTileCost;
-        at.j = x <= 0 ? 0 : (int)min((long long)count, (x + kKeys / 2) / kKeys);
-        if (at.j < kLeastCut || count - at.j < kLeastCut) {
-            at.j = 0;
-            if (2 * off >= w) ++at.t;  // the next tile's start
-        }
-        if (at.t == T) at.t = 0, ++at.h;
-        if (at.h == p.num_kv_heads) at.h = 0, ++at.s;
-        return at;
-    }
-};
+    const int off = (int)(at.t > 0 ? rem - q.cost(at.t) : rem), w = kTileCost + q.keys(at.t);
+    int first, count;
+    tile_span(q, at.t, first, count);
+    at.j = off <= kTileCost ? 0 : min(count, (off - kTileCost + kKeys / 2) / kKeys);
+    // (two key tiles at least on either side of a cut, whose parts are up to 256 rows; few rows are cut anywhere)
+    const int least = q.B <= p.tokens ? 1 : 2;
+    const bool whole = count < 2 * least;  // not to be cut: the nearer end
+    if (whole ? 2 * off >= w : count - at.j < least) at.j = 0, ++at.t;
+    else if (whole || at.j < least) at.j = 0;
+    if (at.t == T) at.t = 0, ++at.h;
+    if (at.h == p.num_kv_heads) at.h = 0, ++at.s;
+    return at;
+}
 
 // Works through the jobs between two places.
 struct Walk {
@@ -186,10 +184,9 @@ struct Walk {
     Seq q;
     int q0;
     __device__ __forceinline__ bool next(Job& g) {
-        const Line line{p};
         while (at.s < end.s || (at.s == end.s && (at.h < end.h || (at.h == end.h && (at.t < end.t || (at.t == end.t && at.j < end.j)))))) {
             if (at.s != known) {
-                q = line.seq(at.s);
+                q = load_seq(p, at.s);
                 q0 = __ldg(p.cu_q + at.s);
                 known = at.s;
             }
@@ -199,7 +196,7 @@ struct Walk {
                 continue;
             }
             int first, count;
-            Line::span(q, at.t, first, count);
+            tile_span(q, at.t, first, count);
             const bool cut = at.same_tile(end);
             g.s = at.s; g.h = at.h; g.t = at.t; g.q0 = q0; g.B = q.B; g.n = q.n;
             g.j0 = first + at.j;
@@ -248,7 +245,7 @@ static_assert(chunk_smem<128>() <= 227 * 1024 && chunk_smem<64>() <= 227 * 1024,
 
 template <int D>
 __global__ void __launch_bounds__(kChunkThreads, 1)
-chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap qmap,
+chunk_attention_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__ CUtensorMap qmap,
                        const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap) {
     using S = Shape<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -288,6 +285,7 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
         tmem_alloc(&sh.tmem, kChunkTmem);
         tmem_relinquish();
     }
+    if (warp == kProducerWarp && lane < 3) prefetch_tensormap(lane == 0 ? &qmap : lane == 1 ? &kmap : &vmap);
     griddep_wait();
     tc_fence_before();
     __syncthreads();
@@ -507,47 +505,59 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
         if (warp == kProducerWarp) {
             // ================= this CTA's part of the line, laid out in jobs; their queries, then K and V tiles through
             // the ring, K first
-            const Line line{p};
-            auto whole = [&](int s) -> long long {
-                if (s >= p.num_seqs) return 0;
-                const Seq q = line.seq(s);
-                return q.B > 0 ? q.cost(q.tiles()) * p.num_kv_heads : 0;
-            };
-            long long total = 0;
-            for (int base = 0; base < p.num_seqs; base += 32) {
-                long long w = whole(base + lane);
+            const int c = blockIdx.x, mine = lane & 1;  // even lanes find this CTA's begin, odd ones the next one's
+            auto take = [&](int s) { return s < p.num_seqs ? load_seq(p, s) : Seq{}; };
+            auto scan = [&](long long w) {
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
-                total += w;
-            }
-            const long long parts = min((long long)gridDim.x, max(1ll, total / kLeastCost));
-            const long long c = blockIdx.x;
-            // cuts at total * c / parts
-            const long long step = total / parts, rest = total % parts;
-            const long long cut[2] = {c * step + c * rest / parts, (c + 1) * step + (c + 1) * rest / parts};
-            Place place[2] = {Place{p.num_seqs, 0, 0, 0}, Place{p.num_seqs, 0, 0, 0}};
-            long long before = 0;
-            if (c < parts) {
-                for (int base = 0; base < p.num_seqs; base += 32) {
-                    const long long w = whole(base + lane);
-                    long long incl = w;
-#pragma unroll
-                    for (int o = 1; o < 32; o <<= 1) {
-                        const long long y = __shfl_up_sync(0xffffffffu, incl, o);
-                        if (lane >= o) incl += y;
-                    }
-                    incl += before;
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const unsigned hit = __ballot_sync(0xffffffffu, w > 0 && incl - w <= cut[e] && cut[e] < incl);
-                        if (hit) {
-                            const int l = __ffs(hit) - 1;
-                            place[e] = line.within(base + l, cut[e] - __shfl_sync(0xffffffffu, incl - w, l));
-                        }
-                    }
-                    before = __shfl_sync(0xffffffffu, incl, 31);
+                for (int o = 1; o < 32; o <<= 1) {
+                    const long long y = __shfl_up_sync(0xffffffffu, w, o);
+                    if (lane >= o) w += y;
                 }
+                return w;
+            };
+            Seq q = take(lane);
+            long long w = seq_cost(p, q), incl = scan(w), total = __shfl_sync(0xffffffffu, incl, 31);
+            for (int base = 32; base < p.num_seqs; base += 32) {
+                long long more = seq_cost(p, take(base + lane));
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) more += __shfl_xor_sync(0xffffffffu, more, o);
+                total += more;
             }
+            // the cuts lie at total * c / parts
+            const int parts = (int)min((long long)gridDim.x, max(1ll, total / kLeastCost));
+            const long long cut = c + mine >= parts               ? total
+                                  : parts == (int)gridDim.x ? (long long)__umul64hi(total * (c + mine), p.grid_inverse)
+                                                            : (long long)((unsigned)total * (unsigned)(c + mine) / (unsigned)parts);
+            Seq my_q = q;
+            int my_s = p.num_seqs;
+            long long my_rem = 0, before = 0;
+            for (int base = 0; c < parts && base < p.num_seqs; base += 32) {
+                if (base > 0) {
+                    q = take(base + lane);
+                    w = seq_cost(p, q);
+                    incl = before + scan(w);
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const long long at = __shfl_sync(0xffffffffu, cut, e);
+                    const unsigned hit = __ballot_sync(0xffffffffu, w > 0 && incl - w <= at && at < incl);
+                    if (hit) {
+                        const int l = __ffs(hit) - 1;
+                        const int B = __shfl_sync(0xffffffffu, q.B, l), n = __shfl_sync(0xffffffffu, q.n, l);
+                        const long long rem = at - __shfl_sync(0xffffffffu, incl - w, l);
+                        if (mine == e) my_s = base + l, my_q = Seq{B, n, 2 * p.tokens, p.causal, p.window}, my_rem = rem;
+                    }
+                }
+                before = __shfl_sync(0xffffffffu, incl, 31);
+            }
+            Place at = Place{p.num_seqs, 0, 0, 0};
+            if (my_s < p.num_seqs) at = place_in(p, my_s, my_q, my_rem);
+            __syncwarp();
+            Place place[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                place[e] = Place{__shfl_sync(0xffffffffu, at.s, e), __shfl_sync(0xffffffffu, at.h, e),
+                                 __shfl_sync(0xffffffffu, at.t, e), __shfl_sync(0xffffffffu, at.j, e)};
             Walk walk{p, place[0], place[1], -1, Seq{}, 0};
             unsigned nj = 0;
             bool ok = true;
@@ -572,11 +582,10 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
             int nq = 0;
             unsigned on_raw = 0, raw_phase = 0;  // per slot: whether its last use is on raw; that barrier's uses, mod 2
             Job g, after;
-            lay_out(g);
-            while (ok && g.s >= 0) {
-                lay_out(after);
+            for (bool have = false; ; have = true) {
+                lay_out(after);  // one ahead of the copies
                 if (!ok) break;
-                if (g.j1 > g.j0) {
+                if (have && g.j1 > g.j0) {
                     const int tok = g.t * 2 * p.tokens;
                     if (nq > 0 && !__all_sync(0xffffffffu, mbar_wait(&sh.q_empty, (nq - 1) & 1, kWaitBudget))) {
                         ok = false;
@@ -634,6 +643,7 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
                         row = row_next;
                     }
                 }
+                if (!ok || after.s < 0) break;
                 g = after;
             }
             if (!ok && lane == 0) raise_error(p.err, kErrTimeout);
@@ -770,18 +780,20 @@ chunk_attention_kernel(const ChunkParams p, const __grid_constant__ CUtensorMap 
     }
 }
 
-// Merges the parts of every work tile that was cut: block (c, y) 32 rows of the tile that CTA c began and did not end.
-// Its parts are c's last and the first ones of the CTAs behind it, up to the one that ends it.  A thread has 8 columns of
-// a row; a warp 32 rows' (a part's lines are read whole).
-constexpr int kMergeRows = 32;
+// Merges the parts of every work tile that was cut: block (c, y) rows [32 y, 32 y + 32) of the tile that CTA c began and
+// did not end.  Its parts are c's last and the first ones of the CTAs behind it, up to the one that ends it.  A warp has a row:
+// its lanes take the parts' (m, l), 32 at a time, and weigh them; then 4 columns each, all parts' loads in flight.
+constexpr int kMergeThreads = 512, kMergeRows = 32;
 template <int D>
-__global__ void __launch_bounds__(kMergeRows * D / 8) chunk_merge_kernel(const ChunkParams p, int grid) {
+__global__ void __launch_bounds__(kMergeThreads) chunk_merge_kernel(const __grid_constant__ ChunkParams p, int grid) {
     griddep_launch_dependents();
     griddep_wait();
-    const int c = blockIdx.x, lane = threadIdx.x & 31, col = (threadIdx.x >> 5) * 8;
+    const int c = blockIdx.x, i = blockIdx.y * kMergeRows / kTileM, r0 = blockIdx.y * kMergeRows % kTileM, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int4 mine = p.info[c];
     if (!(mine.x & kHasTail)) return;
-    const int q0 = p.cu_q[mine.y], B = p.cu_q[mine.y + 1] - q0;
+    const int tok0 = mine.w * 2 * p.tokens + i * p.tokens;
+    const int q0 = p.cu_q[mine.y], rows = min(p.tokens, p.cu_q[mine.y + 1] - q0 - tok0) * p.group;
+    if (r0 + warp >= rows) return;
     int last = c + 1;  // the CTA that ends the tile
     for (int base = c + 1; base < grid; base += 32) {
         const unsigned hit = __ballot_sync(0xffffffffu, base + lane < grid && (p.info[base + lane].x & kHeadEnds));
@@ -790,30 +802,56 @@ __global__ void __launch_bounds__(kMergeRows * D / 8) chunk_merge_kernel(const C
             break;
         }
     }
-    const int row = blockIdx.y * kMergeRows + lane;
-    const int i = row / kTileM, r = row % kTileM, tok = mine.w * 2 * p.tokens + i * p.tokens + r / p.group;
-    if (r / p.group >= p.tokens || tok >= B) return;
-    float acc[8] = {}, m = -INFINITY, l = 0.f;
-    for (int e = c; e <= last; ++e) {
-        const size_t slot = (size_t)e * 2 + (e == c ? 1 : 0);
-        if (e > c && !(p.info[e].x & kHasHead)) continue;
-        const float2 ml = p.part_ml[slot * (2 * kTileM) + row];
-        if (!(ml.y > 0.f)) continue;
-        const float4* o = reinterpret_cast<const float4*>(p.part_o + part_at<D>(slot, row, col));
-        const float4 o0 = o[0], o1 = o[1];
-        const float v[8] = {o0.x, o0.y, o0.z, o0.w, o1.x, o1.y, o1.z, o1.w};
-        const float m_new = fmaxf(m, ml.x), w_old = chunk_exp2(m - m_new), w = chunk_exp2(ml.x - m_new);
-        l = l * w_old + ml.y * w;
+    constexpr int kCols = D / 32;
+    for (int r = r0 + warp; r < min(rows, r0 + kMergeRows); r += kMergeThreads / 32) {
+        const int row = i * kTileM + r;
+        float acc[kCols] = {}, m = -INFINITY, l = 0.f;
+        for (int base = c; base <= last; base += 32) {
+            const int e = base + lane;
+            const size_t slot = (size_t)e * 2 + (e == c ? 1 : 0);
+            float2 ml = make_float2(-INFINITY, 0.f);
+            if (e <= last && (e == c || (p.info[e].x & kHasHead))) ml = p.part_ml[slot * (2 * kTileM) + row];
+            if (!(ml.y > 0.f)) ml = make_float2(-INFINITY, 0.f);  // (no key seen: its columns count for nothing)
+            float top = ml.x;
 #pragma unroll
-        for (int d = 0; d < 8; ++d) acc[d] = acc[d] * w_old + v[d] * w;
-        m = m_new;
+            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const float m_new = fmaxf(m, top);
+            if (m_new == -INFINITY) continue;
+            const float w_old = chunk_exp2(m - m_new), w = ml.y > 0.f ? chunk_exp2(ml.x - m_new) : 0.f;
+            float sum = ml.y * w;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            l = l * w_old + sum;
+            m = m_new;
+#pragma unroll
+            for (int d = 0; d < kCols; ++d) acc[d] *= w_old;
+            const int n = min(32, last + 1 - base);
+#pragma unroll 8
+            for (int k = 0; k < n; ++k) {
+                const float wk = __shfl_sync(0xffffffffu, w, k);
+                const size_t s = (size_t)(base + k) * 2 + (base + k == c ? 1 : 0);
+                const float* o = p.part_o + part_at<D>(s, row, lane * kCols / 8 * 8) + lane * kCols % 8;
+                float v[kCols];
+                if constexpr (kCols == 4) {
+                    const float4 t = *reinterpret_cast<const float4*>(o);
+                    v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
+                } else {
+                    const float2 t = *reinterpret_cast<const float2*>(o);
+                    v[0] = t.x; v[1] = t.y;
+                }
+#pragma unroll
+                for (int d = 0; d < kCols; ++d) acc[d] += wk > 0.f ? wk * v[d] : 0.f;  // (a slot without a part holds anything)
+            }
+        }
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const size_t orow = (size_t)(q0 + tok0 + r / p.group) * p.num_q_heads + mine.z * p.group + r % p.group;
+        __nv_bfloat16* out = p.o + orow * D + lane * kCols;
+        if constexpr (kCols == 4)
+            *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
+        else
+            *reinterpret_cast<uint32_t*>(out) = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+        if (p.lse && lane == 0) p.lse[orow] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
     }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    const size_t orow = (size_t)(q0 + tok) * p.num_q_heads + mine.z * p.group + r % p.group;
-    *reinterpret_cast<uint4*>(p.o + orow * D + col) =
-        make_uint4(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv),
-                   pack_bf16x2(acc[4] * inv, acc[5] * inv), pack_bf16x2(acc[6] * inv, acc[7] * inv));
-    if (p.lse && col == 0) p.lse[orow] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
 template <int D>
@@ -839,6 +877,7 @@ int run(const ChunkAttentionArgs& a, const DeviceInfo& dev, cudaStream_t stream)
     p.scale_log2 = a.scale * 1.4426950408889634f;
     p.err = a.err_word;
     const int grid = std::min(dev.sm_count, kChunkMaxGrid);
+    p.grid_inverse = ~0ull / (unsigned)grid;
     uint8_t* at = static_cast<uint8_t*>(a.scratch);
     p.part_o = reinterpret_cast<float*>(at);
     at += (size_t)kChunkMaxGrid * 2 * 2 * kTileM * D * sizeof(float);
@@ -886,7 +925,7 @@ int run(const ChunkAttentionArgs& a, const DeviceInfo& dev, cudaStream_t stream)
     cfg.numAttrs = 1;
     if (cudaLaunchKernelEx(&cfg, chunk_attention_kernel<D>, p, qmap, kmap, vmap) != cudaSuccess) return BP_ERR_CUDA;
     cfg.gridDim = dim3((unsigned)grid, 2 * kTileM / kMergeRows, 1);
-    cfg.blockDim = dim3(kMergeRows * D / 8, 1, 1);
+    cfg.blockDim = dim3(kMergeThreads, 1, 1);
     cfg.dynamicSmemBytes = 0;
     return cudaLaunchKernelEx(&cfg, chunk_merge_kernel<D>, p, grid) == cudaSuccess ? BP_OK : BP_ERR_CUDA;
 }
