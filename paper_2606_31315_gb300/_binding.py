@@ -210,36 +210,35 @@ def kv_append(k_cache, v_cache, k_new, v_new, cu_new, cu_kv, block_table, page_s
 
 
 # --------------------------------------------------------------------------- prefill
-def _heads(name: str, t, dtype):
+# (Their host time is what a decoding step's small calls take: 12.6 us a call with a helper for every check, 8 of them in
+# this layer; the checks of the usual arguments are written out, and a tensor's attributes read once.)
+def _heads(name: str, t, dtype) -> int:
     """A [tokens, heads, head_dim] CUDA tensor whose heads are contiguous; its stride from a token to the next."""
-    if not (t.is_cuda and t.dim() == 3 and t.dtype == dtype):
+    if t.dtype is not dtype or not t.is_cuda or t.dim() != 3:
         raise ValueError(f"{name} must be a [tokens, heads, head_dim] CUDA tensor of the others' dtype")
     token, head, elt = t.stride()
-    heads, dim = t.shape[1:]
+    n, heads, dim = t.shape
     if (elt != 1 and dim > 1) or (head != dim and heads > 1):
         raise ValueError(f"{name}: the heads of a token must be contiguous")
-    return token if t.shape[0] > 1 else heads * dim
+    return token if n > 1 else heads * dim
 
 
-def _rotation(cos_sin, weights, dtype, dim):
+def _rotation(cos_sin, q_weight, k_weight, dtype, dim):
     """(table, max_pos, rotary_dim) of a cos_sin tensor or None; checks the norms' weights."""
-    _cuda("q_weight k_weight", *weights)
-    for w in weights:
-        if w is not None and (w.dtype != dtype or w.numel() != dim):
-            raise ValueError("q_weight, k_weight must be [head_dim] tensors of the inputs' dtype")
+    for w in (q_weight, k_weight):
+        if w is not None and (w.dtype is not dtype or w.numel() != dim or not (w.is_cuda and w.is_contiguous())):
+            raise ValueError("q_weight, k_weight must be contiguous [head_dim] CUDA tensors of the inputs' dtype")
     if cos_sin is None:
         return None, 0, 0
-    _cuda("cos_sin", cos_sin)
-    if cos_sin.dtype != torch.float32 or cos_sin.dim() != 2:
-        raise ValueError("cos_sin must be a [max_pos, rotary_dim] fp32 tensor")
+    if cos_sin.dtype is not torch.float32 or cos_sin.dim() != 2 or not (cos_sin.is_cuda and cos_sin.is_contiguous()):
+        raise ValueError("cos_sin must be a contiguous [max_pos, rotary_dim] fp32 CUDA tensor")
     return cos_sin.data_ptr(), *cos_sin.shape
 
 
 def _int32(names, *tensors):
-    _cuda(names, *tensors)
     for t in tensors:
-        if t is not None and t.dtype != torch.int32:
-            raise ValueError(f"{names.split()[[x is t for x in tensors].index(True)]} must be int32")
+        if t is not None and (t.dtype is not torch.int32 or not (t.is_cuda and t.is_contiguous())):
+            raise ValueError(f"{names.split()[[x is t for x in tensors].index(True)]} must be a contiguous int32 CUDA tensor")
 
 
 def qk_norm_rope(q, k, cos_sin, positions, q_weight=None, k_weight=None, interleaved: bool = False, eps: float = 1e-6,
@@ -250,38 +249,44 @@ def qk_norm_rope(q, k, cos_sin, positions, q_weight=None, k_weight=None, interle
     [max_pos, rotary_dim] or None, positions int32 [T].  q_out / k_out may be q / k.  Returns (q_out, k_out)."""
     lib = load()
     x = q if q is not None else k
-    dtype = _DTYPES.get(x.dtype)
+    dt = x.dtype
+    dtype = _DTYPES.get(dt)
     if dtype is None:
         raise ValueError("q and k must be bf16 or fp32")
-    t, _, d = x.shape
-    for name, y in (("q", q), ("k", k)):
-        if y is not None and (y.shape[0] != t or y.shape[2] != d):
-            raise ValueError("q and k must have the same tokens and head_dim")
-    table, max_pos, rotary = _rotation(cos_sin, (q_weight, k_weight), x.dtype, d)
-    _int32("positions", positions)
-    if positions.numel() != t:
-        raise ValueError("positions must hold one position for each token")
-    hq = hk = qs = ks = qos = kos = 0
+    t, hq, d = x.shape
+    hk = qs = ks = qos = kos = 0
+    qp = kp = qop = kop = None
     if q is not None:
-        hq, qs = q.shape[1], _heads("q", q, x.dtype)
+        qs = _heads("q", q, dt)
         if q_out is None:
-            q_out = torch.empty((t, hq, d), dtype=q.dtype, device=q.device)
+            q_out = torch.empty((t, hq, d), dtype=dt, device=q.device)
         elif q_out.shape != q.shape:
             raise ValueError("q_out must have q's shape")
-        qos = _heads("q_out", q_out, x.dtype)
+        qos = qs if q_out is q else _heads("q_out", q_out, dt)
+        qp, qop = q.data_ptr(), q_out.data_ptr()
+    else:
+        hq = 0
     if k is not None:
-        hk, ks = k.shape[1], _heads("k", k, x.dtype)
+        n, hk, dk = k.shape
+        if n != t or dk != d:
+            raise ValueError("q and k must have the same tokens and head_dim")
+        ks = _heads("k", k, dt)
         if k_out is None:
-            k_out = torch.empty((t, hk, d), dtype=k.dtype, device=k.device)
+            k_out = torch.empty((t, hk, d), dtype=dt, device=k.device)
         elif k_out.shape != k.shape:
             raise ValueError("k_out must have k's shape")
-        kos = _heads("k_out", k_out, x.dtype)
+        kos = ks if k_out is k else _heads("k_out", k_out, dt)
+        kp, kop = k.data_ptr(), k_out.data_ptr()
+    table, max_pos, rotary = _rotation(cos_sin, q_weight, k_weight, dt, d)
+    if positions.dtype is not torch.int32 or positions.numel() != t or not (positions.is_cuda and positions.is_contiguous()):
+        raise ValueError("positions must be a contiguous int32 CUDA tensor with one position for each token")
     if ws is None:
         ws = workspace(256, x.device)
-    rc = lib.bp_qk_norm_rope(_ptr(q), qs, _ptr(k), ks, _ptr(q_out), qos, _ptr(k_out), kos, _ptr(q_weight),
-                             _ptr(k_weight), table, _ptr(positions), t, hq, hk, d, rotary, max_pos, int(interleaved),
-                             dtype, eps, _ptr(ws), ws.numel(), _stream(stream))
-    _check(rc, "bp_qk_norm_rope")
+    rc = lib.bp_qk_norm_rope(qp, qs, kp, ks, qop, qos, kop, kos, None if q_weight is None else q_weight.data_ptr(),
+                             None if k_weight is None else k_weight.data_ptr(), table, positions.data_ptr(), t, hq, hk,
+                             d, rotary, max_pos, interleaved, dtype, eps, ws.data_ptr(), ws.numel(), _stream(stream))
+    if rc:
+        _check(rc, "bp_qk_norm_rope")
     return q_out, k_out
 
 
@@ -295,13 +300,14 @@ def qkv_append(qkv, k_cache, v_cache, cu_new, cu_kv, block_table, page_size: int
     [num_pages * page_size, Hkv, D]; cu_new / cu_kv int32 [S+1], block_table int32 [S, pages_per_seq] on the device.
     Returns the queries [T, Hq, D] (None without query heads)."""
     lib = load()
-    rows, hkv, d = k_cache.shape
-    _cuda("k_cache v_cache", k_cache, v_cache)
-    _int32("cu_new cu_kv block_table positions", cu_new, cu_kv, block_table, positions)
+    rows, hkv, d = shape = k_cache.shape
     dt = k_cache.dtype
     dtype = _DTYPES.get(dt)
-    if dtype is None or v_cache.dtype != dt or v_cache.shape != k_cache.shape:
+    if dtype is None or v_cache.dtype is not dt or v_cache.shape != shape:
         raise ValueError("the caches must share one shape and dtype (bf16 or fp32)")
+    if not (k_cache.is_cuda and k_cache.is_contiguous() and v_cache.is_cuda and v_cache.is_contiguous()):
+        raise ValueError("the caches must be contiguous CUDA tensors")
+    _int32("cu_new cu_kv block_table positions", cu_new, cu_kv, block_table, positions)
     if torch.is_tensor(qkv):
         qs = ks = vs = _heads("qkv", qkv, dt)
         t, heads, dim = qkv.shape
@@ -323,23 +329,29 @@ def qkv_append(qkv, k_cache, v_cache, cu_new, cu_kv, block_table, page_size: int
         raise ValueError("the new rows must have the caches' head_dim")
     if positions is not None and positions.numel() != t:
         raise ValueError("positions must hold one position for each token")
-    table, max_pos, rotary = _rotation(cos_sin, (q_weight, k_weight), dt, d)
-    qos = 0
+    table, max_pos, rotary = _rotation(cos_sin, q_weight, k_weight, dt, d)
+    qos, qop = 0, None
     if hq == 0:
         qp = q_out = None
-    elif q_out is None:
-        q_out = torch.empty((t, hq, d), dtype=dt, device=k_cache.device)
-    if q_out is not None:
-        if q_out.shape != (t, hq, d):
+    else:
+        if q_out is None:
+            q_out = torch.empty((t, hq, d), dtype=dt, device=k_cache.device)
+        elif q_out.shape != (t, hq, d):
             raise ValueError("q_out must be [tokens, query heads, head_dim]")
-        qos = _heads("q_out", q_out, dt)
+        qos, qop = _heads("q_out", q_out, dt), q_out.data_ptr()
     if ws is None:
         ws = workspace(256, k_cache.device)
-    rc = lib.bp_qkv_append(qp, qs, kp, ks, vp, vs, _ptr(q_out), qos, _ptr(q_weight), _ptr(k_weight), table,
-                           _ptr(positions), _ptr(k_cache), _ptr(v_cache), _ptr(cu_new), _ptr(cu_kv), _ptr(block_table),
-                           block_table.shape[1], int(page_size), rows // int(page_size), cu_new.numel() - 1, t, hq,
-                           hkv, d, rotary, max_pos, int(interleaved), dtype, eps, _ptr(ws), ws.numel(), _stream(stream))
-    _check(rc, "bp_qkv_append")
+    page_size = int(page_size)
+    s, per = block_table.shape
+    if cu_new.numel() != s + 1 or cu_kv.numel() != s + 1:
+        raise ValueError("cu_new and cu_kv must hold one more entry than block_table has rows")
+    rc = lib.bp_qkv_append(qp, qs, kp, ks, vp, vs, qop, qos, None if q_weight is None else q_weight.data_ptr(),
+                           None if k_weight is None else k_weight.data_ptr(), table, _ptr(positions),
+                           k_cache.data_ptr(), v_cache.data_ptr(), cu_new.data_ptr(), cu_kv.data_ptr(),
+                           block_table.data_ptr(), per, page_size, rows // page_size, s, t, hq, hkv, d, rotary,
+                           max_pos, interleaved, dtype, eps, ws.data_ptr(), ws.numel(), _stream(stream))
+    if rc:
+        _check(rc, "bp_qkv_append")
     return q_out
 
 
@@ -362,26 +374,31 @@ def chunk_attention_paged(q, k_cache, v_cache, cu_q, cu_kv, block_table, page_si
     _cuda("k_cache v_cache out lse", k_cache, v_cache, out, lse)
     _int32("cu_q cu_kv block_table", cu_q, cu_kv, block_table)
     dtype = _DTYPES.get(dt)
-    if dtype is None or k_cache.dtype != dt or v_cache.dtype != dt:
+    if dtype is None or k_cache.dtype is not dt or v_cache.dtype is not dt:
         raise ValueError("q, k_cache, v_cache must share one dtype")
-    t, hq, d = q.shape
-    rows, hkv, dk = k_cache.shape
-    if dk != d or v_cache.shape != k_cache.shape:
+    t, hq, d = shape = q.shape
+    rows, hkv, dk = caches = k_cache.shape
+    if dk != d or v_cache.shape != caches:
         raise ValueError("q and the caches must share one head_dim, the caches one shape")
     if out is None:
         out = torch.empty((t, hq, d), dtype=dt, device=q.device)
-    elif out.shape != q.shape or out.dtype != dt:
+    elif out.shape != shape or out.dtype is not dt:
         raise ValueError("out must have q's shape and dtype")
-    if lse is not None and (lse.dtype != torch.float32 or lse.numel() != t * hq):
+    if lse is not None and (lse.dtype is not torch.float32 or lse.numel() != t * hq):
         raise ValueError("lse must be fp32 [tokens, query heads]")
-    s = cu_q.numel() - 1
+    s, per = block_table.shape
+    if cu_q.numel() != s + 1 or cu_kv.numel() != s + 1:
+        raise ValueError("cu_q and cu_kv must hold one more entry than block_table has rows")
     if ws is None:
         ws = workspace(lib.bp_chunk_attention_workspace_size(s, t, hq, hkv, d), q.device)
-    rc = lib.bp_chunk_attention_paged(q.data_ptr(), stride, _ptr(k_cache), _ptr(v_cache), _ptr(out), _ptr(lse),
-                                      _ptr(cu_q), _ptr(cu_kv), _ptr(block_table), block_table.shape[1], int(page_size),
-                                      rows // int(page_size), s, t, int(max_q_len), int(max_kv_len), hq, hkv, d, dtype,
-                                      int(mask), int(window), softmax_scale, _ptr(ws), ws.numel(), _stream(stream))
-    _check(rc, "bp_chunk_attention_paged")
+    page_size = int(page_size)
+    rc = lib.bp_chunk_attention_paged(q.data_ptr(), stride, k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(),
+                                      None if lse is None else lse.data_ptr(), cu_q.data_ptr(), cu_kv.data_ptr(),
+                                      block_table.data_ptr(), per, page_size, rows // page_size, s, t, max_q_len,
+                                      max_kv_len, hq, hkv, d, dtype, mask, window, softmax_scale, ws.data_ptr(),
+                                      ws.numel(), _stream(stream))
+    if rc:
+        _check(rc, "bp_chunk_attention_paged")
     return out, lse
 
 
