@@ -329,8 +329,12 @@ chunk_attention_kernel(const __grid_constant__ ChunkParams p, const __grid_const
             return *const_cast<volatile int*>(&sh.pair_failed[pair]) == 0;
         };
         unsigned nj = 0;
-        bool ok;
-        while (const Job* g = next_job(nj, ok)) {
+        for (;;) {
+            bool ok;
+            const Job* g = next_job(nj, ok);
+            // (a warp that gave up a wait takes its partner along, here and wherever they meet: neither waits alone)
+            failed = named_barrier_or(1 + pair, 64, !ok);
+            if (failed || !g) break;
             const int a = g->a[i], b = g->b[i];
             const int tok = g->t * 2 * p.tokens + i * p.tokens + my_tok;
             const bool active = my_tok < p.tokens && tok < g->B;
@@ -499,7 +503,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkParams p, const __grid_const
             }
             tc_fence_before();
         }
-        if ((failed || !ok) && lane == 0) raise_error(p.err, kErrTimeout);
+        if (failed && lane == 0) raise_error(p.err, kErrTimeout);
     } else {
         regs_dec<kOtherRegs>();
         if (warp == kProducerWarp) {
