@@ -211,7 +211,7 @@ def kv_append(k_cache, v_cache, k_new, v_new, cu_new, cu_kv, block_table, page_s
 
 # --------------------------------------------------------------------------- prefill
 # (Their host time is what a decoding step's small calls take: 12.6 us a call with a helper for every check, 8 of them in
-# this layer; the checks of the usual arguments are written out, and a tensor's attributes read once.)
+# this layer; so the checks of the usual arguments, contiguous tensors, are written out and read every attribute once.)
 def _heads(name: str, t, dtype) -> int:
     """A [tokens, heads, head_dim] CUDA tensor whose heads are contiguous; its stride from a token to the next."""
     if t.dtype is not dtype or not t.is_cuda or t.dim() != 3:
@@ -225,14 +225,18 @@ def _heads(name: str, t, dtype) -> int:
 
 def _rotation(cos_sin, q_weight, k_weight, dtype, dim):
     """(table, max_pos, rotary_dim) of a cos_sin tensor or None; checks the norms' weights."""
-    for w in (q_weight, k_weight):
-        if w is not None and (w.dtype is not dtype or w.numel() != dim or not (w.is_cuda and w.is_contiguous())):
-            raise ValueError("q_weight, k_weight must be contiguous [head_dim] CUDA tensors of the inputs' dtype")
+    if q_weight is not None and (q_weight.dtype is not dtype or q_weight.numel() != dim or
+                                 not (q_weight.is_cuda and q_weight.is_contiguous())):
+        raise ValueError("q_weight must be a contiguous [head_dim] CUDA tensor of the inputs' dtype")
+    if k_weight is not None and (k_weight.dtype is not dtype or k_weight.numel() != dim or
+                                 not (k_weight.is_cuda and k_weight.is_contiguous())):
+        raise ValueError("k_weight must be a contiguous [head_dim] CUDA tensor of the inputs' dtype")
     if cos_sin is None:
         return None, 0, 0
-    if cos_sin.dtype is not torch.float32 or cos_sin.dim() != 2 or not (cos_sin.is_cuda and cos_sin.is_contiguous()):
+    max_pos, rotary = cos_sin.shape
+    if cos_sin.dtype is not torch.float32 or not (cos_sin.is_cuda and cos_sin.is_contiguous()):
         raise ValueError("cos_sin must be a contiguous [max_pos, rotary_dim] fp32 CUDA tensor")
-    return cos_sin.data_ptr(), *cos_sin.shape
+    return cos_sin.data_ptr(), max_pos, rotary
 
 
 def _int32(names, *tensors):
@@ -253,29 +257,33 @@ def qk_norm_rope(q, k, cos_sin, positions, q_weight=None, k_weight=None, interle
     dtype = _DTYPES.get(dt)
     if dtype is None:
         raise ValueError("q and k must be bf16 or fp32")
-    t, hq, d = x.shape
+    t, hq, d = shape = x.shape
     hk = qs = ks = qos = kos = 0
     qp = kp = qop = kop = None
     if q is not None:
-        qs = _heads("q", q, dt)
+        qos = hq * d  # of a contiguous tensor
+        qs = qos if q.is_contiguous() and q.is_cuda else _heads("q", q, dt)
         if q_out is None:
-            q_out = torch.empty((t, hq, d), dtype=dt, device=q.device)
-        elif q_out.shape != q.shape:
-            raise ValueError("q_out must have q's shape")
-        qos = qs if q_out is q else _heads("q_out", q_out, dt)
+            q_out = torch.empty(shape, dtype=dt, device=q.device)
+        elif q_out.shape != shape or q_out.dtype is not dt:
+            raise ValueError("q_out must have q's shape and dtype")
+        elif not (q_out.is_contiguous() and q_out.is_cuda):
+            qos = _heads("q_out", q_out, dt)
         qp, qop = q.data_ptr(), q_out.data_ptr()
     else:
         hq = 0
     if k is not None:
-        n, hk, dk = k.shape
-        if n != t or dk != d:
-            raise ValueError("q and k must have the same tokens and head_dim")
-        ks = _heads("k", k, dt)
+        n, hk, dk = shape = k.shape
+        if n != t or dk != d or k.dtype is not dt:
+            raise ValueError("q and k must have the same tokens, head_dim and dtype")
+        kos = hk * d
+        ks = kos if k.is_contiguous() and k.is_cuda else _heads("k", k, dt)
         if k_out is None:
-            k_out = torch.empty((t, hk, d), dtype=dt, device=k.device)
-        elif k_out.shape != k.shape:
-            raise ValueError("k_out must have k's shape")
-        kos = ks if k_out is k else _heads("k_out", k_out, dt)
+            k_out = torch.empty(shape, dtype=dt, device=k.device)
+        elif k_out.shape != shape or k_out.dtype is not dt:
+            raise ValueError("k_out must have k's shape and dtype")
+        elif not (k_out.is_contiguous() and k_out.is_cuda):
+            kos = _heads("k_out", k_out, dt)
         kp, kop = k.data_ptr(), k_out.data_ptr()
     table, max_pos, rotary = _rotation(cos_sin, q_weight, k_weight, dt, d)
     if positions.dtype is not torch.int32 or positions.numel() != t or not (positions.is_cuda and positions.is_contiguous()):
@@ -309,8 +317,11 @@ def qkv_append(qkv, k_cache, v_cache, cu_new, cu_kv, block_table, page_size: int
         raise ValueError("the caches must be contiguous CUDA tensors")
     _int32("cu_new cu_kv block_table positions", cu_new, cu_kv, block_table, positions)
     if torch.is_tensor(qkv):
-        qs = ks = vs = _heads("qkv", qkv, dt)
         t, heads, dim = qkv.shape
+        if qkv.is_contiguous() and qkv.is_cuda and qkv.dtype is dt:
+            qs = ks = vs = heads * dim
+        else:
+            qs = ks = vs = _heads("qkv", qkv, dt)
         hq = heads - 2 * hkv
         if hq < 0:
             raise ValueError("qkv holds fewer heads than the caches' keys and values have")
@@ -336,9 +347,10 @@ def qkv_append(qkv, k_cache, v_cache, cu_new, cu_kv, block_table, page_size: int
     else:
         if q_out is None:
             q_out = torch.empty((t, hq, d), dtype=dt, device=k_cache.device)
-        elif q_out.shape != (t, hq, d):
-            raise ValueError("q_out must be [tokens, query heads, head_dim]")
-        qos, qop = _heads("q_out", q_out, dt), q_out.data_ptr()
+        elif q_out.shape != (t, hq, d) or q_out.dtype is not dt:
+            raise ValueError("q_out must be [tokens, query heads, head_dim] of the caches' dtype")
+        qos = hq * d if q_out.is_contiguous() and q_out.is_cuda else _heads("q_out", q_out, dt)
+        qop = q_out.data_ptr()
     if ws is None:
         ws = workspace(256, k_cache.device)
     page_size = int(page_size)
@@ -370,13 +382,13 @@ def chunk_attention_paged(q, k_cache, v_cache, cu_q, cu_kv, block_table, page_si
     `window` keys that end with its own.  Returns (o, lse_or_None)."""
     lib = load()
     dt = q.dtype
-    stride = _heads("q", q, dt)
+    t, hq, d = shape = q.shape
+    stride = hq * d if q.is_contiguous() and q.is_cuda else _heads("q", q, dt)
     _cuda("k_cache v_cache out lse", k_cache, v_cache, out, lse)
     _int32("cu_q cu_kv block_table", cu_q, cu_kv, block_table)
     dtype = _DTYPES.get(dt)
     if dtype is None or k_cache.dtype is not dt or v_cache.dtype is not dt:
         raise ValueError("q, k_cache, v_cache must share one dtype")
-    t, hq, d = shape = q.shape
     rows, hkv, dk = caches = k_cache.shape
     if dk != d or v_cache.shape != caches:
         raise ValueError("q and the caches must share one head_dim, the caches one shape")
