@@ -240,7 +240,7 @@ int bp_chunk_attention_paged(const void* q, int64_t q_stride, const void* k_cach
     if (mask != BP_MASK_CAUSAL_BLOCK && mask != BP_MASK_BIDIR_BLOCK) return BP_ERR_INVALID_ARG;
     if (dtype != BP_F32 && dtype != BP_BF16) return BP_ERR_INVALID_ARG;
     if (!(softmax_scale >= 0.f) || isinf(softmax_scale)) return BP_ERR_INVALID_ARG;
-    if (pages_per_seq < 1 || num_pages < 1 || !valid_page_size(page_size)) return BP_ERR_INVALID_ARG;
+    if (max_q_len < 1 || pages_per_seq < 1 || num_pages < 1 || !valid_page_size(page_size)) return BP_ERR_INVALID_ARG;
     if ((long long)pages_per_seq * page_size < max_kv_len || (long long)num_pages * page_size > INT32_MAX)
         return BP_ERR_INVALID_ARG;
     if (q_stride < (int64_t)num_q_heads * head_dim) return BP_ERR_INVALID_ARG;
@@ -257,7 +257,7 @@ int bp_chunk_attention_paged(const void* q, int64_t q_stride, const void* k_cach
     a.q = q; a.q_stride = q_stride; a.k_cache = k_cache; a.v_cache = v_cache; a.o = o; a.lse = lse;
     a.cu_q = cu_q; a.cu_kv = cu_kv; a.block_table = block_table;
     a.pages_per_seq = pages_per_seq; a.page_size = page_size; a.num_pages = num_pages;
-    a.num_seqs = num_seqs; a.total_q = total_q;
+    a.num_seqs = num_seqs; a.total_q = total_q; a.max_q_len = max_q_len;
     a.num_q_heads = num_q_heads; a.num_kv_heads = num_kv_heads; a.head_dim = head_dim;
     a.mask = mask; a.window = window;
     a.scale = softmax_scale == 0.f ? 1.f / sqrtf((float)head_dim) : softmax_scale;

@@ -69,7 +69,8 @@ struct ChunkParams {
     float* part_o;   // [grid][2][D / 8][256][8] (part_at): the first stretch's part (it began in an earlier CTA) and the last one's
     float2* part_ml; // [grid][2][256]
     unsigned long long grid_inverse;  // 2^64 / the grid, rounded down
-    int4* info;      // [grid]: flags, and the sequence, head and tile that the CTA began and did not end
+    int4* info;      // [grid]: flags; of the tile that the CTA began and did not end, its first token's row among the
+                     // queries, its tokens and its KV head
     unsigned int* err;
 };
 enum : int { kHasTail = 1, kHasHead = 2, kHeadEnds = 4 };
@@ -752,7 +753,8 @@ chunk_attention_kernel(const __grid_constant__ ChunkParams p, const __grid_const
                 const Job g = *job;
                 had_job(nj);
                 if (!g.first) left.x |= kHasHead | (g.last ? kHeadEnds : 0);
-                if (g.first && !g.last) left = make_int4(left.x | kHasTail, g.s, g.h, g.t);
+                if (g.first && !g.last)
+                    left = make_int4(left.x | kHasTail, g.q0 + g.t * 2 * p.tokens, min(2 * p.tokens, g.B - g.t * 2 * p.tokens), g.h);
                 if (g.j1 <= g.j0) continue;
                 if (g.j1 * kKeys > g.n) {
                     const unsigned x = x0 + 2 * (g.j1 - 1 - g.j0) + 1;
@@ -787,34 +789,35 @@ chunk_attention_kernel(const __grid_constant__ ChunkParams p, const __grid_const
 // Merges the parts of every work tile that was cut: block (c, y) rows [32 y, 32 y + 32) of the tile that CTA c began and
 // did not end.  Its parts are c's last and the first ones of the CTAs behind it, up to the one that ends it.  A warp has a row:
 // its lanes take the parts' (m, l), 32 at a time, and weigh them; then 4 columns each, all parts' loads in flight.
+// BATCH parts' loads are in flight at once: 4 where tiles have many rows (they are cut once or twice, and the registers are
+// better spent on more blocks: 12 took 14 us more for a prompt of 8192), 16 where every sequence has one tile (its context
+// may be cut for all CTAs: one token over 2048 keys took 18.7 us with 8 of them).
 constexpr int kMergeThreads = 512, kMergeRows = 32;
-template <int D>
-__global__ void __launch_bounds__(kMergeThreads) chunk_merge_kernel(const __grid_constant__ ChunkParams p, int grid) {
+template <int D, int BATCH>
+__global__ void __launch_bounds__(kMergeThreads, BATCH <= 4 ? 3 : 1) chunk_merge_kernel(const __grid_constant__ ChunkParams p, int grid) {
     griddep_launch_dependents();
     griddep_wait();
     const int c = blockIdx.x, i = blockIdx.y * kMergeRows / kTileM, r0 = blockIdx.y * kMergeRows % kTileM, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int4 mine = p.info[c];
-    if (!(mine.x & kHasTail)) return;
-    const int tok0 = mine.w * 2 * p.tokens + i * p.tokens;
-    const int q0 = p.cu_q[mine.y], rows = min(p.tokens, p.cu_q[mine.y + 1] - q0 - tok0) * p.group;
-    if (r0 + warp >= rows) return;
-    int last = c + 1;  // the CTA that ends the tile
-    for (int base = c + 1; base < grid; base += 32) {
-        const unsigned hit = __ballot_sync(0xffffffffu, base + lane < grid && (p.info[base + lane].x & kHeadEnds));
-        if (hit) {
-            last = base + __ffs(hit) - 1;
-            break;
-        }
-    }
+    // this CTA's entry and the 31 behind it, in one round trip
+    const int4 near = c + lane < grid ? p.info[c + lane] : make_int4(0, 0, 0, 0);
+    if (!(__shfl_sync(0xffffffffu, near.x, 0) & kHasTail)) return;
+    const int row0 = __shfl_sync(0xffffffffu, near.y, 0), tokens = __shfl_sync(0xffffffffu, near.z, 0);
+    const int head = __shfl_sync(0xffffffffu, near.w, 0);
+    const int rows = min(p.tokens, tokens - i * p.tokens) * p.group;  // of this stream
     constexpr int kCols = D / 32;
     for (int r = r0 + warp; r < min(rows, r0 + kMergeRows); r += kMergeThreads / 32) {
         const int row = i * kTileM + r;
         float acc[kCols] = {}, m = -INFINITY, l = 0.f;
-        for (int base = c; base <= last; base += 32) {
+        bool more = true;
+        for (int base = c; more; base += 32) {  // 32 CTAs at a time
             const int e = base + lane;
+            const int flags = base == c ? near.x : e < grid ? p.info[e].x : 0;
+            const unsigned ends = __ballot_sync(0xffffffffu, e > c && (flags & kHeadEnds));
+            const int n = ends ? __ffs(ends) : min(32, grid - base);  // of them, up to the one that ends the tile
+            more = !ends && base + 32 < grid;
             const size_t slot = (size_t)e * 2 + (e == c ? 1 : 0);
             float2 ml = make_float2(-INFINITY, 0.f);
-            if (e <= last && (e == c || (p.info[e].x & kHasHead))) ml = p.part_ml[slot * (2 * kTileM) + row];
+            if (lane < n && (e == c || (flags & kHasHead))) ml = p.part_ml[slot * (2 * kTileM) + row];
             if (!(ml.y > 0.f)) ml = make_float2(-INFINITY, 0.f);  // (no key seen: its columns count for nothing)
             float top = ml.x;
 #pragma unroll
@@ -829,26 +832,33 @@ __global__ void __launch_bounds__(kMergeThreads) chunk_merge_kernel(const __grid
             m = m_new;
 #pragma unroll
             for (int d = 0; d < kCols; ++d) acc[d] *= w_old;
-            const int n = min(32, last + 1 - base);
-#pragma unroll 8
-            for (int k = 0; k < n; ++k) {
-                const float wk = __shfl_sync(0xffffffffu, w, k);
-                const size_t s = (size_t)(base + k) * 2 + (base + k == c ? 1 : 0);
-                const float* o = p.part_o + part_at<D>(s, row, lane * kCols / 8 * 8) + lane * kCols % 8;
-                float v[kCols];
-                if constexpr (kCols == 4) {
-                    const float4 t = *reinterpret_cast<const float4*>(o);
-                    v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
-                } else {
-                    const float2 t = *reinterpret_cast<const float2*>(o);
-                    v[0] = t.x; v[1] = t.y;
+#pragma unroll 1
+            for (int k0 = 0; k0 < n; k0 += BATCH) {
+                float v[BATCH][kCols];
+#pragma unroll
+                for (int k = 0; k < BATCH; ++k) {
+                    const size_t s = (size_t)(base + k0 + k) * 2 + (base + k0 + k == c ? 1 : 0);
+                    const float* o = p.part_o + part_at<D>(s, row, lane * kCols / 8 * 8) + lane * kCols % 8;
+                    if (k0 + k >= n) break;
+                    if constexpr (kCols == 4) {
+                        const float4 t = *reinterpret_cast<const float4*>(o);
+                        v[k][0] = t.x; v[k][1] = t.y; v[k][2] = t.z; v[k][3] = t.w;
+                    } else {
+                        const float2 t = *reinterpret_cast<const float2*>(o);
+                        v[k][0] = t.x; v[k][1] = t.y;
+                    }
                 }
 #pragma unroll
-                for (int d = 0; d < kCols; ++d) acc[d] += wk > 0.f ? wk * v[d] : 0.f;  // (a slot without a part holds anything)
+                for (int k = 0; k < BATCH; ++k) {
+                    if (k0 + k >= n) break;
+                    const float wk = __shfl_sync(0xffffffffu, w, k0 + k);
+#pragma unroll
+                    for (int d = 0; d < kCols; ++d) acc[d] += wk > 0.f ? wk * v[k][d] : 0.f;  // (a slot without a part holds anything)
+                }
             }
         }
         const float inv = l > 0.f ? 1.f / l : 0.f;
-        const size_t orow = (size_t)(q0 + tok0 + r / p.group) * p.num_q_heads + mine.z * p.group + r % p.group;
+        const size_t orow = (size_t)(row0 + i * p.tokens + r / p.group) * p.num_q_heads + head * p.group + r % p.group;
         __nv_bfloat16* out = p.o + orow * D + lane * kCols;
         if constexpr (kCols == 4)
             *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
@@ -928,10 +938,15 @@ int run(const ChunkAttentionArgs& a, const DeviceInfo& dev, cudaStream_t stream)
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     if (cudaLaunchKernelEx(&cfg, chunk_attention_kernel<D>, p, qmap, kmap, vmap) != cudaSuccess) return BP_ERR_CUDA;
-    cfg.gridDim = dim3((unsigned)grid, 2 * kTileM / kMergeRows, 1);
+    // (rows behind the first stream's only where some sequence may have them)
+    const bool few = a.max_q_len <= p.tokens;
+    const int merge_rows = few ? a.max_q_len * p.group : 2 * kTileM;
+    cfg.gridDim = dim3((unsigned)grid, (unsigned)((merge_rows + kMergeRows - 1) / kMergeRows), 1);
     cfg.blockDim = dim3(kMergeThreads, 1, 1);
     cfg.dynamicSmemBytes = 0;
-    return cudaLaunchKernelEx(&cfg, chunk_merge_kernel<D>, p, grid) == cudaSuccess ? BP_OK : BP_ERR_CUDA;
+    const cudaError_t e = few ? cudaLaunchKernelEx(&cfg, chunk_merge_kernel<D, 16>, p, grid)
+                              : cudaLaunchKernelEx(&cfg, chunk_merge_kernel<D, 4>, p, grid);
+    return e == cudaSuccess ? BP_OK : BP_ERR_CUDA;
 }
 
 }  // namespace

@@ -71,7 +71,7 @@ def test_append_refusals(lib, change, status):
 @pytest.mark.parametrize("change,status", [
     (dict(t=-1), INVALID), (dict(q=None), INVALID), (dict(o=None), INVALID), (dict(bt=None), INVALID), (dict(hq=30), INVALID),
     (dict(hk=0), INVALID), (dict(mask=2), INVALID), (dict(dt=9), INVALID), (dict(win=-1), INVALID), (dict(scale=-1.0), INVALID),
-    (dict(scale=float("nan")), INVALID), (dict(page=96), INVALID), (dict(mk=641), INVALID), (dict(np=1 << 26), INVALID),
+    (dict(scale=float("nan")), INVALID), (dict(page=96), INVALID), (dict(mk=641), INVALID), (dict(mq=0), INVALID), (dict(np=1 << 26), INVALID),
     (dict(qs=4095), INVALID), (dict(qs=4100), INVALID), (dict(q=P + 4), INVALID), (dict(k=P + 8), INVALID),
     (dict(dt=0), UNSUPPORTED), (dict(d=96), UNSUPPORTED), (dict(hq=129, hk=1, qs=129 * 128), UNSUPPORTED),
     (dict(ws=None), WORKSPACE), (dict(ws=WS + 8), WORKSPACE), (dict(wsb=256), WORKSPACE), (dict(t=0, q=None), OK),
