@@ -259,7 +259,8 @@ int bp_chunk_attention_paged(const void* q, int64_t q_stride, const void* k_cach
     a.pages_per_seq = pages_per_seq; a.page_size = page_size; a.num_pages = num_pages;
     a.num_seqs = num_seqs; a.total_q = total_q; a.max_q_len = max_q_len;
     a.num_q_heads = num_q_heads; a.num_kv_heads = num_kv_heads; a.head_dim = head_dim;
-    a.mask = mask; a.window = window;
+    a.mask = mask;
+    a.window = window >= max_kv_len ? 0 : window;  // (no sequence is longer: every key is within it)
     a.scale = softmax_scale == 0.f ? 1.f / sqrtf((float)head_dim) : softmax_scale;
     a.scratch = scratch(workspace);
     a.err_word = err_word(workspace);

@@ -349,6 +349,61 @@ def test_empty_calls():
     assert bp.qkv_append(z(0, 4, 64), z(16, 1, 64), z(16, 1, 64), _offsets([0]), _offsets([5]), table, 16, None).shape == (0, 2, 64)
 
 
+def test_more_tokens_than_a_grid_has_rows():
+    """Half a million tokens: blocks take more than one group of tokens."""
+    g = _gen(11)
+    t = 65535 * 8 + 1003
+    q = torch.randn(t, 1, 16, device="cuda", generator=g)
+    pos = torch.randint(0, 50, (t,), device="cuda", generator=g).to(torch.int32)
+    table = _table(50, 16)
+    ws = bp.workspace(256, "cuda")
+    out, _ = bp.qk_norm_rope(q, None, table, pos, ws=ws)
+    assert bp.get_status(ws) == 0
+    _near_turned(out, _turned(q, None, table, pos, False, 1e-6))
+
+
+def test_offsets_beyond_32_bits():
+    """Pages whose rows lie more than 2^31 elements into their pool, by append and attention."""
+    g = _gen(12)
+    hkv, dim, page, ctx, new = 8, 128, 64, 100, 60
+    rows = (2 ** 31 // (hkv * dim) // page + 40) * page
+    kc, vc = [torch.empty(rows, hkv, dim, device="cuda", dtype=torch.bfloat16) for _ in range(2)]
+    table = torch.tensor([[rows // page - 1, 1, rows // page - 30]], dtype=torch.int32, device="cuda")
+    j = torch.arange(ctx + new, device="cuda")
+    at = table[0].long()[j // page] * page + j % page
+    for c in (kc, vc):
+        c[at[:ctx]] = torch.randn(ctx, hkv, dim, device="cuda", generator=g).to(torch.bfloat16)
+    qkv = torch.randn(new, 16 + 2 * hkv, dim, device="cuda", generator=g).to(torch.bfloat16)
+    ws = bp.workspace(bp.chunk_attention_workspace_size(1, new, 16, hkv, dim), "cuda")
+    q = bp.qkv_append(qkv, kc, vc, _offsets([new]), _offsets([ctx + new]), table, page, None, ws=ws)
+    assert torch.equal(q, qkv[:, :16]) and torch.equal(kc[at[ctx:]], qkv[:, 16:24]) and torch.equal(vc[at[ctx:]], qkv[:, 24:])
+    o, _ = bp.chunk_attention_paged(q, kc, vc, _offsets([new]), _offsets([ctx + new]), table, page, new, ctx + new, ws=ws)
+    assert bp.get_status(ws) == 0
+    ref, size, _ = _attend(q, kc, vc, at, True, 0, dim ** -0.5)
+    assert torch.all((o.double() - ref).abs() <= (U + 1e-3) * size + U * ref.abs() + 1e-30)
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 400])
+def test_a_window_over_everything(window):
+    """Wider than every context: the same bits as without one, rows without keys among them."""
+    args = dict(ctx=(-50, 200, 0), new=(80, 150, 300), causal=False)
+    assert torch.equal(_check_chunk(**args, window=window), _check_chunk(**args))
+
+
+def test_batch_does_not_matter():
+    """Many sequences (more than one round of the plan), and rows of other sequences that are not numbers."""
+    ctx, new = tuple(range(0, 1400, 20)), (1, 3, 40, 0, 2) * 14
+    _check_chunk(ctx, new, hq=4, hkv=1, dim=64)
+    g = _gen(5)
+    (kc, vc), table, keys = _paged([70, 30], 16, 1, 64, torch.bfloat16, g, [70, 30])
+    q = torch.randn(25, 2, 64, device="cuda", generator=g).to(torch.bfloat16)
+    q[20:] = math.nan  # the second sequence's
+    ws = bp.workspace(bp.chunk_attention_workspace_size(2, 25, 2, 1, 64), "cuda")
+    o, _ = bp.chunk_attention_paged(q, kc, vc, _offsets([20, 5]), _offsets([70, 30]), table, 16, 20, 70, ws=ws)
+    ref, size, _ = _attend(q[:20], kc, vc, keys[0], True, 0, 0.125)
+    assert torch.all((o[:20].double() - ref).abs() <= (U + 1e-3) * size + U * ref.abs() + 1e-30) and torch.isnan(o[20:].float()).all()
+
+
 def test_example_runs():
     """The example's prompts give the same rows in chunks as at once, and its block the same as a chunk, up to the
     rounding of two layers' bf16 activations (a few roundings of 2^-9 on average each: below 2e-2 of a row's size)."""
