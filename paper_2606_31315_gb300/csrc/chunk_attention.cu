@@ -681,7 +681,6 @@ chunk_attention_kernel(const __grid_constant__ ChunkParams p, const __grid_const
             const uint32_t k_lo = (uint32_t)smem_desc(smem_addr(sKV), 16, 0, 0);
             const uint32_t v_lo = (uint32_t)smem_desc(smem_addr(sKV), kHalfBytes, 0, 0);
             const uint32_t t_s = tmem + i * 128, t_o = tmem + S::col_o + i * D;
-            auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, kWaitBudget)) != 0; };
             // this stream's arrival on `bar`: when its MMAs so far are done, or at once if it had none there
             auto release = [&](uint64_t* bar, bool used) {
                 if (used) umma_commit(bar); else mbar_arrive(bar);
@@ -694,21 +693,22 @@ chunk_attention_kernel(const __grid_constant__ ChunkParams p, const __grid_const
                 const int a = g->a[i], b = g->b[i], j0 = g->j0, j1 = g->j1, n = g->n;
                 had_job(nj);
                 if (j1 <= j0) continue;
-                fine = wait(&sh.q_full, nq & 1);
-                for (int j = j0; j <= j1 && fine; ++j, ++turn, x += 2) {  // x: K of tile j
-                    const int kslot = x % S::slots, vslot = (x - 1) % S::slots;
-                    const bool pv = j > a && j <= b, qk = j >= a && j < b;
-                    if (j < j1) fine = wait(&sh.full[kslot], (x / S::slots) & 1);
-                    if (fine && j > j0) fine = wait(&sh.full[vslot], ((x - 1) / S::slots) & 1);
-                    if (fine && pv) fine = wait(&sh.p[i], np++ & 1);
-                    if (fine) fine = wait(&sh.turn[i], (turn & 1) ^ (i ^ 1));
-                    if (!fine) break;
-                    tc_fence_after();
-                    // keys past the sequence's last in steps of 16: the tail warp has cleared the rest of a step
-                    const int steps = pv ? min(kKeys / 16, (n - (j - 1) * kKeys + 15) / 16) : 0;
-                    const uint32_t vl = v_lo + vslot * (S::tile_bytes >> 4), kl = k_lo + kslot * (S::tile_bytes >> 4);
-                    uint32_t on = j - 1 > a ? 1u : 0u;
-                    if (elect_one()) {
+                if (elect_one()) {  // one thread throughout: its waits need no votes, its operands are known to be uniform
+                    fine = mbar_wait(&sh.q_full, nq & 1, kWaitBudget);
+                    unsigned xk = x, my_turn = turn, my_p = np;
+                    for (int j = j0; j <= j1 && fine; ++j, ++my_turn, xk += 2) {  // xk: K of tile j
+                        const int kslot = xk % S::slots, vslot = (xk - 1) % S::slots;
+                        const bool pv = j > a && j <= b, qk = j >= a && j < b;
+                        if (j < j1) fine = mbar_wait(&sh.full[kslot], (xk / S::slots) & 1, kWaitBudget);
+                        if (fine && j > j0) fine = mbar_wait(&sh.full[vslot], ((xk - 1) / S::slots) & 1, kWaitBudget);
+                        if (fine && pv) fine = mbar_wait(&sh.p[i], my_p++ & 1, kWaitBudget);
+                        if (fine) fine = mbar_wait(&sh.turn[i], (my_turn & 1) ^ (i ^ 1), kWaitBudget);
+                        if (!fine) break;
+                        tc_fence_after();
+                        // keys past the sequence's last in steps of 16: the tail warp has cleared the rest of a step
+                        const int steps = pv ? min(kKeys / 16, (n - (j - 1) * kKeys + 15) / 16) : 0;
+                        const uint32_t vl = v_lo + vslot * (S::tile_bytes >> 4), kl = k_lo + kslot * (S::tile_bytes >> 4);
+                        uint32_t on = j - 1 > a ? 1u : 0u;
                         // O += P V of tile j - 1 (P's 64-key halves lie 64 columns apart)
                         if (steps == kKeys / 16) {
 #pragma unroll
@@ -737,13 +737,15 @@ chunk_attention_kernel(const __grid_constant__ ChunkParams p, const __grid_const
                         if (pv && j == b) umma_commit(&sh.o[i]);
                         if (j > j0) release(&sh.empty[vslot], pv);
                         if (j < j1) release(&sh.empty[kslot], qk);
-                        if (j == j1 - 1) release(&sh.q_empty, any || qk);
+                        if (j == j1 - 1) release(&sh.q_empty, any || b > a);
                     }
-                    __syncwarp();
-                    any = any || qk;
                 }
-                x -= 2;  // (the step behind the last tile has no K)
+                x += 2 * (j1 - j0);
+                turn += j1 - j0 + 1;
+                np += max(0, b - a);
+                any = any || b > a;
                 ++nq;
+                fine = __all_sync(0xffffffffu, fine);
                 if (!fine) break;
             }
             if ((!fine || !ok) && lane == 0) raise_error(p.err, kErrTimeout);
