@@ -257,7 +257,7 @@ int bp_chunk_attention_paged(const void* q, int64_t q_stride, const void* k_cach
     a.q = q; a.q_stride = q_stride; a.k_cache = k_cache; a.v_cache = v_cache; a.o = o; a.lse = lse;
     a.cu_q = cu_q; a.cu_kv = cu_kv; a.block_table = block_table;
     a.pages_per_seq = pages_per_seq; a.page_size = page_size; a.num_pages = num_pages;
-    a.num_seqs = num_seqs; a.total_q = total_q; a.max_q_len = max_q_len;
+    a.num_seqs = num_seqs; a.total_q = total_q; a.max_q_len = max_q_len; a.max_kv_len = max_kv_len;
     a.num_q_heads = num_q_heads; a.num_kv_heads = num_kv_heads; a.head_dim = head_dim;
     a.mask = mask;
     a.window = window >= max_kv_len ? 0 : window;  // (no sequence is longer: every key is within it)

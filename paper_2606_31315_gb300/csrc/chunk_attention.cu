@@ -49,6 +49,7 @@ constexpr uint32_t kChunkTmem = 512;
 // with 448, 374 with 640.
 constexpr int kTileCost = 400;
 constexpr int kLeastCost = 2 * kKeys;            // of a CTA's stretch: below it, fewer CTAs take part
+constexpr int kLeastCut = 2;                     // key tiles on either side of a cut
 constexpr int kJobs = 4;                         // jobs laid out ahead
 
 template <int D>
@@ -175,11 +176,9 @@ __device__ __forceinline__ Place place_in(const ChunkParams& p, int s, const Seq
     int first, count;
     tile_span(q, at.t, first, count);
     at.j = off <= kTileCost ? 0 : min(count, (off - kTileCost + kKeys / 2) / kKeys);
-    // (two key tiles at least on either side of a cut, whose parts are up to 256 rows; few rows are cut anywhere)
-    const int least = q.B <= p.tokens ? 1 : 2;
-    const bool whole = count < 2 * least;  // not to be cut: the nearer end
-    if (whole ? 2 * off >= w : count - at.j < least) at.j = 0, ++at.t;
-    else if (whole || at.j < least) at.j = 0;
+    const bool whole = count < 2 * kLeastCut;  // not to be cut: the nearer end
+    if (whole ? 2 * off >= w : count - at.j < kLeastCut) at.j = 0, ++at.t;
+    else if (whole || at.j < kLeastCut) at.j = 0;
     if (at.t == T) at.t = 0, ++at.h;
     if (at.h == p.num_kv_heads) at.h = 0, ++at.s;
     return at;
@@ -948,6 +947,7 @@ int run(const ChunkAttentionArgs& a, const DeviceInfo& dev, cudaStream_t stream)
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     if (cudaLaunchKernelEx(&cfg, chunk_attention_kernel<D>, p, qmap, kmap, vmap) != cudaSuccess) return BP_ERR_CUDA;
+    if (a.max_kv_len <= (2 * kLeastCut - 1) * kKeys) return BP_OK;  // too short to be cut: nothing to merge
     // (rows behind the first stream's only where some sequence may have them)
     const bool few = a.max_q_len <= p.tokens;
     const int merge_rows = few ? a.max_q_len * p.group : 2 * kTileM;

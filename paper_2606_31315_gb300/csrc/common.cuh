@@ -109,7 +109,7 @@ struct ChunkAttentionArgs {
     const int32_t* cu_q;
     const int32_t* cu_kv;
     const int32_t* block_table;
-    int pages_per_seq, page_size, num_pages, num_seqs, total_q, max_q_len;
+    int pages_per_seq, page_size, num_pages, num_seqs, total_q, max_q_len, max_kv_len;
     int num_q_heads, num_kv_heads, head_dim;
     int mask, window;
     float scale;
