@@ -8,9 +8,10 @@
 //
 // All in fp32, rounded once to the output's type.  A head is a row of pieces, one a lane; the lanes of a head sum the
 // squares by shuffles.  In the usual form (halves, the whole head turned) a lane has a piece of either half, so that its
-// pairs are its own; in the others it gets their other elements from the lane that has them.  A round is the 32 / LANES heads that a warp has at once: queries, keys or values, the same in all its lanes.
-// A warp has all of a token's rounds (fewer in small calls), the next one in flight, and forms the token's cosines
-// and sines times the norm's weights once for all of a kind.
+// pairs are its own; in the others it gets their other elements from the lane that has them.  A round is the 32 / LANES
+// heads that a warp has at once: queries, keys or values, the same in all its lanes.  A warp has all of a token's rounds
+// (fewer in small calls), the next one in flight, and forms the token's cosines and sines times the norm's weights once
+// for all of a kind.
 //
 // Memory bounds it: nothing is read or written twice.  What it takes to get near is few instructions (215 a KB with
 // eight elements a lane and their pairs in another one, half of that now) and warps enough to hide a token's chain of
