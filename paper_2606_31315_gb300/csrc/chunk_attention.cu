@@ -73,6 +73,7 @@ struct ChunkParams {
     int num_seqs, num_q_heads, num_kv_heads, group;
     int tokens;  // of one stream's tile: floor(128 / group)
     int pages_per_seq, page_shift, num_pages;
+    int max_q, max_kv;  // of a sequence: the merge's launch rests on them
     int causal, window;
     float scale_log2;
     float* part_o;   // [grid][2][D / 8][256][8] (part_at): the first stretch's part (it began in an earlier CTA) and the last one's
@@ -197,6 +198,7 @@ struct Walk {
                 q = load_seq(p, at.s);
                 q0 = __ldg(p.cu_q + at.s);
                 known = at.s;
+                if (q.B > p.max_q || (q.B > 0 && q.n > p.max_kv)) raise_error(p.err, kErrDeviceArg);
             }
             const int T = q.tiles();
             if (T <= 0) {
@@ -895,6 +897,8 @@ int run(const ChunkAttentionArgs& a, const DeviceInfo& dev, cudaStream_t stream)
     p.page_shift = 0;
     while ((1 << p.page_shift) < a.page_size) ++p.page_shift;
     p.num_pages = a.num_pages;
+    p.max_q = a.max_q_len;
+    p.max_kv = a.max_kv_len;
     p.causal = a.mask == BP_MASK_CAUSAL_BLOCK;
     p.window = a.window;
     p.scale_log2 = a.scale * 1.4426950408889634f;

@@ -339,6 +339,17 @@ def test_a_bad_page_is_reported():
     assert bp.get_status(ws) == bp._binding.BP_ERR_DEVICE_FLAG
 
 
+@pytest.mark.parametrize("max_q, max_kv", [(63, 1200), (64, 1199), (1, 300), (64, 1200), (1000, 1216)])
+def test_a_sequence_past_the_bounds_is_reported(max_q, max_kv):
+    """The merge is sized by the bounds, so a longer sequence than they say must not pass unnoticed."""
+    g = _gen(12)
+    (kc, vc), table, _ = _paged([900, 1200], 64, 1, 64, torch.bfloat16, g, [900, 1200])
+    q = torch.randn(65, 2, 64, device="cuda", generator=g).to(torch.bfloat16)
+    ws = bp.workspace(bp.chunk_attention_workspace_size(2, 65, 2, 1, 64), "cuda")
+    bp.chunk_attention_paged(q, kc, vc, _offsets([1, 64]), _offsets([900, 1200]), table, 64, max_q, max_kv, ws=ws)
+    assert bp.get_status(ws) == (0 if max_q >= 64 and max_kv >= 1200 else bp._binding.BP_ERR_DEVICE_FLAG)
+
+
 def test_empty_calls():
     z = lambda *s: torch.zeros(*s, device="cuda", dtype=torch.bfloat16)  # noqa: E731
     ws = bp.workspace(bp.chunk_attention_workspace_size(1, 0, 2, 1, 64), "cuda")
