@@ -21,7 +21,7 @@
 //
 // What bounds it: of a pair of key tiles' 2 x 16 MMAs, 2,048 cycles at D = 128, about 2,950 are taken: a stream's softmax
 // (1,050), its MMAs (1,024) and the hand-overs between them follow one another, with two streams in turn.  2048 tokens
-// over 32768 keys, 32 query and 8 KV heads: 700 to 750 us, 1.42 to 1.52 PFLOP/s; a prompt of 8192: 364 to 400 us; one
+// over 32768 keys, 32 query and 8 KV heads: 700 to 770 us, 1.38 to 1.52 PFLOP/s; a prompt of 8192: 364 to 400 us; one
 // token over 2048 keys: 16 us, a chain of latencies (9 over 100 keys, which need no merge).  The code's length counts: it runs from an instruction cache that
 // all roles share (MMA loops of twice the code took 20 % more, not unrolled ones 50 %).
 #include <cuda_bf16.h>
