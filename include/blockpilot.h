@@ -206,7 +206,8 @@ BP_API int bp_qkv_append(const void* q, int64_t q_stride, const void* k_new, int
  *                       lo = max(0, p + 1 - window), or 0 where window is 0
  *   O[i,h] = sum_j softmax_j(scale * <q_{i,h}, k_{j,h/g}>) v_{j,h/g},  g = num_q_heads / num_kv_heads
  *
- * A row that sees no key (a sequence with fewer keys than new tokens has such rows) gets 0, and -inf in lse.
+ * A row that sees no key (a sequence with fewer keys than new tokens has such rows) gets 0, and -inf in lse.  A NaN in a
+ * row's query or in a key that it sees, or a score that overflows fp32, makes the row NaN, and its lse.
  *   q        rows of [num_q_heads][head_dim] bf16, q_stride elements from a token to the next; o [total_q][num_q_heads]
  *            [head_dim] bf16; lse [total_q][num_q_heads] fp32 or NULL
  *   cu_q, cu_kv, block_table, pages_per_seq, page_size, k_cache, v_cache  as bp_block_attention_paged, but of a page's

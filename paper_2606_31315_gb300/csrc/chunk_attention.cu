@@ -98,6 +98,15 @@ __device__ __forceinline__ float chunk_exp2(float x) {
     return y;
 }
 
+// What a row's maximum and sum say of it.  A row saw no key where its maximum is still -inf and its sum 0 (the least sum
+// otherwise is the weight of the maximum); all others are divided by what was summed, so that a NaN or an overflow, which
+// makes the sum a NaN, shows in the output and in the log-sum-exp.
+__device__ __forceinline__ bool saw_no_key(float m, float l) { return m == -INFINITY && l == 0.f; }
+__device__ __forceinline__ float row_inverse(float m, float l) { return saw_no_key(m, l) ? 0.f : 1.f / l; }
+__device__ __forceinline__ float row_lse(float m, float l) {
+    return saw_no_key(m, l) ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+}
+
 // A sequence of B new tokens that ends n keys; tile t holds the tokens [t * Q, (t + 1) * Q).
 struct Seq {
     int B, n, Q;
@@ -460,7 +469,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkParams p, const __grid_const
             }
             named_barrier(1 + pair, 64);  // both have read it before the next job's first tile writes there
             l = half ? others + l : l + others;
-            const float inv = whole ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
+            const float inv = whole ? row_inverse(m, l) : 1.f;
             const size_t slot = (size_t)blockIdx.x * 2 + (first ? 1 : 0);
             // the rows of this lane's group of four, each of which the four store together
             long long rows[4];
@@ -509,7 +518,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkParams p, const __grid_const
             }
             if (active && half == 0) {
                 if (!whole) p.part_ml[slot * (2 * kTileM) + i * kTileM + r] = make_float2(m, l);
-                else if (p.lse) p.lse[orow] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+                else if (p.lse) p.lse[orow] = row_lse(m, l);
             }
             tc_fence_before();
         }
@@ -829,13 +838,14 @@ __global__ void __launch_bounds__(kMergeThreads, BATCH <= 4 ? 3 : 1) chunk_merge
             const size_t slot = (size_t)e * 2 + (e == c ? 1 : 0);
             float2 ml = make_float2(-INFINITY, 0.f);
             if (lane < n && (e == c || (flags & kHasHead))) ml = p.part_ml[slot * (2 * kTileM) + row];
-            if (!(ml.y > 0.f)) ml = make_float2(-INFINITY, 0.f);  // (no key seen: its columns count for nothing)
+            // those in which the row saw a key; a part whose sum is a NaN is one (its maximum may be -inf)
+            const unsigned seen = __ballot_sync(0xffffffffu, !saw_no_key(ml.x, ml.y));
+            if (!seen) continue;
             float top = ml.x;
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
             const float m_new = fmaxf(m, top);
-            if (m_new == -INFINITY) continue;
-            const float w_old = chunk_exp2(m - m_new), w = ml.y > 0.f ? chunk_exp2(ml.x - m_new) : 0.f;
+            const float w_old = m == m_new ? 1.f : chunk_exp2(m - m_new), w = ml.x == m_new ? 1.f : chunk_exp2(ml.x - m_new);
             float sum = ml.y * w;
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -864,18 +874,18 @@ __global__ void __launch_bounds__(kMergeThreads, BATCH <= 4 ? 3 : 1) chunk_merge
                     if (k0 + k >= n) break;
                     const float wk = __shfl_sync(0xffffffffu, w, k0 + k);
 #pragma unroll
-                    for (int d = 0; d < kCols; ++d) acc[d] += wk > 0.f ? wk * v[k][d] : 0.f;  // (a slot without a part holds anything)
+                    for (int d = 0; d < kCols; ++d) acc[d] += seen >> (k0 + k) & 1 ? wk * v[k][d] : 0.f;  // (a slot without a part holds anything)
                 }
             }
         }
-        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const float inv = row_inverse(m, l);
         const size_t orow = (size_t)(row0 + i * p.tokens + r / p.group) * p.num_q_heads + head * p.group + r % p.group;
         __nv_bfloat16* out = p.o + orow * D + lane * kCols;
         if constexpr (kCols == 4)
             *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
         else
             *reinterpret_cast<uint32_t*>(out) = pack_bf16x2(acc[0] * inv, acc[1] * inv);
-        if (p.lse && lane == 0) p.lse[orow] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        if (p.lse && lane == 0) p.lse[orow] = row_lse(m, l);
     }
 }
 

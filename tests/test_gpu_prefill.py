@@ -427,3 +427,48 @@ def test_example_runs():
     spec.loader.exec_module(example)
     off, near, finite = example.main()
     assert off < 2e-2 and near < 2e-2 and finite
+
+
+@pytest.mark.parametrize("dim", [128, 64])
+@pytest.mark.parametrize("new", [1, 70])
+@pytest.mark.parametrize("ctx", [100, 6000])
+def test_what_is_no_number_shows(ctx, new, dim):
+    """A NaN in a query or in a key that a row sees, and a score past fp32, make that row NaN in o and in the log-sum-exp,
+    whether its keys are one CTA's (100) or cut among many (6000); the rows that see none of it keep their bits."""
+    g = _gen(ctx + new)
+    n, hq = ctx + new, 4
+    (kc, vc), table, keys = _paged([n], 64, 1, dim, torch.bfloat16, g, [n])
+    q = torch.randn(new, hq, dim, device="cuda", generator=g).to(torch.bfloat16)
+    ws = bp.workspace(bp.chunk_attention_workspace_size(1, new, hq, 1, dim), "cuda")
+
+    def attend(q, k):
+        lse = torch.full((new, hq), 7.0, device="cuda")
+        o, _ = bp.chunk_attention_paged(q, k, vc, _offsets([new]), _offsets([n]), table, 64, new, n, lse=lse, ws=ws)
+        assert bp.get_status(ws) == 0
+        return o, lse
+
+    def is_lost(got, lost):
+        o, lse = got
+        assert torch.isnan(o[lost].float()).all() and torch.isnan(lse[lost]).all()
+        assert torch.equal(o[~lost], clean[0][~lost]) and torch.equal(lse[~lost], clean[1][~lost])
+
+    clean = attend(q, kc)
+    assert torch.isfinite(clean[0].float()).all() and torch.isfinite(clean[1]).all()
+    lost = torch.zeros(new, hq, dtype=torch.bool, device="cuda")
+    lost[new // 2, 2] = True
+    bad_q = q.clone()
+    bad_q[lost] = math.nan
+    is_lost(attend(bad_q, kc), lost)
+    for key in (0, ctx // 2, ctx + new // 2, n - 1):
+        bad_k = kc.clone()
+        bad_k[keys[0][key], 0, 5] = math.nan
+        lost = (torch.arange(ctx, n, device="cuda") >= key)[:, None].expand(new, hq)
+        is_lost(attend(q, bad_k), lost)
+    # 1e30 times 1e30 in one score; all others stay below 1e32
+    bad_q, bad_k = q.clone(), kc.clone()
+    bad_q[0, 1] = 0
+    bad_q[0, 1, 0] = 1e30
+    bad_k[keys[0][ctx // 2]] = 0
+    bad_k[keys[0][ctx // 2], 0, 0] = 1e30
+    o, lse = attend(bad_q, bad_k)
+    assert torch.isnan(o[0, 1].float()).all() and not torch.isfinite(lse[0, 1])
