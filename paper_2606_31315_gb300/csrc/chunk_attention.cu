@@ -22,8 +22,8 @@
 // What bounds it: of a pair of key tiles' 2 x 16 MMAs, 2,048 cycles at D = 128, about 2,950 are taken: a stream's softmax
 // (1,050), its MMAs (1,024) and the hand-overs between them follow one another, with two streams in turn.  2048 tokens
 // over 32768 keys, 32 query and 8 KV heads: 700 to 770 us, 1.38 to 1.52 PFLOP/s; a prompt of 8192: 364 to 400 us; one
-// token over 2048 keys: 16 us, a chain of latencies (9 over 100 keys, which need no merge).  The code's length counts: it runs from an instruction cache that
-// all roles share (MMA loops of twice the code took 20 % more, not unrolled ones 50 %).
+// token over 2048 keys: 16 us, a chain of latencies (9 over 100 keys, which need no merge).  How the MMA loops are
+// unrolled counts: over the ring's slots as well they took 20 % more, not at all 50 %.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -703,7 +703,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkParams p, const __grid_const
                 const int a = g->a[i], b = g->b[i], j0 = g->j0, j1 = g->j1, n = g->n;
                 had_job(nj);
                 if (j1 <= j0) continue;
-                if (elect_one()) {  // one thread throughout: its waits need no votes, its operands are known to be uniform
+                if (elect_one()) {  // one thread throughout: its waits need no votes
                     fine = mbar_wait(&sh.q_full, nq & 1, kWaitBudget);
                     unsigned xk = x, my_turn = turn, my_p = np;
                     for (int j = j0; j <= j1 && fine; ++j, ++my_turn, xk += 2) {  // xk: K of tile j

@@ -211,8 +211,8 @@ __device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64
         "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-// One lane of a whole warp: a branch on this is known to be a single thread's, whose operands then take fewer
-// instructions to reach the uniform registers (an MMA's issue: 11 to 16 instructions, under `lane == 0` 28 to 51).
+// One lane of a whole warp.  The chunk attention's MMAs issued under this instead of `lane == 0`: 2048 tokens over 32768
+// keys 767 to 740 us, a prompt of 8192 461 to 446 us.
 __device__ __forceinline__ bool elect_one() {
     uint32_t e;
     asm volatile(

@@ -13,8 +13,8 @@
 // (fewer in small calls), the next one in flight, and forms the token's cosines and sines times the norm's weights once
 // for all of a kind.
 //
-// Memory bounds it: nothing is read or written twice.  What it takes to get near is few instructions (215 a KB with
-// eight elements a lane and their pairs in another one, half of that now) and warps enough to hide a token's chain of
+// Memory bounds it: nothing is read or written twice.  What it takes to get near is few instructions (executed ones
+// by ncu's counter: 215 a KB with eight elements a lane and their pairs in another one, 90 now) and warps enough to hide a token's chain of
 // loads, position, table row, weights: more rounds in flight cost registers, and with them warps.  16381 tokens of 32 + 8
 // heads of 128, bf16: 59 us, 5.8 TB/s; 8192 tokens to their pages with 8 heads of values: 40 us, 5.2 TB/s.
 #include <cuda_bf16.h>
