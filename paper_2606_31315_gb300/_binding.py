@@ -1,9 +1,10 @@
 """ctypes binding of libblockpilot (argument marshalling only).
 
 Every function takes CUDA tensors, passes their device pointers and the current torch
-stream to the C ABI and returns the output tensors.  No step of the computation happens
-here; if the library is missing or the call fails the binding raises -- there is no
-fallback path.
+stream (or the one given as `stream`) to the C ABI and returns the output tensors.  No step of
+the computation happens here; if the library is missing or the call fails the binding raises --
+there is no fallback path.  Outputs and workspaces that are not given are allocated on the call's
+stream: elsewhere they are used as any tensor of that stream (wait for it first).
 """
 from __future__ import annotations
 
@@ -131,9 +132,21 @@ def _cuda(names, *tensors):
             raise ValueError(f"{bad} must be a contiguous CUDA tensor")
 
 
-def workspace(nbytes: int, device) -> torch.Tensor:
-    """Zero-filled device workspace (the library itself never allocates)."""
-    return torch.zeros(max(int(nbytes), 256), dtype=torch.uint8, device=device)
+def workspace(nbytes: int, device, stream=None) -> torch.Tensor:
+    """Zero-filled device workspace (the library itself never allocates), cleared on `stream` (None: the current one)."""
+    nbytes = max(int(nbytes), 256)
+    if stream is None:
+        return torch.zeros(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.zeros(nbytes, dtype=torch.uint8, device=device)
+
+
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """An output that the caller did not give, of the memory of the stream that the call runs on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 # --------------------------------------------------------------------------- attention
@@ -156,9 +169,9 @@ def block_attention(q, k, v, cu_q, cu_kv, max_q_len: int, max_kv_len: int, mask:
     total_kv, hkv, _ = k.shape
     s = cu_q.numel() - 1
     if out is None:
-        out = torch.empty_like(q)
+        out = _empty(q.shape, q.dtype, q.device, stream)
     if ws is None:
-        ws = workspace(lib.bp_block_attention_workspace_size(s, max_q_len, hq, hkv, d), q.device)
+        ws = workspace(lib.bp_block_attention_workspace_size(s, max_q_len, hq, hkv, d), q.device, stream)
     rc = lib.bp_block_attention(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), _ptr(cu_q), _ptr(cu_kv), s, total_q,
                                 total_kv, int(max_q_len), int(max_kv_len), hq, hkv, d, dtype, int(mask),
                                 float(softmax_scale), _ptr(ws), ws.numel(), _stream(stream))
@@ -182,9 +195,9 @@ def block_attention_paged(q, k_cache, v_cache, cu_q, cu_kv, block_table, page_si
     pool_rows, hkv, _ = k_cache.shape
     s = cu_q.numel() - 1
     if out is None:
-        out = torch.empty_like(q)
+        out = _empty(q.shape, q.dtype, q.device, stream)
     if ws is None:
-        ws = workspace(lib.bp_block_attention_workspace_size(s, max_q_len, hq, hkv, d), q.device)
+        ws = workspace(lib.bp_block_attention_workspace_size(s, max_q_len, hq, hkv, d), q.device, stream)
     rc = lib.bp_block_attention_paged(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(out), _ptr(lse), _ptr(cu_q),
                                       _ptr(cu_kv), _ptr(block_table), block_table.shape[1], int(page_size),
                                       pool_rows // int(page_size), s, total_q, int(total_kv), int(max_q_len),
@@ -264,7 +277,7 @@ def qk_norm_rope(q, k, cos_sin, positions, q_weight=None, k_weight=None, interle
         qos = hq * d  # of a contiguous tensor
         qs = qos if q.is_contiguous() and q.is_cuda else _heads("q", q, dt)
         if q_out is None:
-            q_out = torch.empty(shape, dtype=dt, device=q.device)
+            q_out = _empty(shape, dt, q.device, stream)
         elif q_out.shape != shape or q_out.dtype is not dt:
             raise ValueError("q_out must have q's shape and dtype")
         elif not (q_out.is_contiguous() and q_out.is_cuda):
@@ -279,7 +292,7 @@ def qk_norm_rope(q, k, cos_sin, positions, q_weight=None, k_weight=None, interle
         kos = hk * d
         ks = kos if k.is_contiguous() and k.is_cuda else _heads("k", k, dt)
         if k_out is None:
-            k_out = torch.empty(shape, dtype=dt, device=k.device)
+            k_out = _empty(shape, dt, k.device, stream)
         elif k_out.shape != shape or k_out.dtype is not dt:
             raise ValueError("k_out must have k's shape and dtype")
         elif not (k_out.is_contiguous() and k_out.is_cuda):
@@ -289,7 +302,7 @@ def qk_norm_rope(q, k, cos_sin, positions, q_weight=None, k_weight=None, interle
     if positions.dtype is not torch.int32 or positions.numel() != t or not (positions.is_cuda and positions.is_contiguous()):
         raise ValueError("positions must be a contiguous int32 CUDA tensor with one position for each token")
     if ws is None:
-        ws = workspace(256, x.device)
+        ws = workspace(256, x.device, stream)
     rc = lib.bp_qk_norm_rope(qp, qs, kp, ks, qop, qos, kop, kos, None if q_weight is None else q_weight.data_ptr(),
                              None if k_weight is None else k_weight.data_ptr(), table, positions.data_ptr(), t, hq, hk,
                              d, rotary, max_pos, interleaved, dtype, eps, ws.data_ptr(), ws.numel(), _stream(stream))
@@ -346,13 +359,13 @@ def qkv_append(qkv, k_cache, v_cache, cu_new, cu_kv, block_table, page_size: int
         qp = q_out = None
     else:
         if q_out is None:
-            q_out = torch.empty((t, hq, d), dtype=dt, device=k_cache.device)
+            q_out = _empty((t, hq, d), dt, k_cache.device, stream)
         elif q_out.shape != (t, hq, d) or q_out.dtype is not dt:
             raise ValueError("q_out must be [tokens, query heads, head_dim] of the caches' dtype")
         qos = hq * d if q_out.is_contiguous() and q_out.is_cuda else _heads("q_out", q_out, dt)
         qop = q_out.data_ptr()
     if ws is None:
-        ws = workspace(256, k_cache.device)
+        ws = workspace(256, k_cache.device, stream)
     page_size = int(page_size)
     s, per = block_table.shape
     if cu_new.numel() != s + 1 or cu_kv.numel() != s + 1:
@@ -393,7 +406,7 @@ def chunk_attention_paged(q, k_cache, v_cache, cu_q, cu_kv, block_table, page_si
     if dk != d or v_cache.shape != caches:
         raise ValueError("q and the caches must share one head_dim, the caches one shape")
     if out is None:
-        out = torch.empty((t, hq, d), dtype=dt, device=q.device)
+        out = _empty((t, hq, d), dt, q.device, stream)
     elif out.shape != shape or out.dtype is not dt:
         raise ValueError("out must have q's shape and dtype")
     if lse is not None and (lse.dtype is not torch.float32 or lse.numel() != t * hq):
@@ -402,7 +415,7 @@ def chunk_attention_paged(q, k_cache, v_cache, cu_q, cu_kv, block_table, page_si
     if cu_q.numel() != s + 1 or cu_kv.numel() != s + 1:
         raise ValueError("cu_q and cu_kv must hold one more entry than block_table has rows")
     if ws is None:
-        ws = workspace(lib.bp_chunk_attention_workspace_size(s, t, hq, hkv, d), q.device)
+        ws = workspace(lib.bp_chunk_attention_workspace_size(s, t, hq, hkv, d), q.device, stream)
     page_size = int(page_size)
     rc = lib.bp_chunk_attention_paged(q.data_ptr(), stride, k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(),
                                       None if lse is None else lse.data_ptr(), cu_q.data_ptr(), cu_kv.data_ptr(),
@@ -431,13 +444,13 @@ def spec_accept(target_logits, draft_logits, draft_tokens, cu_draft, temperature
     vocab = target_logits.shape[1]
     dev = target_logits.device
     if n_accepted is None:
-        n_accepted = torch.empty(s, dtype=torch.int32, device=dev)
+        n_accepted = _empty(s, torch.int32, dev, stream)
     if out_tokens is None:
-        out_tokens = torch.empty(total_draft + s, dtype=torch.int32, device=dev)
+        out_tokens = _empty(total_draft + s, torch.int32, dev, stream)
     if accept_prob is None and want_accept_prob:
-        accept_prob = torch.empty(total_draft, dtype=torch.float32, device=dev)
+        accept_prob = _empty(total_draft, torch.float32, dev, stream)
     if ws is None:
-        ws = workspace(lib.bp_spec_accept_workspace_size(s, total_draft, vocab), dev)
+        ws = workspace(lib.bp_spec_accept_workspace_size(s, total_draft, vocab), dev, stream)
     rc = lib.bp_spec_accept(_ptr(target_logits), _ptr(draft_logits), _ptr(draft_tokens), _ptr(cu_draft), s,
                             total_draft, vocab, float(temperature), _ptr(u_accept), _ptr(u_sample), _ptr(n_accepted),
                             _ptr(out_tokens), _ptr(accept_prob), _ptr(ws), ws.numel(), _stream(stream))
@@ -465,13 +478,13 @@ def verify_epilogue(lm_head, h_target, h_draft, draft_tokens, cu_draft, temperat
     vocab, hidden = lm_head.shape
     dev = lm_head.device
     if n_accepted is None:
-        n_accepted = torch.empty(s, dtype=torch.int32, device=dev)
+        n_accepted = _empty(s, torch.int32, dev, stream)
     if out_tokens is None:
-        out_tokens = torch.empty(total_draft + s, dtype=torch.int32, device=dev)
+        out_tokens = _empty(total_draft + s, torch.int32, dev, stream)
     if accept_prob is None and want_accept_prob:
-        accept_prob = torch.empty(total_draft, dtype=torch.float32, device=dev)
+        accept_prob = _empty(total_draft, torch.float32, dev, stream)
     if ws is None:
-        ws = workspace(lib.bp_verify_epilogue_workspace_size(s, total_draft, vocab), dev)
+        ws = workspace(lib.bp_verify_epilogue_workspace_size(s, total_draft, vocab), dev, stream)
     rc = lib.bp_verify_epilogue(_ptr(lm_head), _ptr(h_target), _ptr(h_draft), hidden, vocab, _ptr(draft_tokens),
                                 _ptr(cu_draft), s, total_draft, float(temperature), _ptr(u_accept), _ptr(u_sample),
                                 _ptr(n_accepted), _ptr(out_tokens), _ptr(accept_prob), _ptr(logits_out), _ptr(ws),
@@ -491,9 +504,9 @@ def verify_commit(ctx_lens, n_accepted, out_tokens, cu_draft, capacity: int, anc
     s = ctx_lens.numel()
     dev = ctx_lens.device
     if cu_kv_next is None:
-        cu_kv_next = torch.empty(s + 1, dtype=torch.int32, device=dev)
+        cu_kv_next = _empty(s + 1, torch.int32, dev, stream)
     if ws is None:
-        ws = workspace(256, dev)
+        ws = workspace(256, dev, stream)
     rc = lib.bp_verify_commit(_ptr(ctx_lens), _ptr(n_accepted), _ptr(out_tokens), _ptr(cu_draft), s, int(capacity),
                               _ptr(anchor), _ptr(cu_kv_next), _ptr(ws), ws.numel(), _stream(stream))
     _check(rc, "bp_verify_commit")
@@ -518,15 +531,15 @@ def tau_select(gamma, candidates, train_block: int, alpha: float, predicted=None
     nc = cand.size
     dev = gamma.device
     if tau is None and want_tau:
-        tau = torch.empty(n, nc, dtype=torch.float32, device=dev)
+        tau = _empty((n, nc), torch.float32, dev, stream)
     if best is None:
-        best = torch.empty(n, dtype=torch.int32, device=dev)
+        best = _empty(n, torch.int32, dev, stream)
     if regret is None and predicted is not None:
-        regret = torch.empty(n, dtype=torch.float32, device=dev)
+        regret = _empty(n, torch.float32, dev, stream)
     if summary is None:
-        summary = torch.empty(4, dtype=torch.float64, device=dev)
+        summary = _empty(4, torch.float64, dev, stream)
     if ws is None:
-        ws = workspace(lib.bp_tau_select_workspace_size(n), dev)
+        ws = workspace(lib.bp_tau_select_workspace_size(n), dev, stream)
     rc = lib.bp_tau_select(_ptr(g), n, jmax, cand.ctypes.data, nc, int(train_block), float(alpha), _ptr(predicted),
                            _ptr(tau), _ptr(best), _ptr(regret), _ptr(summary), _ptr(ws), ws.numel(), _stream(stream))
     _check(rc, "bp_tau_select")
@@ -551,11 +564,11 @@ def policy_select(feats, w1, b1, w2, b2, candidates, row_index=None, num_reqs=No
     n = num_reqs if num_reqs is not None else (row_index.numel() if row_index is not None else feats.shape[0])
     dev = feats.device
     if block_size is None:
-        block_size = torch.empty(n, dtype=torch.int32, device=dev)
+        block_size = _empty(n, torch.int32, dev, stream)
     if logits is None and want_logits:
-        logits = torch.empty((n, c), dtype=torch.float32, device=dev)
+        logits = _empty((n, c), torch.float32, dev, stream)
     if ws is None:
-        ws = workspace(lib.bp_policy_select_workspace_size(n, d_in, hidden, c), dev)
+        ws = workspace(lib.bp_policy_select_workspace_size(n, d_in, hidden, c), dev, stream)
     rc = lib.bp_policy_select(_ptr(feats), feats.stride(0), _ptr(row_index), n, d_in, _ptr(w1), _ptr(b1), hidden,
                               _ptr(w2), _ptr(b2), c, _ptr(candidates), wdtype, _ptr(logits), _ptr(block_size),
                               _ptr(ws), ws.numel(), _stream(stream))

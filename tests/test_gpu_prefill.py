@@ -472,3 +472,25 @@ def test_what_is_no_number_shows(ctx, new, dim):
     bad_k[keys[0][ctx // 2], 0, 0] = 1e30
     o, lse = attend(bad_q, bad_k)
     assert torch.isnan(o[0, 1].float()).all() and not torch.isfinite(lse[0, 1])
+
+
+def test_calls_on_a_stream_of_their_own():
+    """stream= with nothing else given, while the current stream is busy and its free memory is written to right after each
+    call: the same bits as with outputs and workspaces of the caller's."""
+    g = _gen(31)
+    n, hq, hkv, dim = 3000, 8, 2, 128
+    (kc, vc), table, _ = _paged([n], 64, hkv, dim, torch.bfloat16, g, [n])
+    q = torch.randn(40, hq, dim, device="cuda", generator=g).to(torch.bfloat16)
+    tab, pos, cu, cu_kv = _table(n, dim), torch.arange(40, device="cuda", dtype=torch.int32), _offsets([40]), _offsets([n])
+    want_o, _ = bp.chunk_attention_paged(q, kc, vc, cu, cu_kv, table, 64, 40, n)
+    want_q, want_k = bp.qk_norm_rope(q, q[:, :2], tab, pos)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)  # about 10 ms on the current stream
+    got_o, _ = bp.chunk_attention_paged(q, kc, vc, cu, cu_kv, table, 64, 40, n, stream=side)
+    got_q, got_k = bp.qk_norm_rope(q, q[:, :2], tab, pos, stream=side)
+    taken = [torch.full((bp.chunk_attention_workspace_size(1, 40, hq, hkv, dim),), 255, device="cuda", dtype=torch.uint8) for _ in range(3)]
+    side.synchronize()
+    got = [x.clone() for x in (got_o, got_q, got_k)]
+    torch.cuda.synchronize()
+    assert len(taken) == 3 and all(torch.equal(a, b) for a, b in zip(got, (want_o, want_q, want_k)))
