@@ -214,8 +214,8 @@ BP_API int bp_qkv_append(const void* q, int64_t q_stride, const void* k_new, int
  *            rows only those of the sequence's keys have to be finite: what is behind them is not used
  *   max_q_len, max_kv_len  host-side upper bounds of B_s and n_s; pages_per_seq * page_size >= max_kv_len
  * Limits: dtype BP_BF16, head_dim 64 or 128, g <= 128, num_pages * page_size < 2^31.  A page id outside [0, num_pages),
- * a sequence past its table row or one past max_q_len or max_kv_len sets BP_ERR_DEVICE_FLAG.  The result does not depend
- * on scheduling.
+ * a sequence past its table row or one past max_q_len or max_kv_len sets BP_ERR_DEVICE_FLAG, and so does one with query
+ * rows outside [0, total_q), which is not computed.  The result does not depend on scheduling.
  * ------------------------------------------------------------------------------- */
 BP_API size_t bp_chunk_attention_workspace_size(int num_seqs, int total_q, int num_q_heads, int num_kv_heads,
                                                 int head_dim);

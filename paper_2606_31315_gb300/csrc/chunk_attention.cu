@@ -70,7 +70,7 @@ struct ChunkParams {
     const int32_t* cu_q;
     const int32_t* cu_kv;
     const int32_t* block_table;
-    int num_seqs, num_q_heads, num_kv_heads, group;
+    int num_seqs, total_q, num_q_heads, num_kv_heads, group;
     int tokens;  // of one stream's tile: floor(128 / group)
     int pages_per_seq, page_shift, num_pages;
     int max_q, max_kv;  // of a sequence: the merge's launch rests on them
@@ -154,7 +154,10 @@ struct Job {
 
 __device__ __forceinline__ Seq load_seq(const ChunkParams& p, int s) {
     const int q0 = __ldg(p.cu_q + s), q1 = __ldg(p.cu_q + s + 1), k0 = __ldg(p.cu_kv + s), k1 = __ldg(p.cu_kv + s + 1);
-    return Seq{q1 - q0, k1 - k0, 2 * p.tokens, p.causal, p.window};
+    // (a sequence whose rows are not all among the call's is left out: they would be written behind the outputs' ends)
+    const bool there = q0 >= 0 && q1 <= p.total_q;
+    if (!there) raise_error(p.err, kErrDeviceArg);
+    return Seq{there ? q1 - q0 : 0, k1 - k0, 2 * p.tokens, p.causal, p.window};
 }
 // Key tiles [first, first + count) under tile t.
 __device__ __forceinline__ void tile_span(const Seq& q, int t, int& first, int& count) {
@@ -899,6 +902,7 @@ int run(const ChunkAttentionArgs& a, const DeviceInfo& dev, cudaStream_t stream)
     p.cu_kv = a.cu_kv;
     p.block_table = a.block_table;
     p.num_seqs = a.num_seqs;
+    p.total_q = a.total_q;
     p.num_q_heads = a.num_q_heads;
     p.num_kv_heads = a.num_kv_heads;
     p.group = a.num_q_heads / a.num_kv_heads;

@@ -494,3 +494,27 @@ def test_calls_on_a_stream_of_their_own():
     got = [x.clone() for x in (got_o, got_q, got_k)]
     torch.cuda.synchronize()
     assert len(taken) == 3 and all(torch.equal(a, b) for a, b in zip(got, (want_o, want_q, want_k)))
+
+
+@pytest.mark.parametrize("first", [0, 3])
+def test_rows_past_the_call_are_not_written(first):
+    """Offsets that name more rows than the call has (a batch that grew past the room of a replayed call): reported, that
+    sequence left out, nothing written behind the outputs, the others computed."""
+    g = _gen(13)
+    lens, new, total, hq, dim = [700, 3000], [4, 8], 8, 2, 64
+    (kc, vc), table, keys = _paged(lens, 64, 1, dim, torch.bfloat16, g, lens)
+    q = torch.randn(total, hq, dim, device="cuda", generator=g).to(torch.bfloat16)
+    out, lse = torch.full((40, hq, dim), 7.0, device="cuda", dtype=torch.bfloat16), torch.full((40, hq), 7.0, device="cuda")
+    ws = bp.workspace(bp.chunk_attention_workspace_size(2, total, hq, 1, dim), "cuda")
+    cu = _offsets(new) + first
+    bp.chunk_attention_paged(q, kc, vc, cu, _offsets(lens), table, 64, 8, 3000, out=out[:total], lse=lse[:total], ws=ws)
+    assert bp.get_status(ws) == bp._binding.BP_ERR_DEVICE_FLAG
+    rows = slice(first, first + new[0])
+    ref, size, _ = _attend(q[rows], kc, vc, keys[0], True, 0, dim ** -0.5)
+    assert torch.all((out[rows].double() - ref).abs() <= (U + 1e-3) * size + U * ref.abs() + 1e-30)
+    for x in (out, lse):
+        assert torch.all(x[:first] == 7.0) and torch.all(x[first + new[0]:] == 7.0)
+    bp.chunk_attention_paged(q, kc, vc, cu + 100, _offsets(lens), table, 64, 8, 3000, out=out[:total], lse=lse[:total], ws=ws)
+    assert bp.get_status(ws) == bp._binding.BP_ERR_DEVICE_FLAG and torch.all(out[total:] == 7.0)
+    bp.chunk_attention_paged(q, kc, vc, cu - first - 1, _offsets(lens), table, 64, 8, 3000, out=out[:total], lse=lse[:total], ws=ws)
+    assert bp.get_status(ws) == bp._binding.BP_ERR_DEVICE_FLAG and torch.all(out[total:] == 7.0)
