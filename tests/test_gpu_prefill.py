@@ -518,3 +518,37 @@ def test_rows_past_the_call_are_not_written(first):
     assert bp.get_status(ws) == bp._binding.BP_ERR_DEVICE_FLAG and torch.all(out[total:] == 7.0)
     bp.chunk_attention_paged(q, kc, vc, cu - first - 1, _offsets(lens), table, 64, 8, 3000, out=out[:total], lse=lse[:total], ws=ws)
     assert bp.get_status(ws) == bp._binding.BP_ERR_DEVICE_FLAG and torch.all(out[total:] == 7.0)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dim", [128, 64])
+@pytest.mark.parametrize("hq,hkv", [(32, 8), (5, 1), (0, 3)])
+@pytest.mark.parametrize("ctx,new,at", [((0,), (1,), False), ((5, 100, 0, 33, 63), (3, 1, 70, 0, 1), True), ((1000, 7), (600, 400), False)])
+def test_append_of_whole_heads_in_halves(dtype, dim, hq, hkv, ctx, new, at):
+    """The usual form (the whole head turned in halves, both norms weighted), packed and in tensors of their own: queries,
+    keys and values against 64 bits, at the keys' numbers and at given positions; nothing else of the pool touched."""
+    g = _gen(dim + hq)
+    total, page = sum(new), 16
+    qkv = (2 * torch.randn(total, hq + 2 * hkv, dim, device="cuda", generator=g)).to(dtype)
+    q, k, v = qkv.split([hq, hkv, hkv], 1)
+    qw, kw = [(1 + 0.3 * torch.randn(dim, device="cuda", generator=g)).to(dtype) for _ in range(2)]
+    lens = [c + n for c, n in zip(ctx, new)]
+    tab = _table(2000, dim)
+    pos = torch.cat([torch.arange(c, c + n, device="cuda") for c, n in zip(ctx, new)])
+    if at:
+        pos = torch.randint(0, 2000, (total,), device="cuda", generator=g)
+    bits = torch.int16 if dtype == torch.bfloat16 else torch.int32
+    for given in (qkv, (q if hq else None, k.contiguous(), v)):
+        (kc, vc), table, keys = _paged(lens, page, hkv, dim, dtype, g, ctx)
+        rows = torch.cat([r[c:] for r, c in zip(keys, ctx)])
+        want_k, want_v = kc.clone(), vc.clone()
+        want_v[rows] = v
+        ws = bp.workspace(256, "cuda")
+        qo = bp.qkv_append(given, kc, vc, _offsets(new), _offsets(lens), table, page, tab,
+                           positions=pos.to(torch.int32) if at else None, q_weight=qw, k_weight=kw, eps=1e-5, ws=ws)
+        assert bp.get_status(ws) == 0
+        if hq:
+            _near_turned(qo, _turned(q, qw, tab, pos, False, 1e-5))
+        _near_turned(kc[rows], _turned(k, kw, tab, pos, False, 1e-5))
+        want_k[rows] = kc[rows]
+        assert torch.equal(kc.view(bits), want_k.view(bits)) and torch.equal(vc.view(bits), want_v.view(bits))
