@@ -552,3 +552,11 @@ def test_append_of_whole_heads_in_halves(dtype, dim, hq, hkv, ctx, new, at):
         _near_turned(kc[rows], _turned(k, kw, tab, pos, False, 1e-5))
         want_k[rows] = kc[rows]
         assert torch.equal(kc.view(bits), want_k.view(bits)) and torch.equal(vc.view(bits), want_v.view(bits))
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (8, 8), (6, 2), (10, 2), (7, 1), (32, 8), (16, 1), (128, 1), (100, 1)])
+@pytest.mark.parametrize("dim,page", [(128, 64), (64, 16)])
+@pytest.mark.parametrize("new", [(70, 1, 140), (1, 1, 1)])
+def test_chunk_heads_of_cut_contexts(hq, hkv, dim, page, new):
+    """Contexts that are cut among CTAs: both forms of the merge, with any number of heads and tokens a tile."""
+    _check_chunk((6000, 17, 2500), new, hq=hq, hkv=hkv, dim=dim, page=page, seed=hq)
