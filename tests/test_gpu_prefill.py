@@ -560,3 +560,63 @@ def test_append_of_whole_heads_in_halves(dtype, dim, hq, hkv, ctx, new, at):
 def test_chunk_heads_of_cut_contexts(hq, hkv, dim, page, new):
     """Contexts that are cut among CTAs: both forms of the merge, with any number of heads and tokens a tile."""
     _check_chunk((6000, 17, 2500), new, hq=hq, hkv=hkv, dim=dim, page=page, seed=hq)
+
+
+def test_a_graph_replays_with_other_lengths():
+    """Norm and rotation, append and attention captured once, with room for 300 tokens of 3 sequences, and replayed over
+    other lengths, pages and values: every call reads them from the device."""
+    g = _gen(21)
+    room, hq, hkv, dim, page, most = 300, 8, 2, 128, 64, 5000
+    per = most // page + 1
+    qkv = torch.zeros(room, hq + 2 * hkv, dim, device="cuda", dtype=torch.bfloat16)
+    kc, vc = [torch.zeros(3 * per * page, hkv, dim, device="cuda", dtype=torch.bfloat16) for _ in range(2)]
+    w = [(1 + 0.1 * torch.randn(dim, device="cuda", generator=g)).to(torch.bfloat16) for _ in range(2)]
+    tab = _table(most, dim)
+    cu_new, cu_kv = [torch.zeros(4, dtype=torch.int32, device="cuda") for _ in range(2)]
+    table = torch.zeros(3, per, dtype=torch.int32, device="cuda")
+    pos = torch.zeros(room, dtype=torch.int32, device="cuda")
+    q = torch.empty(room, hq, dim, device="cuda", dtype=torch.bfloat16)
+    q2, o = torch.empty_like(q), torch.empty_like(q)
+    lse = torch.empty(room, hq, device="cuda")
+    small, ws = bp.workspace(256, "cuda"), bp.workspace(bp.chunk_attention_workspace_size(3, room, hq, hkv, dim), "cuda")
+
+    def step():
+        bp.qkv_append(qkv, kc, vc, cu_new, cu_kv, table, page, tab, q_weight=w[0], k_weight=w[1], q_out=q, ws=small)
+        bp.qk_norm_rope(qkv[:, :hq], None, tab, pos, q_weight=w[0], q_out=q2, ws=small)
+        bp.chunk_attention_paged(q, kc, vc, cu_new, cu_kv, table, page, room, most, out=o, lse=lse, ws=ws)
+
+    step()  # nothing to do: no sequence has a token
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for ctx, new in (((4000, 0, 70), (1, 200, 1)), ((10, 4900, 0), (100, 100, 100)), ((0, 0, 3000), (0, 0, 1)), ((4000, 0, 70), (1, 200, 1))):
+        lens, total = [c + n for c, n in zip(ctx, new)], sum(new)
+        order = torch.randperm(3 * per, device="cuda", generator=g).to(torch.int32).view(3, per)
+        qkv.copy_(torch.randn(qkv.shape, device="cuda", generator=g))
+        for c in (kc, vc):
+            c.copy_(torch.randn(c.shape, device="cuda", generator=g))
+        table.copy_(order)
+        cu_new.copy_(_offsets(new))
+        cu_kv.copy_(_offsets(lens))
+        here = torch.cat([torch.arange(c, c + n, device="cuda") for c, n in zip(ctx, new)])
+        pos[:total] = here
+        for t in (q, o, lse):
+            t.fill_(7.0)
+        graph.replay()
+        assert bp.get_status(small) == 0 and bp.get_status(ws) == 0
+        _near_turned(q[:total], _turned(qkv[:total, :hq], w[0], tab, here, False, 1e-6))
+        assert torch.equal(q2[:total], q[:total])
+        assert torch.all(q[total:] == 7.0) and torch.all(o[total:] == 7.0) and torch.all(lse[total:] == 7.0)
+        at = 0
+        for s, (c, n) in enumerate(zip(ctx, new)):
+            if n:
+                j = torch.arange(c + n, device="cuda")
+                rows = order[s].long()[j // page] * page + j % page
+                _near_turned(kc[rows[c:]], _turned(qkv[at:at + n, hq:hq + hkv], w[1], tab, j[c:], False, 1e-6))
+                assert torch.equal(vc[rows[c:]], qkv[at:at + n, hq + hkv:])
+                ref, size, z = _attend(q[at:at + n], kc, vc, rows, True, 0, dim ** -0.5)
+                err = (o[at:at + n].double() - ref).abs()
+                assert torch.all(err <= (U + 1e-3) * size + U * ref.abs() + 1e-30)
+                assert float((lse[at:at + n].double() - z).abs().max()) <= 5e-4
+            at += n
