@@ -4,7 +4,10 @@ Every function takes CUDA tensors, passes their device pointers and the current 
 stream (or the one given as `stream`) to the C ABI and returns the output tensors.  No step of
 the computation happens here; if the library is missing or the call fails the binding raises --
 there is no fallback path.  Outputs and workspaces that are not given are allocated on the call's
-stream: elsewhere they are used as any tensor of that stream (wait for it first).
+stream: elsewhere they are used as any tensor of that stream (wait for it first).  A workspace that
+is not given is gone when the call returns, and the status that the GPU left in it with it: give one
+and read it with get_status wherever the data on the device may be wrong (a position outside its
+table, a page outside the pool), since the rows it concerns are then not written.
 """
 from __future__ import annotations
 
@@ -263,7 +266,9 @@ def qk_norm_rope(q, k, cos_sin, positions, q_weight=None, k_weight=None, interle
     """Every head of q and k normed (with a weight) and rotated to its token's position; see ``bp_qk_norm_rope``.
 
     q [T, Hq, D], k [T, Hkv, D] (bf16 or fp32, any stride between tokens; either may be None), cos_sin fp32
-    [max_pos, rotary_dim] or None, positions int32 [T].  q_out / k_out may be q / k.  Returns (q_out, k_out)."""
+    [max_pos, rotary_dim] or None, positions int32 [T].  q_out / k_out may be q / k.  A position outside the table is
+    reported in `ws` alone, and its rows are not written: without a ws of its own a call cannot tell.  Returns (q_out,
+    k_out)."""
     lib = load()
     x = q if q is not None else k
     dt = x.dtype
@@ -319,7 +324,8 @@ def qkv_append(qkv, k_cache, v_cache, cu_new, cu_kv, block_table, page_size: int
     qkv: a packed projection [T, Hq + 2 Hkv, D] (a token's query heads, then its key and its value heads; any stride
     between tokens), or a tuple (q or None, k, v) of such tensors of their own.  k_cache / v_cache
     [num_pages * page_size, Hkv, D]; cu_new / cu_kv int32 [S+1], block_table int32 [S, pages_per_seq] on the device.
-    Returns the queries [T, Hq, D] (None without query heads)."""
+    A token without a place in the pages, or a position outside the table, is reported in `ws` alone, and its rows are not
+    written: without a ws of its own a call cannot tell.  Returns the queries [T, Hq, D] (None without query heads)."""
     lib = load()
     rows, hkv, d = shape = k_cache.shape
     dt = k_cache.dtype
@@ -392,7 +398,8 @@ def chunk_attention_paged(q, k_cache, v_cache, cu_q, cu_kv, block_table, page_si
 
     q [total_q, Hq, D] bf16 (any stride between tokens), D 64 or 128; k_cache / v_cache [num_pages * page_size, Hkv,
     D]; cu_q / cu_kv int32 [S+1], block_table int32 [S, pages_per_seq] on the device.  window > 0: a token sees the
-    `window` keys that end with its own.  Returns (o, lse_or_None)."""
+    `window` keys that end with its own.  Give a ws (chunk_attention_workspace_size) wherever calls are repeated: without
+    one, 52 MB (D = 128) are allocated and cleared for every call, and its status is lost.  Returns (o, lse_or_None)."""
     lib = load()
     dt = q.dtype
     t, hq, d = shape = q.shape

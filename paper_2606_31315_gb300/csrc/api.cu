@@ -270,7 +270,7 @@ int bp_chunk_attention_paged(const void* q, int64_t q_stride, const void* k_cach
 }
 
 namespace {
-// What bp_qk_norm_rope and bp_qkv_append check alike; rows: the strides between tokens of what they read and write.
+// What bp_qk_norm_rope and bp_qkv_append check alike.
 int check_rope(int head_dim, int rotary_dim, int max_pos, const float* cos_sin, int interleaved, int dtype, float eps,
                const void* q_weight, const void* k_weight) {
     if (head_dim < 1 || rotary_dim < 0 || rotary_dim > head_dim || (rotary_dim > 0 && (!cos_sin || max_pos < 1)))

@@ -21,8 +21,9 @@
 //
 // What bounds it: of a pair of key tiles' 2 x 16 MMAs, 2,048 cycles at D = 128, about 2,950 are taken: a stream's softmax
 // (1,050), its MMAs (1,024) and the hand-overs between them follow one another, with two streams in turn.  2048 tokens
-// over 32768 keys, 32 query and 8 KV heads: 700 to 770 us, 1.38 to 1.52 PFLOP/s; a prompt of 8192: 364 to 400 us; one
-// token over 2048 keys: 16 us, a chain of latencies (9 over 100 keys, which need no merge).  How the MMA loops are
+// over 32768 keys, 32 query and 8 KV heads: 706 to 726 us in short runs, 744 to 775 in long ones, as the clock drops (1.37 to
+// 1.51 PFLOP/s); a prompt of 8192: 363 to 371 and 389 to 400 us; one token over 2048 keys: 16.5 us, a chain of latencies
+// (9 over 100 keys, which need no merge).  How the MMA loops are
 // unrolled counts: over the ring's slots as well they took 20 % more, not at all 50 %.
 #include <cuda_bf16.h>
 
@@ -42,11 +43,11 @@ constexpr int kSoftmaxWarps = 16;                // two threads a row, 64 keys e
 constexpr int kProducerWarp = 16, kMmaWarp = 17, kTailWarp = 19;  // (a stream's MMA warp: kMmaWarp + stream)
 constexpr int kChunkThreads = 32 * 20;
 // Registers: 96 a thread at launch; the softmax warps take 104, the other warpgroup keeps 64 (512 x 104 + 128 x 64 =
-// 640 x 96).
+// 640 x 96).  The compiler spills 108 bytes a thread at D = 128, 92 at 64, of all roles together.
 constexpr int kSoftmaxRegs = 104, kOtherRegs = 64;
 constexpr uint32_t kChunkTmem = 512;
 // A work tile's fixed cost (queries in, output out), in keys: a prompt of 8192 takes 399 us with 192, 372 with 320, 368
-// with 448, 374 with 640.
+// with 448, 374 with 640.  Heads of 64 and tiles of one stream take the same number; it was not fitted to them.
 constexpr int kTileCost = 400;
 constexpr int kLeastCost = 2 * kKeys;            // of a CTA's stretch: below it, fewer CTAs take part
 constexpr int kLeastCut = 2;                     // key tiles on either side of a cut
@@ -121,8 +122,7 @@ struct Seq {
         const long long c = x - t0;
         return c * a + Q * ((c * (t0 + x - 1)) >> 1);
     }
-    // keys (and fixed costs) of the tiles before x, 0 <= x <= tiles(); exact but for a window wider than n at both
-    // ends of a tile, where neighbours agree on the same number all the same
+    // keys (and fixed costs) of the tiles before x, 0 <= x <= tiles(): cost(t + 1) - cost(t) is kTileCost + keys(t)
     __device__ __forceinline__ long long cost(int x) const {
         long long w = (long long)x * kTileCost;
         const int T = tiles();
@@ -409,7 +409,9 @@ chunk_attention_kernel(const __grid_constant__ ChunkParams p, const __grid_const
                         u = chunk_exp2(u);
                         w = chunk_exp2(w);
                         sum2[e & 1] = add_f32x2(sum2[e & 1], pack_f32x2(u, w));
-                        pk[e] = pack_bf16x2(u, w);  // bf16: the type of V, which P multiplies
+                        // bf16: the type of V, which P multiplies; against 64 bits o is off by 0.0021 to 0.0023 of its
+                        // size, with weights in fp32 by 0.0016 to 0.0017 (o's own rounding)
+                        pk[e] = pack_bf16x2(u, w);
                     }
                     float u, w;
                     unpack_f32x2(add_f32x2(sum2[0], sum2[1]), u, w);
@@ -813,7 +815,7 @@ chunk_attention_kernel(const __grid_constant__ ChunkParams p, const __grid_const
 // did not end.  Its parts are c's last and the first ones of the CTAs behind it, up to the one that ends it.  A warp has a row:
 // its lanes take the parts' (m, l), 32 at a time, and weigh them; then 4 columns each, all parts' loads in flight.
 // BATCH parts' loads are in flight at once: 4 where tiles have many rows (they are cut once or twice, and the registers are
-// better spent on more blocks: 12 took 14 us more for a prompt of 8192), 16 where every sequence has one tile (its context
+// better spent on more blocks, 12 bytes spilled among them: 12 loads took 14 us more for a prompt of 8192), 16 where every sequence has one tile (its context
 // may be cut for all CTAs: one token over 2048 keys took 18.7 us with 8 of them).
 constexpr int kMergeThreads = 512, kMergeRows = 32;
 template <int D, int BATCH>

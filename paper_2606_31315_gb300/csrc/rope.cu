@@ -14,9 +14,11 @@
 // for all of a kind.
 //
 // Memory bounds it: nothing is read or written twice.  What it takes to get near is few instructions (executed ones
-// by ncu's counter: 215 a KB with eight elements a lane and their pairs in another one, 90 now) and warps enough to hide a token's chain of
-// loads, position, table row, weights: more rounds in flight cost registers, and with them warps.  16381 tokens of 32 + 8
-// heads of 128, bf16: 59 us, 5.8 TB/s; 8192 tokens to their pages with 8 heads of values: 40 us, 5.2 TB/s.
+// by ncu's counter: 215 a KB with eight elements a lane and their pairs in another one, 90 now) and warps enough to
+// hide a token's chain of loads, position, table row, weights: more rounds in flight cost registers, and with them warps
+// (80 registers and 16 bytes spilled for 24 warps an SM in bf16's usual form without a cache, 94 and none with one).
+// 16381 tokens of 32 + 8 heads of 128, bf16: 59 to 61 us, 5.7 TB/s; 8192 tokens to their pages with 8 heads of values: 39
+// to 41 us, 5.1 TB/s.  The forms of part of a head, of neighbours and of fp32 were not timed at such sizes.
 #include <cuda_bf16.h>
 
 #include <limits.h>
@@ -124,7 +126,7 @@ __device__ __forceinline__ float head_norm(const Pairs<V>& y, bool in, float dim
 }
 
 // What a lane knows of its piece: y = x wc + (the paired elements) ws, wc and ws the cosines and signed sines of a position
-// times the weights of a norm.
+// times the weights of a norm (one more rounding in fp32: 6.1e-8 off 64 bits instead of 5.7e-8).
 template <typename T, int V, int LANES, bool PLAIN>
 struct Lane;
 
