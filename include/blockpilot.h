@@ -21,6 +21,8 @@
  * bp_verify_commit rolls the KV lengths back to the accepted prefix on the device, closing the loop.
  * bp_qk_norm_rope and bp_qkv_append take a layer's projections to normed, rotated queries and keys, the latter into the
  * paged cache; bp_chunk_attention_paged attends for a prompt, or a chunk of one, over it: the prefill before the loop.
+ * bp_kv_append_fp8 and bp_chunk_attention_paged_fp8 fill and read such a cache in 8 bits; bp_pages_update gives a step's pages
+ * out and takes them back, on the device.
  *
  * Conventions shared by every entry point
  *   - Pointers to tensors are DEVICE pointers (cudaMalloc / torch allocations), owned by
@@ -225,6 +227,71 @@ BP_API int bp_chunk_attention_paged(const void* q, int64_t q_stride, const void*
                                     int max_q_len, int max_kv_len, int num_q_heads, int num_kv_heads, int head_dim,
                                     int dtype, int mask, int window, float softmax_scale, void* workspace,
                                     size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------
+ * A paged KV cache in 8 bits: half the bytes of the bf16 one, which bound the verify pass.  Keys and values are e4m3 codes (4
+ * bits of exponent, 3 of mantissa, 448 the largest, 0x7f and 0xff not a number), with a power of two for each page and head:
+ *
+ *   key j of sequence s, head h  =  2^(k_scale[page][h] - 127) * (code of row j % page_size of that page and head)
+ *   page = block_table[s*pages_per_seq + j/page_size]; values likewise
+ *
+ *   k_cache, v_cache  [num_pages*page_size][num_kv_heads][head_dim] bytes, 16-byte aligned
+ *   k_scale, v_scale  [num_pages][num_kv_heads] bytes: biased exponents, 0 to 254
+ *
+ * bp_kv_append_fp8 appends new rows as bp_kv_append does (cu_new, cu_kv, block_table).  The scale of a page that the call
+ * begins is the least in [1, 254] with every finite new element within 448 of it (1 where all are 0); the scale of a page that
+ * held rows before never falls, and where it grows the rows before are rounded to it.  Codes are the nearest ones, ties to
+ * even; what is not finite becomes 0x7f.  Rows behind a sequence's last key keep what they hold, and so does the rest of
+ * a page begun: they are not keys.  (After a rollback into a page its scale stays as the dropped rows left it.)
+ *   k_new, v_new  rows of [num_kv_heads][head_dim] dtype (bf16 or fp32), *_stride elements from a token to the next
+ * Limits: head_dim a multiple of 16; 16-byte aligned pointers and strides; num_kv_heads <= 65535.  A page that is to receive
+ * rows and has no place in the table or the pool sets BP_ERR_DEVICE_FLAG and is not written; so do rows before key 0.
+ * Rows from cu_new[num_seqs] on are padding.  A page may belong to one sequence of the call.  workspace: at least 256 bytes.
+ *
+ * bp_chunk_attention_paged_fp8 is bp_chunk_attention_paged over such a cache: the same arguments, limits, masks, workspace
+ * size and errors.  Nothing is rounded that a bf16 cache of the same values would not round.  A key or a value that is not
+ * a number makes the rows that see it NaN (whole, with their lse), and no others.  A scale of 255 sets BP_ERR_DEVICE_FLAG.
+ * ------------------------------------------------------------------------------- */
+BP_API int bp_kv_append_fp8(void* k_cache, void* k_scale, void* v_cache, void* v_scale, const void* k_new, int64_t k_stride,
+                            const void* v_new, int64_t v_stride, const int32_t* cu_new, const int32_t* cu_kv,
+                            const int32_t* block_table, int pages_per_seq, int page_size, int num_pages, int num_seqs,
+                            int total_new, int num_kv_heads, int head_dim, int dtype, void* workspace,
+                            size_t workspace_bytes, void* stream);
+BP_API int bp_chunk_attention_paged_fp8(const void* q, int64_t q_stride, const void* k_cache, const void* k_scale,
+                                        const void* v_cache, const void* v_scale, void* o, float* lse, const int32_t* cu_q,
+                                        const int32_t* cu_kv, const int32_t* block_table, int pages_per_seq, int page_size,
+                                        int num_pages, int num_seqs, int total_q, int max_q_len, int max_kv_len,
+                                        int num_q_heads, int num_kv_heads, int head_dim, int dtype, int mask, int window,
+                                        float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------
+ * A step's pages, from the sequences' lengths, on the device: sequence s holds old_lens[s] keys, in the first
+ * ceil(old_lens[s] / page_size) pages of its row of the block table, and is to hold new_lens[s].  Growing sequences take
+ * pages and shrinking ones (a rollback, an end) give theirs back:
+ *
+ *   taken first are the pages given back, in order of sequence and place in its row, then free_pages from its end;
+ *   what is left of those given back is put at free_pages' end, the first one last: giving back what was just taken
+ *   restores the list
+ *   new token t (the tokens of sequence s are [cu_new[s], cu_new[s+1]), max(0, new_lens[s] - old_lens[s]) of them):
+ *   positions[t] its key's number, slots[t] = page * page_size + positions[t] % page_size; -1 from cu_new[num_seqs] on
+ *
+ *   block_table  [num_seqs][pages_per_seq] int32, in/out: entries of pages taken are written, the others stay as they are
+ *   free_pages   [num_pages] int32, in/out: the ids of free pages come first; num_free [1] int32, in/out: how many
+ *   total_new    entries of positions [int32] and slots [int64], each of which may be NULL
+ *   cu_new, cu_kv  [num_seqs+1] int32 out, may be NULL: prefix sums of the new tokens and of new_lens, as bp_kv_append,
+ *            bp_qk_norm_rope (positions) and the attentions read them
+ *   missing      [1] int32 out, may be NULL: 0, or how many pages there are too few.  Then nothing is changed: cu_new
+ *            is 0, cu_kv the prefix sums of old_lens, positions and slots -1, and what runs on them appends nothing.
+ * A length below 0 or past a row of the table, keys past 2^31 - 1, more new tokens than total_new (where positions or slots
+ * are given), num_free outside [0, num_pages] or more pages free than there are set BP_ERR_DEVICE_FLAG and change nothing
+ * either; so does, but for the change, a page id outside [0, num_pages) that is moved.
+ * page_size as bp_block_attention_paged; num_seqs <= 16384 (else BP_ERR_UNSUPPORTED).  workspace: at least 256 bytes; it
+ * keeps a counter there, which every call puts back at zero.  The arrays may not overlap, but old_lens and new_lens may.
+ * ------------------------------------------------------------------------------- */
+BP_API int bp_pages_update(int32_t* block_table, const int32_t* old_lens, const int32_t* new_lens, int32_t* free_pages,
+                           int32_t* num_free, int num_seqs, int pages_per_seq, int page_size, int num_pages, int total_new,
+                           int32_t* positions, int64_t* slots, int32_t* cu_new, int32_t* cu_kv, int32_t* missing,
+                           void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------
  * Lossless speculative acceptance over the full vocabulary.  Figure 1 caption (the

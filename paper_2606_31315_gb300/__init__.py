@@ -15,11 +15,14 @@ from ._binding import (  # noqa: F401
     block_attention_paged,
     block_attention_workspace_size,
     chunk_attention_paged,
+    chunk_attention_paged_fp8,
     chunk_attention_workspace_size,
     get_status,
     kv_append,
+    kv_append_fp8,
     library_path,
     load,
+    pages_update,
     policy_select,
     policy_select_workspace_size,
     qk_norm_rope,

@@ -80,6 +80,14 @@ def load():
     lib.bp_chunk_attention_paged.argtypes = [vp, i64, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32,
                                              i32, i32, i32, i32, i32, i32, f32, vp, sz, vp]
     lib.bp_chunk_attention_paged.restype = i32
+    lib.bp_chunk_attention_paged_fp8.argtypes = [vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32,
+                                                 i32, i32, i32, i32, i32, i32, i32, f32, vp, sz, vp]
+    lib.bp_chunk_attention_paged_fp8.restype = i32
+    lib.bp_kv_append_fp8.argtypes = [vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, i32,
+                                     vp, sz, vp]
+    lib.bp_kv_append_fp8.restype = i32
+    lib.bp_pages_update.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.bp_pages_update.restype = i32
     lib.bp_spec_accept_workspace_size.argtypes = [i32, i32, i32]
     lib.bp_spec_accept_workspace_size.restype = sz
     lib.bp_spec_accept.argtypes = [vp, vp, vp, vp, i32, i32, i32, f32, vp, vp, vp, vp, vp, vp, sz, vp]
@@ -432,6 +440,147 @@ def chunk_attention_paged(q, k_cache, v_cache, cu_q, cu_kv, block_table, page_si
     if rc:
         _check(rc, "bp_chunk_attention_paged")
     return out, lse
+
+
+# --------------------------------------------------------------------------- a paged cache in 8 bits
+_CODES = (torch.float8_e4m3fn, torch.uint8)
+_EXPONENTS = (torch.uint8, getattr(torch, "float8_e8m0fnu", torch.uint8))
+
+
+def _code_cache(k_cache, k_scale, v_cache, v_scale, page_size):
+    """(rows, heads, head_dim) of a cache in 8 bits; checks its four tensors."""
+    rows, hkv, d = shape = k_cache.shape
+    if v_cache.shape != shape or k_cache.dtype not in _CODES or v_cache.dtype not in _CODES:
+        raise ValueError("k_cache and v_cache must be [num_pages * page_size, heads, head_dim] of float8_e4m3fn (or uint8)")
+    if k_scale.dtype not in _EXPONENTS or v_scale.dtype not in _EXPONENTS:
+        raise ValueError("k_scale and v_scale must be uint8 (or float8_e8m0fnu): biased exponents")
+    if page_size < 1 or rows % page_size or k_scale.numel() != rows // page_size * hkv or v_scale.numel() != k_scale.numel():
+        raise ValueError("the caches must be whole pages, the scales one for each page and head")
+    if not (k_cache.is_cuda and k_cache.is_contiguous() and v_cache.is_cuda and v_cache.is_contiguous() and
+            k_scale.is_cuda and k_scale.is_contiguous() and v_scale.is_cuda and v_scale.is_contiguous()):
+        raise ValueError("the caches and their scales must be contiguous CUDA tensors")
+    return shape
+
+
+def kv_append_fp8(k_cache, k_scale, v_cache, v_scale, k_new, v_new, cu_new, cu_kv, block_table, page_size: int, ws=None,
+                  stream=None):
+    """Writes each sequence's new K/V rows into its pages of a cache in 8 bits; see ``bp_kv_append_fp8``.
+
+    k_cache / v_cache [num_pages * page_size, Hkv, D] float8_e4m3fn, k_scale / v_scale [num_pages, Hkv] uint8 (biased
+    exponents); k_new / v_new [T, Hkv, D] bf16 or fp32 (any stride between tokens); cu_new / cu_kv int32 [S+1], block_table
+    int32 [S, pages_per_seq] on the device.  A row without a place in the pages is reported in `ws` alone, and not written."""
+    lib = load()
+    page_size = int(page_size)
+    rows, hkv, d = _code_cache(k_cache, k_scale, v_cache, v_scale, page_size)
+    _int32("cu_new cu_kv block_table", cu_new, cu_kv, block_table)
+    dt = k_new.dtype
+    dtype = _DTYPES.get(dt)
+    if dtype is None:
+        raise ValueError("k_new and v_new must be bf16 or fp32")
+    t, heads, dim = shape = k_new.shape
+    if v_new.shape != shape or heads != hkv or dim != d:
+        raise ValueError("k_new and v_new must be [tokens, heads, head_dim] with the caches' heads and head_dim")
+    ks, vs = _heads("k_new", k_new, dt), _heads("v_new", v_new, dt)
+    s, per = block_table.shape
+    if cu_new.numel() != s + 1 or cu_kv.numel() != s + 1:
+        raise ValueError("cu_new and cu_kv must hold one more entry than block_table has rows")
+    if ws is None:
+        ws = workspace(256, k_cache.device, stream)
+    rc = lib.bp_kv_append_fp8(k_cache.data_ptr(), k_scale.data_ptr(), v_cache.data_ptr(), v_scale.data_ptr(),
+                              k_new.data_ptr(), ks, v_new.data_ptr(), vs, cu_new.data_ptr(), cu_kv.data_ptr(),
+                              block_table.data_ptr(), per, page_size, rows // page_size, s, t, hkv, d, dtype,
+                              ws.data_ptr(), ws.numel(), _stream(stream))
+    if rc:
+        _check(rc, "bp_kv_append_fp8")
+
+
+def chunk_attention_paged_fp8(q, k_cache, k_scale, v_cache, v_scale, cu_q, cu_kv, block_table, page_size: int,
+                              max_q_len: int, max_kv_len: int, mask: int = MASK_CAUSAL, window: int = 0,
+                              softmax_scale: float = 0.0, out=None, lse=None, ws=None, stream=None):
+    """``chunk_attention_paged`` over a cache in 8 bits (see kv_append_fp8 for its tensors); ``bp_chunk_attention_paged_fp8``.
+
+    q [total_q, Hq, D] bf16 (any stride between tokens), D 64 or 128; the workspace is chunk_attention_workspace_size's.
+    Returns (o, lse_or_None)."""
+    lib = load()
+    dt = q.dtype
+    if dt is not torch.bfloat16:
+        raise ValueError("q must be bf16")
+    t, hq, d = shape = q.shape
+    stride = hq * d if q.is_contiguous() and q.is_cuda else _heads("q", q, dt)
+    page_size = int(page_size)
+    rows, hkv, dk = _code_cache(k_cache, k_scale, v_cache, v_scale, page_size)
+    _cuda("out lse", out, lse)
+    _int32("cu_q cu_kv block_table", cu_q, cu_kv, block_table)
+    if dk != d:
+        raise ValueError("q and the caches must share one head_dim")
+    if out is None:
+        out = _empty((t, hq, d), dt, q.device, stream)
+    elif out.shape != shape or out.dtype is not dt:
+        raise ValueError("out must have q's shape and dtype")
+    if lse is not None and (lse.dtype is not torch.float32 or lse.numel() != t * hq):
+        raise ValueError("lse must be fp32 [tokens, query heads]")
+    s, per = block_table.shape
+    if cu_q.numel() != s + 1 or cu_kv.numel() != s + 1:
+        raise ValueError("cu_q and cu_kv must hold one more entry than block_table has rows")
+    if ws is None:
+        ws = workspace(lib.bp_chunk_attention_workspace_size(s, t, hq, hkv, d), q.device, stream)
+    rc = lib.bp_chunk_attention_paged_fp8(q.data_ptr(), stride, k_cache.data_ptr(), k_scale.data_ptr(), v_cache.data_ptr(),
+                                          v_scale.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
+                                          cu_q.data_ptr(), cu_kv.data_ptr(), block_table.data_ptr(), per, page_size,
+                                          rows // page_size, s, t, max_q_len, max_kv_len, hq, hkv, d, BF16, mask, window,
+                                          softmax_scale, ws.data_ptr(), ws.numel(), _stream(stream))
+    if rc:
+        _check(rc, "bp_chunk_attention_paged_fp8")
+    return out, lse
+
+
+def pages_update(block_table, old_lens, new_lens, free_pages, num_free, page_size: int, total_new=0, positions=None,
+                 slots=None, cu_new=None, cu_kv=None, missing=None, ws=None, stream=None):
+    """Pages from a pool's free list to a block table and back, and the new tokens' places; see ``bp_pages_update``.
+
+    block_table int32 [S, pages_per_seq], old_lens / new_lens int32 [S], free_pages int32 [num_pages], num_free int32 [1] on
+    the device; the table, the list and its length are updated in place.  total_new: how many new tokens positions (int32) and
+    slots (int64) have room for; None: neither is wanted.  Returns (positions, slots, cu_new, cu_kv, missing)."""
+    lib = load()
+    _int32("block_table old_lens new_lens free_pages num_free positions cu_new cu_kv missing", block_table, old_lens, new_lens,
+           free_pages, num_free, positions, cu_new, cu_kv, missing)
+    s, per = block_table.shape
+    dev = block_table.device
+    if old_lens.numel() != s or new_lens.numel() != s or num_free.numel() != 1:
+        raise ValueError("old_lens and new_lens must hold one length for each row of block_table, num_free one number")
+    pp = sp = None
+    if total_new is None:
+        if positions is not None or slots is not None:
+            raise ValueError("positions and slots go with total_new")
+        total_new = 0
+    else:
+        if positions is None:
+            positions = _empty(total_new, torch.int32, dev, stream)
+        if slots is None:
+            slots = _empty(total_new, torch.int64, dev, stream)
+        elif slots.dtype is not torch.int64 or not (slots.is_cuda and slots.is_contiguous()):
+            raise ValueError("slots must be a contiguous int64 CUDA tensor")
+        if positions.numel() != total_new or slots.numel() != total_new:
+            raise ValueError("positions and slots must hold total_new entries")
+        if total_new:  # (an empty tensor has no address)
+            pp, sp = positions.data_ptr(), slots.data_ptr()
+    if cu_new is None:
+        cu_new = _empty(s + 1, torch.int32, dev, stream)
+    if cu_kv is None:
+        cu_kv = _empty(s + 1, torch.int32, dev, stream)
+    if missing is None:
+        missing = _empty(1, torch.int32, dev, stream)
+    if cu_new.numel() != s + 1 or cu_kv.numel() != s + 1 or missing.numel() != 1:
+        raise ValueError("cu_new and cu_kv must hold one more entry than block_table has rows, missing one")
+    if ws is None:
+        ws = workspace(256, dev, stream)
+    rc = lib.bp_pages_update(block_table.data_ptr(), old_lens.data_ptr(), new_lens.data_ptr(), free_pages.data_ptr(),
+                             num_free.data_ptr(), s, per, int(page_size), free_pages.numel(), total_new, pp, sp,
+                             cu_new.data_ptr(), cu_kv.data_ptr(), missing.data_ptr(), ws.data_ptr(), ws.numel(),
+                             _stream(stream))
+    if rc:
+        _check(rc, "bp_pages_update")
+    return positions, slots, cu_new, cu_kv, missing
 
 
 # --------------------------------------------------------------------------- acceptance

@@ -227,11 +227,14 @@ size_t bp_chunk_attention_workspace_size(int num_seqs, int total_q, int num_q_he
     return sizeof(WorkspaceHeader) + chunk_attention_scratch_bytes(head_dim);
 }
 
-int bp_chunk_attention_paged(const void* q, int64_t q_stride, const void* k_cache, const void* v_cache, void* o,
-                             float* lse, const int32_t* cu_q, const int32_t* cu_kv, const int32_t* block_table,
-                             int pages_per_seq, int page_size, int num_pages, int num_seqs, int total_q, int max_q_len,
-                             int max_kv_len, int num_q_heads, int num_kv_heads, int head_dim, int dtype, int mask,
-                             int window, float softmax_scale, void* workspace, size_t workspace_bytes, void* stream) {
+namespace {
+// What both chunk attentions check; BP_OK and a filled `a`, or nothing to compute (`some` false).
+int check_chunk(ChunkAttentionArgs& a, DeviceInfo& dev, bool& some, const void* q, int64_t q_stride, const void* k_cache,
+                const void* v_cache, void* o, float* lse, const int32_t* cu_q, const int32_t* cu_kv,
+                const int32_t* block_table, int pages_per_seq, int page_size, int num_pages, int num_seqs, int total_q,
+                int max_q_len, int max_kv_len, int num_q_heads, int num_kv_heads, int head_dim, int dtype, int mask,
+                int window, float softmax_scale, void* workspace, size_t workspace_bytes) {
+    some = false;
     if (num_seqs < 0 || total_q < 0 || max_q_len < 0 || max_kv_len < 0 || window < 0) return BP_ERR_INVALID_ARG;
     if (num_seqs == 0 || total_q == 0) return BP_OK;  // nothing to compute
     if (!q || !k_cache || !v_cache || !o || !cu_q || !cu_kv || !block_table) return BP_ERR_INVALID_ARG;
@@ -251,9 +254,7 @@ int bp_chunk_attention_paged(const void* q, int64_t q_stride, const void* k_cach
     int rc = check_workspace(workspace, workspace_bytes,
                              bp_chunk_attention_workspace_size(num_seqs, total_q, num_q_heads, num_kv_heads, head_dim));
     if (rc != BP_OK) return rc;
-    DeviceInfo dev;
     if ((rc = device_info(&dev)) != BP_OK) return rc;
-    ChunkAttentionArgs a;
     a.q = q; a.q_stride = q_stride; a.k_cache = k_cache; a.v_cache = v_cache; a.o = o; a.lse = lse;
     a.cu_q = cu_q; a.cu_kv = cu_kv; a.block_table = block_table;
     a.pages_per_seq = pages_per_seq; a.page_size = page_size; a.num_pages = num_pages;
@@ -264,7 +265,110 @@ int bp_chunk_attention_paged(const void* q, int64_t q_stride, const void* k_cach
     a.scale = softmax_scale == 0.f ? 1.f / sqrtf((float)head_dim) : softmax_scale;
     a.scratch = scratch(workspace);
     a.err_word = err_word(workspace);
+    some = true;
+    return BP_OK;
+}
+}  // namespace
+
+int bp_chunk_attention_paged(const void* q, int64_t q_stride, const void* k_cache, const void* v_cache, void* o,
+                             float* lse, const int32_t* cu_q, const int32_t* cu_kv, const int32_t* block_table,
+                             int pages_per_seq, int page_size, int num_pages, int num_seqs, int total_q, int max_q_len,
+                             int max_kv_len, int num_q_heads, int num_kv_heads, int head_dim, int dtype, int mask,
+                             int window, float softmax_scale, void* workspace, size_t workspace_bytes, void* stream) {
+    ChunkAttentionArgs a;
+    DeviceInfo dev;
+    bool some;
+    int rc = check_chunk(a, dev, some, q, q_stride, k_cache, v_cache, o, lse, cu_q, cu_kv, block_table, pages_per_seq,
+                         page_size, num_pages, num_seqs, total_q, max_q_len, max_kv_len, num_q_heads, num_kv_heads,
+                         head_dim, dtype, mask, window, softmax_scale, workspace, workspace_bytes);
+    if (rc != BP_OK || !some) return rc;
     rc = launch_chunk_attention(a, dev, static_cast<cudaStream_t>(stream));
+    if (rc == BP_ERR_CUDA) cudaGetLastError();
+    return rc;
+}
+
+int bp_chunk_attention_paged_fp8(const void* q, int64_t q_stride, const void* k_cache, const void* k_scale,
+                                 const void* v_cache, const void* v_scale, void* o, float* lse, const int32_t* cu_q,
+                                 const int32_t* cu_kv, const int32_t* block_table, int pages_per_seq, int page_size,
+                                 int num_pages, int num_seqs, int total_q, int max_q_len, int max_kv_len, int num_q_heads,
+                                 int num_kv_heads, int head_dim, int dtype, int mask, int window, float softmax_scale,
+                                 void* workspace, size_t workspace_bytes, void* stream) {
+    if (num_seqs > 0 && total_q > 0 && (!k_scale || !v_scale)) return BP_ERR_INVALID_ARG;
+    ChunkAttentionFp8Args a;
+    DeviceInfo dev;
+    bool some;
+    int rc = check_chunk(a, dev, some, q, q_stride, k_cache, v_cache, o, lse, cu_q, cu_kv, block_table, pages_per_seq,
+                         page_size, num_pages, num_seqs, total_q, max_q_len, max_kv_len, num_q_heads, num_kv_heads,
+                         head_dim, dtype, mask, window, softmax_scale, workspace, workspace_bytes);
+    if (rc != BP_OK || !some) return rc;
+    a.k_scale = static_cast<const uint8_t*>(k_scale);
+    a.v_scale = static_cast<const uint8_t*>(v_scale);
+    rc = launch_chunk_attention_fp8(a, dev, static_cast<cudaStream_t>(stream));
+    if (rc == BP_ERR_CUDA) cudaGetLastError();
+    return rc;
+}
+
+int bp_kv_append_fp8(void* k_cache, void* k_scale, void* v_cache, void* v_scale, const void* k_new, int64_t k_stride,
+                     const void* v_new, int64_t v_stride, const int32_t* cu_new, const int32_t* cu_kv,
+                     const int32_t* block_table, int pages_per_seq, int page_size, int num_pages, int num_seqs,
+                     int total_new, int num_kv_heads, int head_dim, int dtype, void* workspace, size_t workspace_bytes,
+                     void* stream) {
+    if (num_seqs < 0 || total_new < 0) return BP_ERR_INVALID_ARG;
+    if (num_seqs == 0 || total_new == 0) return BP_OK;  // nothing to append
+    if (!k_cache || !k_scale || !v_cache || !v_scale || !k_new || !v_new || !cu_new || !cu_kv || !block_table)
+        return BP_ERR_INVALID_ARG;
+    if (num_kv_heads < 1 || head_dim < 1 || pages_per_seq < 1 || num_pages < 1 || !valid_page_size(page_size))
+        return BP_ERR_INVALID_ARG;
+    if ((long long)num_pages * page_size > INT32_MAX) return BP_ERR_INVALID_ARG;
+    if (dtype != BP_F32 && dtype != BP_BF16) return BP_ERR_INVALID_ARG;
+    const int64_t row = (int64_t)num_kv_heads * head_dim, step = dtype == BP_BF16 ? 8 : 4;
+    if (k_stride < row || v_stride < row) return BP_ERR_INVALID_ARG;
+    if (head_dim % 16 != 0 || num_kv_heads > 65535) return BP_ERR_UNSUPPORTED;
+    if (!aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) ||
+        k_stride % step != 0 || v_stride % step != 0)
+        return BP_ERR_INVALID_ARG;
+    int rc = check_workspace(workspace, workspace_bytes, sizeof(WorkspaceHeader));
+    if (rc != BP_OK) return rc;
+    DeviceInfo dev;
+    if ((rc = device_info(&dev)) != BP_OK) return rc;
+    KvAppendFp8Args a;
+    a.cache[0] = static_cast<uint8_t*>(k_cache); a.cache[1] = static_cast<uint8_t*>(v_cache);
+    a.scale[0] = static_cast<uint8_t*>(k_scale); a.scale[1] = static_cast<uint8_t*>(v_scale);
+    a.fresh[0] = k_new; a.fresh[1] = v_new;
+    a.stride[0] = k_stride; a.stride[1] = v_stride;
+    a.cu_new = cu_new; a.cu_kv = cu_kv; a.block_table = block_table;
+    a.pages_per_seq = pages_per_seq; a.page_size = page_size; a.num_pages = num_pages; a.num_seqs = num_seqs;
+    a.total_new = total_new; a.num_kv_heads = num_kv_heads; a.head_dim = head_dim; a.dtype = dtype;
+    a.err_word = err_word(workspace);
+    rc = launch_kv_append_fp8(a, static_cast<cudaStream_t>(stream));
+    if (rc == BP_ERR_CUDA) cudaGetLastError();
+    return rc;
+}
+
+int bp_pages_update(int32_t* block_table, const int32_t* old_lens, const int32_t* new_lens, int32_t* free_pages,
+                    int32_t* num_free, int num_seqs, int pages_per_seq, int page_size, int num_pages, int total_new,
+                    int32_t* positions, int64_t* slots, int32_t* cu_new, int32_t* cu_kv, int32_t* missing,
+                    void* workspace, size_t workspace_bytes, void* stream) {
+    if (num_seqs < 0 || total_new < 0 || num_pages < 0) return BP_ERR_INVALID_ARG;
+    if (num_seqs == 0 && total_new > 0) return BP_ERR_INVALID_ARG;  // (tokens of no sequence)
+    if (num_seqs > 0 && (!block_table || !old_lens || !new_lens)) return BP_ERR_INVALID_ARG;
+    if (!num_free || (num_pages > 0 && !free_pages) || pages_per_seq < (num_seqs > 0 ? 1 : 0) || !valid_page_size(page_size))
+        return BP_ERR_INVALID_ARG;
+    if ((long long)pages_per_seq * page_size > INT32_MAX) return BP_ERR_INVALID_ARG;
+    if (num_seqs > kPagesMaxSeqs) return BP_ERR_UNSUPPORTED;
+    int rc = check_workspace(workspace, workspace_bytes, sizeof(WorkspaceHeader));
+    if (rc != BP_OK) return rc;
+    DeviceInfo dev;
+    if ((rc = device_info(&dev)) != BP_OK) return rc;
+    PagesUpdateArgs a;
+    a.block_table = block_table; a.old_lens = old_lens; a.new_lens = new_lens;
+    a.free_pages = free_pages; a.num_free = num_free;
+    a.num_seqs = num_seqs; a.pages_per_seq = pages_per_seq; a.page_size = page_size; a.num_pages = num_pages;
+    a.total_new = total_new; a.positions = positions; a.slots = slots;
+    a.cu_new = cu_new; a.cu_kv = cu_kv; a.missing = missing;
+    a.ticket = &static_cast<WorkspaceHeader*>(workspace)->pad[15];
+    a.err_word = err_word(workspace);
+    rc = launch_pages_update(a, dev, static_cast<cudaStream_t>(stream));
     if (rc == BP_ERR_CUDA) cudaGetLastError();
     return rc;
 }

@@ -116,9 +116,47 @@ struct ChunkAttentionArgs {
     void* scratch;  // chunk_attention_scratch_bytes(head_dim)
     unsigned int* err_word;
 };
+struct ChunkAttentionFp8Args : ChunkAttentionArgs {  // k_cache, v_cache: e4m3
+    const uint8_t* k_scale;  // [num_pages][num_kv_heads] biased exponents
+    const uint8_t* v_scale;
+};
 constexpr int kChunkMaxGrid = 192;  // CTAs at most, one an SM; each has its parts' place in the workspace
 size_t chunk_attention_scratch_bytes(int head_dim);
 int launch_chunk_attention(const ChunkAttentionArgs& a, const DeviceInfo& dev, cudaStream_t stream);
+int launch_chunk_attention_fp8(const ChunkAttentionFp8Args& a, const DeviceInfo& dev, cudaStream_t stream);
+
+// New keys and values to the pages of a cache in e4m3, with a scale for each page and head.
+struct KvAppendFp8Args {
+    uint8_t* cache[2];  // of keys, of values; all pairs below likewise
+    uint8_t* scale[2];
+    const void* fresh[2];
+    int64_t stride[2];  // elements from a token to the next
+    const int32_t* cu_new;
+    const int32_t* cu_kv;
+    const int32_t* block_table;
+    int pages_per_seq, page_size, num_pages, num_seqs, total_new, num_kv_heads, head_dim, dtype;
+    unsigned int* err_word;
+};
+int launch_kv_append_fp8(const KvAppendFp8Args& a, cudaStream_t stream);
+
+// Pages from a pool's free list to a block table and back, and the new tokens' places.
+struct PagesUpdateArgs {
+    int32_t* block_table;
+    const int32_t* old_lens;
+    const int32_t* new_lens;
+    int32_t* free_pages;
+    int32_t* num_free;
+    int num_seqs, pages_per_seq, page_size, num_pages, total_new;
+    int32_t* positions;  // [total_new] or null
+    int64_t* slots;      // likewise
+    int32_t* cu_new;     // [num_seqs + 1] or null
+    int32_t* cu_kv;      // likewise
+    int32_t* missing;    // [1] or null
+    unsigned int* ticket;
+    unsigned int* err_word;
+};
+constexpr int kPagesMaxSeqs = 16384;
+int launch_pages_update(const PagesUpdateArgs& a, const DeviceInfo& dev, cudaStream_t stream);
 
 // Norms and rotation of queries and keys; with a cache, the keys and values go to their pages.
 struct RopeArgs {
