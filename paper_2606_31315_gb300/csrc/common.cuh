@@ -57,7 +57,8 @@ inline size_t tmem_smem(const DeviceInfo& dev, int columns, size_t bytes) {
 
 // Encodes a tiled TMA descriptor (driver entry point resolved once).
 int encode_tensor_map(CUtensorMap* map, CUtensorMapDataType dt, cuuint32_t rank, void* base, const cuuint64_t* dims,
-                      const cuuint64_t* strides_bytes, const cuuint32_t* box, CUtensorMapSwizzle swizzle);
+                      const cuuint64_t* strides_bytes, const cuuint32_t* box, CUtensorMapSwizzle swizzle,
+                      CUtensorMapL2promotion promotion = CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 
 // Launchers (host side).  They assume the arguments were validated by the API layer.
 struct AttentionArgs {
