@@ -5,13 +5,13 @@
 //
 // Nothing is rounded that a bf16 cache would not round:
 //   * S = Q K^T on the codes as they lie in memory, kind::f8f6f4.  A query row, scaled by a power of two to at most 256, is the
-//     sum of two e4m3 numbers, its nearest and what is left: bf16's 8 bits are twice 4.  (Elements below 2^-10 of the row's
-//     largest lose bits under 2^-18 of it.)  The row's and the page's powers multiply the scores in the softmax.
+//     sum of two e4m3 numbers: bf16's 8 bits are twice 4.  (Elements below 2^-9 of the row's largest lose what is under
+//     2^-16 of it.)  The row's and the page's powers multiply the scores in the softmax.
 //   * P V in fp16, which holds every e4m3 number; four warps turn a tile's codes into them, in shared memory.  The weights take
 //     the values' powers of two.
-// The rest is as there: the line of work, two streams of a query tile each, the merge.  Where
-// a work tile has the rows of one stream only (blocks, decoding), both streams take its queries and every other key tile,
-// and add what they have at the end: a stream alone is a chain of latencies.
+// The line of work and the merge are chunk_attention.cu's.  Two kernels: chunk_attention_fp8_kernel for any call, its two streams a
+// query tile each (where a work tile has the rows of one only, both take them, and every other key tile, and add what they
+// have at the end), and block_attention_fp8_kernel for calls whose work tiles all are such: blocks and single tokens.
 //
 // Roles: warps 0-3 and 4-7 softmax of stream 0 and 1 (a thread a row; they read and split the queries too), warp 8 lays out
 // the jobs and issues K's TMA copies, 9 and 10 issue the streams' MMAs, 11 V's copies and what the merge has to know, 12-15
@@ -21,40 +21,43 @@
 #include <algorithm>
 #include <mutex>
 
+namespace bp {
+namespace {
+// A work tile's fixed cost (queries in, output out), in keys: a prompt of 8192 takes 607 us with 400, 552 with 800, 567 with 1200.
+constexpr int kTileCost = 800;
+}  // namespace
+}  // namespace bp
+
 #include "chunk_plan.cuh"
 
 namespace bp {
 namespace {
 
 constexpr int kHalfBytes = kKeys * 128;          // 128 rows of 64 fp16 columns (or of 128 codes), 128-byte swizzle
-constexpr int kSoftmaxWarps = 8;                 // a thread a row
-constexpr int kProducerWarp = 8, kMmaWarp = 9, kConvertWarp = 12;  // (a stream's MMA warp: kMmaWarp + stream)
+constexpr uint32_t kChunkTmem = 512;
+constexpr int kSoftmaxWarps = 8;                 // a thread a row, four warps a stream
+constexpr int kKeyWarp = 8, kMmaWarp = 9, kValueWarp = 11, kConvertWarp = 12;  // (a stream's MMA warp: kMmaWarp + stream)
 constexpr int kConvertWarps = 4;                 // 32 keys of a tile each
-constexpr int kFp8Threads = 32 * 16;
+constexpr int kThreads = 32 * (kConvertWarp + kConvertWarps);
 // Registers: 128 a thread at launch (512 x 128); 256 x 192 + 256 x 64 are as many.
 constexpr int kSoftmaxRegs = 192, kOtherRegs = 64;
-constexpr uint32_t kChunkTmem = 512;
 constexpr int kJobs = 4;                         // jobs laid out ahead
+constexpr int kBatches = 8;                      // of 32 boxes' scales: jobs and tiles that may be under way at once, and more
 
-template <int D>
+// FEW: work tiles of one stream only.  Their kernel has no second query tile.
+template <int D, bool FEW>
 struct Shape {
     static constexpr int code_bytes = kKeys * D;                // one K or V tile of codes
     static constexpr int v_bytes = 2 * code_bytes;              // one V tile in fp16
     static constexpr int q_bytes = 2 * code_bytes;              // one query tile, both parts
     static constexpr int k_slots = D == 128 ? 3 : 8;
-    static constexpr int raw_slots = D == 128 ? 3 : 7;          // V's codes
+    static constexpr int raw_slots = (D == 128 ? 3 : 7) + 2 * FEW;  // V's codes
     static constexpr int v_slots = D == 128 ? 2 : 4;
-    static constexpr int notes = D == 128 ? 8 : 16;             // of key tiles: more than can be under way at once
-    static constexpr int at_k = 2 * q_bytes;
+    static constexpr int at_k = (FEW ? 1 : 2) * q_bytes;
     static constexpr int at_raw = at_k + k_slots * code_bytes;
     static constexpr int at_v = at_raw + raw_slots * code_bytes;
     static constexpr int tiles = at_v + v_slots * v_bytes;
-    static constexpr uint32_t col_o = 256;                      // O of stream i: columns col_o + i * D
 };
-static_assert(Shape<128>::tiles >= tmem_smem_share((int)kChunkTmem, 228 * 1024) &&
-                  Shape<64>::tiles >= tmem_smem_share((int)kChunkTmem, 228 * 1024),
-              "leaves no other CTA's tensor memory room");
-
 struct Fp8Params {
     ChunkParams c;
     const __nv_bfloat16* q;
@@ -64,31 +67,30 @@ struct Fp8Params {
     const uint8_t* v;  // the cache's codes
 };
 
-// Shared memory behind the tiles.
-template <int D>
-struct Shared {
-    using S = Shape<D>;
+// Shared memory of a block that needs so much: it leaves no other CTA's tensor memory room.
+constexpr int whole_sm(int bytes) {
+    const int share = tmem_smem_share((int)kChunkTmem, 228 * 1024);
+    return bytes > share ? bytes : share;
+}
+
+// Shared memory behind the tiles: what both kernels have.
+template <int D, bool FEW>
+struct Common {
+    using S = Shape<D, FEW>;
     uint64_t k_full[S::k_slots], k_empty[S::k_slots], raw_full[S::raw_slots], raw_empty[S::raw_slots];
     uint64_t v_full[S::v_slots], v_empty[S::v_slots];
-    uint64_t q_ready[2], drain[2], turn[2];
-    uint64_t s[2], p[2], o[2];                       // of a stream: scores, weights, the accumulator
     uint64_t job_full[kJobs], job_empty[kJobs];
-    float k_power[S::notes][8];                      // the scales of a tile's boxes, of keys
-    uint8_t v_below[S::raw_slots][8];                // of values: how far below the tile's largest one, as powers of two
-    int v_ref[S::notes];                             // that one, biased
+    // The scales of the boxes (Boxes), 32 at a time: of keys; of values how far below the largest one of their tile, as
+    // powers of two, and that one.  Biased exponents.
+    uint8_t k_exp[kBatches][32], v_below[kBatches][32], v_ref[kBatches][32];
     Job job[kJobs];
     int job_nan[kJobs];                              // a code among its values is not a number
     uint32_t tmem;
-    float2 row[2][kTileM];                           // of a split job's streams: row maxima and sums
-    int row_ref[2][4];                               // and what their accumulators are in units of
 };
-template <int D>
-constexpr int fp8_smem() { return Shape<D>::tiles + (int)sizeof(Shared<D>); }
-static_assert(fp8_smem<128>() <= 227 * 1024 && fp8_smem<64>() <= 227 * 1024, "a block's shared memory");
 
 // The values' powers of two: a tile's are held against its largest one (below 2^-24 of it they are 0; fp16 has e4m3's 18
 // powers and 22 more), and that one against the largest so far, `ref`: the weights take the difference, times 2^7.  So they
-// are at most 2^15 in fp16, and a tile's whose values are 2^-14 of others' still have all their bits at a weight of 2^-7.
+// are at most 2^15 in fp16, and a tile whose values are 2^-14 of others' still has all its weights' bits down to 2^-7.
 constexpr uint32_t kLeastRef = 15;  // of a tile, so that the accumulator's power is a number too
 
 // 2^(e - 127) of a biased exponent below 255.
@@ -109,7 +111,7 @@ __device__ __forceinline__ uint32_t split_queries(const __nv_bfloat16* q, int64_
         return tile + row * 128 + (D == 128 ? part * kHalfBytes : 0) + (((i + (D == 128 ? 0 : part * 4)) ^ (row & 7)) << 4);
     };
     const int piece = lane % kPieces;
-#pragma unroll 2
+#pragma unroll 8
     for (int k = 0; k < kPieces; ++k) {
         const int row = k * kRows + lane / kPieces;
         const int64_t from = __shfl_sync(0xffffffffu, at, row);
@@ -118,7 +120,7 @@ __device__ __forceinline__ uint32_t split_queries(const __nv_bfloat16* q, int64_
     cp_async_wait_all();
     __syncwarp();
     uint32_t top = 0;
-#pragma unroll 2
+#pragma unroll 8
     for (int i = 0; i < D / 8; ++i) {
         const uint4 v = *reinterpret_cast<const uint4*>(place(lane, i & 1, i >> 1));
         const uint32_t x = max(max(v.x & 0x7fffu, v.y & 0x7fffu), max(v.z & 0x7fffu, v.w & 0x7fffu));
@@ -197,14 +199,14 @@ __device__ __forceinline__ void write_rows(const ChunkParams& p, uint32_t mine, 
     }
 }
 
-// Whether one of the values of keys [key, key + 64) that lie in [lo, hi) has a code that is not a number; lo and hi are of
+// Whether one of the values of key tile [key, key + kKeys) that lie in [lo, hi) has a code that is not a number; lo and hi are of
 // the lane's row, and the whole warp calls this.
 template <int D>
 __device__ __forceinline__ bool sees_nan(const Fp8Params& fp, const Job& g, int key, int lo, int hi) {
     const ChunkParams& p = fp.c;
     const int lane = threadIdx.x & 31;
     bool sees = false;
-    for (const int end = min(g.n, key + 64); key < end; ++key) {
+    for (const int end = min(g.n, key + kKeys); key < end; ++key) {
         const int pg = key >> p.page_shift;
         int id = pg < p.pages_per_seq ? __ldg(p.block_table + (size_t)g.s * p.pages_per_seq + pg) : 0;
         if ((unsigned)id >= (unsigned)p.num_pages) id = 0;  // (reported where the tile was asked for)
@@ -217,81 +219,302 @@ __device__ __forceinline__ bool sees_nan(const Fp8Params& fp, const Job& g, int 
     return sees;
 }
 
-// The boxes that a job's key tiles come in, one a page or, of larger pages, one a tile: their pages and scales, looked up by
-// a whole warp, 32 boxes at a time, the next ones in flight meanwhile (tile by tile, table and then scale, they alone took
-// 1.5 us a tile).
+// The boxes that a job's key tiles come in, one a page or, of larger pages, one a tile: looked up by a whole warp, 32 boxes (a
+// batch) at a time and a lane each, the next ones in flight meanwhile.  (Tile by tile, table and then scale, they alone took 1.5 us
+// a tile.)  A job begins a new batch.
 struct Boxes {
     const ChunkParams& p;
     const uint8_t* scale;
     const Job& g;
-    int rows, of_tile, last_page;  // keys of a box; boxes of a tile; the sequence's last page
-    int near, far, used = 0;       // this lane's page of the 32 boxes at hand and of the next 32 (-1: none); boxes done with
-    uint32_t near_e, far_e;        // their scales
-    uint32_t exponent;             // the scale of this lane's box of the tile that next() was for
+    int rows, of_tile, ahead;  // keys of a box; boxes of a tile; tiles of a batch
+    int row;                   // this lane's box of the batch at hand: its first key's row in the pool (-1: none)
+    uint32_t exponent;         // and its scale
+    int far_id;                // of the next batch
+    uint32_t far_exponent;
 
     __device__ __forceinline__ Boxes(const ChunkParams& params, const uint8_t* scales, const Job& job)
-        : p(params), scale(scales), g(job), rows(min(kKeys, 1 << params.page_shift)), of_tile(kKeys / rows),
-          last_page((job.n - 1) >> params.page_shift) {
-        look_up(g.j0, near, near_e);
-        look_up(g.j0 + 32 / of_tile, far, far_e);
+        : p(params), scale(scales), g(job), rows(min(kKeys, 1 << params.page_shift)), of_tile(kKeys / rows), ahead(32 / of_tile) {
+        look_up(g.j0);
     }
-    __device__ __forceinline__ void look_up(int j, int& id, uint32_t& e) const {
+    __device__ __forceinline__ int key_of(int j) const {
         const int lane = threadIdx.x & 31;
-        j += lane / of_tile;
-        const int pg = (j * kKeys + lane % of_tile * rows) >> p.page_shift;
-        id = -1;
-        e = 127;
-        if (j < g.j1 && pg <= last_page) {
-            id = pg < p.pages_per_seq ? __ldg(p.block_table + (size_t)g.s * p.pages_per_seq + pg) : -1;
-            if ((unsigned)id >= (unsigned)p.num_pages) {
+        return (j + lane / of_tile) * kKeys + lane % of_tile * rows;
+    }
+    __device__ __forceinline__ void look_up(int j) {
+        const int key = key_of(j), pg = key >> p.page_shift;
+        far_id = -1;
+        far_exponent = 127;
+        if (key / kKeys < g.j1 && key < g.n) {
+            far_id = pg < p.pages_per_seq ? __ldg(p.block_table + (size_t)g.s * p.pages_per_seq + pg) : -1;
+            if ((unsigned)far_id >= (unsigned)p.num_pages) {
                 raise_error(p.err, kErrDeviceArg);
-                id = 0;
+                far_id = 0;
             }
-            e = __ldg(scale + (size_t)id * p.num_kv_heads + g.h);
+            far_exponent = __ldg(scale + (size_t)far_id * p.num_kv_heads + g.h);
         }
     }
-    // The pool row of this lane's box of tile j, -1 where it has none.
-    __device__ __forceinline__ int next(int j) {
-        const int lane = threadIdx.x & 31, at = (used + lane) & 31;
-        const int id = __shfl_sync(0xffffffffu, near, at);
-        exponent = __shfl_sync(0xffffffffu, near_e, at);
-        if ((used += of_tile) == 32) {
-            used = 0;
-            near = far;
-            near_e = far_e;
-            look_up(j + 1 + 32 / of_tile, far, far_e);
-        }
-        if (lane >= of_tile || id < 0) return -1;
+    // The batch that begins with tile j.
+    __device__ __forceinline__ void next(int j) {
+        row = far_id < 0 ? -1 : (far_id << p.page_shift) + (key_of(j) & ((1 << p.page_shift) - 1));
+        exponent = far_exponent;
         if (exponent == 255) {
             raise_error(p.err, kErrDeviceArg);
             exponent = 254;
         }
-        return (id << p.page_shift) + ((j * kKeys + lane * rows) & ((1 << p.page_shift) - 1));
+        look_up(j + ahead);
     }
     // The keys of tile j's boxes.
     __device__ __forceinline__ uint32_t keys(int j) const { return min(of_tile, (g.n - j * kKeys + rows - 1) / rows) * rows; }
 };
+// A job's batches before the one of its tile t, and the place of that tile's box `b` in it (of boxes of 2^shift keys).
+__device__ __forceinline__ unsigned batch_of(int t, int shift) { return (unsigned)t >> (shift - 2); }
+__device__ __forceinline__ int in_batch(int t, int b, int shift) { return ((t << (7 - shift)) + b) & 31; }
+__device__ __forceinline__ unsigned batches_of(int tiles, int shift) { return (unsigned)(tiles + (1 << (shift - 2)) - 1) >> (shift - 2); }
 
-// FACTORS: scales that a tile of 128 keys may have: 8 with pages of 16, 2 from pages of 64 on.
-template <int D, int FACTORS>
-__global__ void __launch_bounds__(kFp8Threads, 1)
-chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_constant__ CUtensorMap kmap,
-                           const __grid_constant__ CUtensorMap vmap) {
-    using S = Shape<D>;
+// The next job, for a warp that has had `nj` of them; none if there are no more (or a wait was given up: ok is false).  The
+// warp reads what it needs and calls had_job.
+template <class Sh>
+__device__ __forceinline__ const Job* next_job(Sh& sh, unsigned nj, bool& ok) {
+    ok = __all_sync(0xffffffffu, mbar_wait(&sh.job_full[nj % kJobs], (nj / kJobs) & 1, kWaitBudget));
+    if (!ok) return nullptr;
+    const Job* g = &sh.job[nj % kJobs];
+    return g->s >= 0 ? g : nullptr;
+}
+template <class Sh>
+__device__ __forceinline__ void had_job(Sh& sh, unsigned& nj) {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(&sh.job_empty[nj % kJobs]);
+    ++nj;
+}
+
+// A warp's role: this CTA's part of the line, laid out in jobs; K tiles of codes through their ring.
+template <int D, bool FEW, class Sh>
+__device__ __forceinline__ void bring_keys(const Fp8Params& fp, const CUtensorMap* kmap, Sh& sh, uint8_t* smem) {
+    using S = Shape<D, FEW>;
     const ChunkParams& p = fp.c;
-    extern __shared__ __align__(1024) uint8_t smem[];
-    Shared<D>& sh = *reinterpret_cast<Shared<D>*>(smem + S::tiles);
+    const int lane = threadIdx.x & 31;
+    Place place[2];
+    find_places(p, lane, place);
+    Walk walk{p, place[0], place[1], -1, Seq{}, 0};
+    unsigned nj = 0;
+    bool ok = true;
+    // lays out the next job, or the end of them
+    auto lay_out = [&](Job& g) {
+        if (!walk.next(g)) g.s = -1;
+        const int e = nj % kJobs;
+        if (nj >= kJobs && !__all_sync(0xffffffffu, mbar_wait(&sh.job_empty[e], ((nj / kJobs) - 1) & 1, kWaitBudget))) {
+            ok = false;
+            return;
+        }
+        if (lane == 0) {
+            sh.job[e] = g;
+            sh.job_nan[e] = 0;
+            mbar_arrive(&sh.job_full[e]);
+        }
+        ++nj;
+    };
+    unsigned x = 0, batch = 0;  // tiles asked for, batches
+    Job g, after;
+    for (bool have = false; ; have = true) {
+        lay_out(after);  // one ahead of the copies
+        if (!ok) break;
+        if (have && g.j1 > g.j0) {
+            Boxes box(p, fp.k_scale, g);
+            for (int j = g.j0; j < g.j1 && ok; ++batch) {
+                box.next(j);
+                sh.k_exp[batch % kBatches][lane] = (uint8_t)box.exponent;
+                __syncwarp();
+                for (int k = 0; k < box.ahead && j < g.j1; ++k, ++j, ++x) {
+                    const int slot = x % S::k_slots;
+                    ok = x < (unsigned)S::k_slots || __all_sync(0xffffffffu, mbar_wait(&sh.k_empty[slot], (x / S::k_slots - 1) & 1, kWaitBudget));
+                    if (!ok) break;
+                    const int mine = lane - k * box.of_tile;  // this lane's box of the tile
+                    if (mine == 0) mbar_arrive_expect_tx(&sh.k_full[slot], box.keys(j) * D);
+                    if (mine >= 0 && mine < box.of_tile && box.row >= 0)
+                        tma_load_3d(smem + S::at_k + slot * S::code_bytes + mine * box.rows * D, kmap, &sh.k_full[slot], 0, g.h, box.row);
+                    __syncwarp();
+                }
+            }
+        }
+        if (!ok || after.s < 0) break;
+        g = after;
+    }
+    if (!ok && lane == 0) raise_error(p.err, kErrTimeout);
+    // no copy may still be in flight when the CTA leaves
+    for (unsigned y = x > (unsigned)S::k_slots ? x - S::k_slots : 0; y < x; ++y)
+        if (!mbar_wait(&sh.k_full[y % S::k_slots], (y / S::k_slots) & 1, kDrainBudget) && lane == 0) raise_error(p.err, kErrTimeout);
+}
+
+// A warp's role: V tiles of codes through their ring; what this CTA leaves to the merge.
+template <int D, bool FEW, class Sh>
+__device__ __forceinline__ void bring_values(const Fp8Params& fp, const CUtensorMap* vmap, Sh& sh, uint8_t* smem) {
+    using S = Shape<D, FEW>;
+    const ChunkParams& p = fp.c;
+    const int lane = threadIdx.x & 31;
+    unsigned x = 0, batch = 0, nj = 0;
+    int4 left = make_int4(0, 0, 0, 0);
+    bool ok, fine = true;
+    while (const Job* job = next_job(sh, nj, ok)) {
+        const Job g = *job;
+        had_job(sh, nj);
+        if (!g.first) left.x |= kHasHead | (g.last ? kHeadEnds : 0);
+        if (g.first && !g.last)
+            left = make_int4(left.x | kHasTail, g.q0 + g.t * 2 * p.tokens, min(2 * p.tokens, g.B - g.t * 2 * p.tokens), g.h);
+        if (g.j1 <= g.j0) continue;
+        Boxes box(p, fp.v_scale, g);
+        for (int j = g.j0; j < g.j1 && fine; ++batch) {
+            box.next(j);
+            uint32_t ref = box.row >= 0 ? max(box.exponent, kLeastRef) : kLeastRef;
+            for (int o = 1; o < box.of_tile; o <<= 1) ref = max(ref, __shfl_xor_sync(0xffffffffu, ref, o));
+            sh.v_ref[batch % kBatches][lane] = (uint8_t)ref;
+            sh.v_below[batch % kBatches][lane] = (uint8_t)(box.row >= 0 ? ref - box.exponent : 0u);
+            __syncwarp();
+            for (int k = 0; k < box.ahead && j < g.j1; ++k, ++j, ++x) {
+                const int slot = x % S::raw_slots;
+                fine = x < (unsigned)S::raw_slots || __all_sync(0xffffffffu, mbar_wait(&sh.raw_empty[slot], (x / S::raw_slots - 1) & 1, kWaitBudget));
+                if (!fine) break;
+                const int mine = lane - k * box.of_tile;
+                if (mine == 0) mbar_arrive_expect_tx(&sh.raw_full[slot], box.keys(j) * D);
+                if (mine >= 0 && mine < box.of_tile && box.row >= 0)
+                    tma_load_3d(smem + S::at_raw + slot * S::code_bytes + mine * box.rows * D, vmap, &sh.raw_full[slot], 0, g.h, box.row);
+                __syncwarp();
+            }
+        }
+        if (!fine) break;
+    }
+    if ((!ok || !fine) && lane == 0) raise_error(p.err, kErrTimeout);
+    for (unsigned y = x > (unsigned)S::raw_slots ? x - S::raw_slots : 0; y < x; ++y)
+        if (!mbar_wait(&sh.raw_full[y % S::raw_slots], (y / S::raw_slots) & 1, kDrainBudget) && lane == 0) raise_error(p.err, kErrTimeout);
+    if (lane == 0) p.info[blockIdx.x] = left;
+}
+
+// The role of warp w of those that turn V from codes to fp16, in shared memory: keys [32 w, 32 w + 32) of every tile.
+template <int D, bool FEW, class Sh>
+__device__ __forceinline__ void convert_values(const ChunkParams& p, Sh& sh, uint8_t* smem, int w) {
+    using S = Shape<D, FEW>;
+    // Eight lanes read all banks, and write them: a key's lower pieces of 16 codes with the next key's upper ones (form 0; 1:
+    // the other way round; of 64 columns: the two keys' pieces all together).  From one piece of a lane to the next of its
+    // form it is 8 keys, which the swizzle does not tell apart.
+    constexpr int kForms = D == 128 ? 2 : 1, kPieces = 2 * kForms;  // pieces of 16 keys
+    const int lane = threadIdx.x & 31, e = lane & 7;
+    const int key0 = w * 32 + (lane >> 3) * 2 + (e >> 2);
+    int from[kForms], to[kForms];
+#pragma unroll
+    for (int form = 0; form < kForms; ++form) {
+        const int piece = (e & 3) + (D == 128 ? 4 * ((e >> 2) ^ form) : 0);
+        from[form] = key0 * D + piece * 16;
+        to[form] = (piece >> 2) * kHalfBytes + key0 * 128 + (((2 * (piece & 3)) ^ (key0 & 7)) << 4);
+    }
+    const int box_shift = min(7, p.page_shift);
+    unsigned x = 0, batch0 = 0, nj = 0;
+    bool ok, fine = true;
+    while (const Job* g = next_job(sh, nj, ok)) {
+        const int j0 = g->j0, j1 = g->j1, n = g->n;
+        int* const nan = &sh.job_nan[nj % kJobs];
+        had_job(sh, nj);
+        for (int j = j0; j < j1; ++j, ++x) {
+            const int rs = x % S::raw_slots, vs = x % S::v_slots;
+            fine = __all_sync(0xffffffffu, mbar_wait(&sh.raw_full[rs], (x / S::raw_slots) & 1, kWaitBudget));
+            const uint8_t* raw = smem + S::at_raw + rs * S::code_bytes;
+            uint8_t* out = smem + S::at_v + vs * S::v_bytes;
+            const int left = n - j * kKeys;  // keys from this one on are none: zeros
+            uint32_t look[4] = {0, 0, 0, 0};
+            auto power = [&](int h) {  // what half h's values are multiplied by, as fp16
+                const int below = sh.v_below[(batch0 + batch_of(j - j0, box_shift)) % kBatches][in_batch(j - j0, (w * 32 + h * 16) >> box_shift, box_shift)];
+                return (below < 15 ? (15 - below) << 10 : below < 25 ? 1 << (24 - below) : 0) * 0x10001u;
+            };
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {  // 16 keys at a time: boxes are no smaller
+                uint32_t v[kPieces][4];
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) {
+                    const uint4 c = *reinterpret_cast<const uint4*>(raw + from[k % kForms] + (h * kPieces + k) / kForms * 8 * D);
+                    v[k][0] = c.x; v[k][1] = c.y; v[k][2] = c.z; v[k][3] = c.w;
+                }
+                if (left < kKeys) {
+#pragma unroll
+                    for (int k = 0; k < kPieces; ++k)
+                        if (key0 + (h * kPieces + k) / kForms * 8 >= left) v[k][0] = v[k][1] = v[k][2] = v[k][3] = 0;
+                }
+                uint32_t y[kPieces][8];
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        e4m3x4_to_f16x4(v[k][c], y[k][2 * c], y[k][2 * c + 1]);
+                        look[c] |= (v[k][c] & 0x7f7f7f7fu) + 0x01010101u;  // bit 7 of a byte: its code is 0x7f or 0xff
+                    }
+                const uint32_t mul = power(h);
+                if (mul != 0x3c003c00u) {
+#pragma unroll
+                    for (int k = 0; k < kPieces; ++k)
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) y[k][c] = mul_f16x2(y[k][c], mul);
+                }
+                if (h == 0) {
+                    if (fine && x >= (unsigned)S::v_slots) fine = mbar_wait(&sh.v_empty[vs], (x / S::v_slots - 1) & 1, kWaitBudget);
+                    fine = __all_sync(0xffffffffu, fine);
+                    if (!fine) break;
+                }
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) {
+                    uint8_t* const at = out + (h * kPieces + k) / kForms * 1024;
+                    *reinterpret_cast<uint4*>(at + to[k % kForms]) = make_uint4(y[k][0], y[k][1], y[k][2], y[k][3]);
+                    *reinterpret_cast<uint4*>(at + (to[k % kForms] ^ 16)) = make_uint4(y[k][4], y[k][5], y[k][6], y[k][7]);
+                }
+            }
+            if (!fine) break;
+            // 0 in the place of what is not a number: rare, and after all is stored (with a vote before it 64 x 1 tokens over
+            // 4096 keys took 187 us instead of 147).
+            if ((look[0] | look[1] | look[2] | look[3]) & 0x80808080u) {
+#pragma unroll 1
+                for (int k = 0; k < 2 * kPieces; ++k) {
+                    const int form = k % kForms, at = k / kForms * 1024;
+                    const uint4 c = *reinterpret_cast<const uint4*>(raw + from[0] + (form ? from[kForms - 1] - from[0] : 0) + k / kForms * 8 * D);
+                    uint8_t* const piece = out + (form ? to[kForms - 1] : to[0]) + at;
+                    if (key0 + k / kForms * 8 >= left) continue;
+                    const uint32_t v[4] = {c.x, c.y, c.z, c.w}, mul = power(k / kPieces);
+                    uint32_t y[8], none = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        e4m3x4_to_f16x4(v[i], y[2 * i], y[2 * i + 1]);
+                        none |= ((v[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+                    }
+                    if (!none) continue;
+                    *nan = 1;  // (the softmax warps look once all of the job's values have been used)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) y[i] = mul_f16x2(drop_nan_f16x2(y[i]), mul);
+                    *reinterpret_cast<uint4*>(piece) = make_uint4(y[0], y[1], y[2], y[3]);
+                    *reinterpret_cast<uint4*>(out + ((form ? to[kForms - 1] : to[0]) ^ 16) + at) = make_uint4(y[4], y[5], y[6], y[7]);
+                }
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(&sh.v_full[vs]);
+                mbar_arrive(&sh.raw_empty[rs]);
+            }
+        }
+        if (!fine) break;
+        batch0 += batches_of(max(0, j1 - j0), box_shift);
+    }
+    if ((!fine || !ok) && lane == 0) raise_error(p.err, kErrTimeout);
+}
+
+// What both kernels begin with: barriers, tensor memory; false where the shared memory is not as they need it.
+template <int D, bool FEW, class Sh>
+__device__ __forceinline__ bool begin(const ChunkParams& p, const CUtensorMap* kmap, const CUtensorMap* vmap, Sh& sh, uint8_t* smem,
+                                      int arrivals_empty) {
+    using S = Shape<D, FEW>;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int G = p.group;
     if (smem_addr(smem) & 1023) {  // (the swizzled tiles' alignment: dynamic shared memory starts on such a boundary)
         if (tid == 0) raise_error(p.err, kErrDeviceArg);
-        return;
+        return false;
     }
-
     if (tid == 0) {
         for (int i = 0; i < S::k_slots; ++i) {
             mbar_init(&sh.k_full[i], 1);
-            mbar_init(&sh.k_empty[i], 2);
+            mbar_init(&sh.k_empty[i], arrivals_empty);
         }
         for (int i = 0; i < S::raw_slots; ++i) {
             mbar_init(&sh.raw_full[i], 1);
@@ -299,46 +522,140 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
         }
         for (int i = 0; i < S::v_slots; ++i) {
             mbar_init(&sh.v_full[i], kConvertWarps);
-            mbar_init(&sh.v_empty[i], 2);
-        }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(&sh.q_ready[i], 4);
-            mbar_init(&sh.s[i], 1);
-            mbar_init(&sh.p[i], 4);
-            mbar_init(&sh.o[i], 1);
-            mbar_init(&sh.drain[i], 1);
-            mbar_init(&sh.turn[i], 1);
+            mbar_init(&sh.v_empty[i], arrivals_empty);
         }
         for (int i = 0; i < kJobs; ++i) {
             mbar_init(&sh.job_full[i], 1);
-            mbar_init(&sh.job_empty[i], kSoftmaxWarps + 3 + kConvertWarps);
+            mbar_init(&sh.job_empty[i], kSoftmaxWarps + arrivals_empty + 1 + kConvertWarps);  // (the MMA warps, V's)
         }
+        sh.init();
         fence_mbar_init();
     }
     if (warp == kMmaWarp) {
         tmem_alloc(&sh.tmem, kChunkTmem);
         tmem_relinquish();
     }
-    if (warp == kProducerWarp && lane < 2) prefetch_tensormap(lane == 0 ? &kmap : &vmap);
+    if (warp == kKeyWarp && lane < 2) prefetch_tensormap(lane == 0 ? kmap : vmap);
     griddep_wait();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     griddep_launch_dependents();
+    return true;
+}
+
+// What both softmaxes do with a tile's scores.  Weights 2^(f * score - m) of a row's columns [64 h, 64 h + 64), x, times 2^power
+// with `negm` = power - m: in pairs, fp16 as the converted values are, to tensor memory at `to`; their sums.
+template <int FACTORS>
+__device__ __forceinline__ void weigh(const uint32_t (&x)[4][16], const float (&f)[FACTORS], int h, float negm, uint64_t (&sum2)[2], uint32_t to) {
+    const uint64_t negm2 = pack_f32x2(negm, negm);
+#pragma unroll
+    for (int c = 0; c < 4; c += 2) {
+        uint32_t pk[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float factor = f[(h * 4 + c + (e >> 3)) * FACTORS / 8];
+            const uint32_t* y = &x[c + (e >> 3)][2 * (e & 7)];
+            float u, w;
+            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(y[0]), __uint_as_float(y[1])), pack_f32x2(factor, factor), negm2), u, w);
+            u = chunk_exp2(u);
+            w = chunk_exp2(w);
+            sum2[e & 1] = add_f32x2(sum2[e & 1], pack_f32x2(u, w));
+            pk[e] = pack_f16x2(u, w);  // 11 bits
+        }
+        tmem_st16(to + h * 32 + c * 8, pk);
+    }
+}
+// Scores of columns [64 h, 64 h + 64) at `at`, those outside [from, to) struck out unless the whole tile is seen; the maxima
+// of 16 columns each.
+__device__ __forceinline__ void take_scores(uint32_t at, int h, bool full, int from, int to, uint32_t (&x)[4][16], float (&mx)[4]) {
+    if (full) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld16_max(at + h * 64 + c * 16, x[c], mx[c]);
+        tmem_ld_wait();
+    } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld16(at + h * 64 + c * 16, x[c]);
+        tmem_ld_wait();
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            mx[c] = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                if (h * 64 + c * 16 + e < from || h * 64 + c * 16 + e >= to) x[c][e] = 0xff800000u;  // -inf
+                mx[c] = fmaxf(mx[c], __uint_as_float(x[c][e]));
+            }
+        }
+    }
+}
+// The largest of a row's scores times their factors, of the 16 columns' maxima.
+template <int FACTORS>
+__device__ __forceinline__ float top_score(const float (&lower)[4], const float (&upper)[4], const float (&f)[FACTORS]) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+        if constexpr (FACTORS == 2) {
+            if (c % 4 == 0) {
+                const float (&m)[4] = c ? upper : lower;
+                top = fmaxf(top, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * f[c / 4]);
+            }
+        } else {
+            top = fmaxf(top, (c < 4 ? lower[c & 3] : upper[c & 3]) * f[c]);
+        }
+    }
+    return top;
+}
+// The accumulator's columns of a warp's rows times alpha.
+template <int D>
+__device__ __forceinline__ void rescale(uint32_t o_addr, float alpha) {
+#pragma unroll 1
+    for (int c = 0; c < D / 16; ++c) {
+        uint32_t v[16];
+        tmem_ld16(o_addr + c * 16, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * alpha);
+        tmem_st16(o_addr + c * 16, v);
+    }
+}
+
+// Shared memory of chunk_attention_fp8_kernel behind the tiles.
+template <int D>
+struct Shared : Common<D, false> {
+    uint64_t q_ready[2], drain[2], turn[2];
+    uint64_t s[2], p[2], o[2];                       // of a stream: scores, weights, the accumulator
+    int row_ref[2][4];                               // of a split job's streams: what their accumulators are in units of
+    __device__ void init() {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&q_ready[i], 4);
+            mbar_init(&s[i], 1);
+            mbar_init(&p[i], 4);
+            mbar_init(&o[i], 1);
+            mbar_init(&drain[i], 1);
+            mbar_init(&turn[i], 1);
+        }
+    }
+};
+template <int D>
+constexpr int chunk_smem() { return whole_sm(Shape<D, false>::tiles + (int)sizeof(Shared<D>)); }
+static_assert(chunk_smem<128>() <= 227 * 1024 && chunk_smem<64>() <= 227 * 1024, "a block's shared memory");
+
+// FACTORS: scales that a tile of 128 keys may have: 8 with pages of 16, 2 from pages of 64 on.
+template <int D, int FACTORS>
+__global__ void __launch_bounds__(kThreads, 1)
+chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_constant__ CUtensorMap kmap,
+                           const __grid_constant__ CUtensorMap vmap) {
+    using S = Shape<D, false>;
+    constexpr uint32_t kColO = 256;  // O of stream i: columns kColO + i * D
+    const ChunkParams& p = fp.c;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    Shared<D>& sh = *reinterpret_cast<Shared<D>*>(smem + S::tiles);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int G = p.group;
+    if (!begin<D, false>(p, &kmap, &vmap, sh, smem, 2)) return;
     const uint32_t tmem = sh.tmem;
-    // The next job, for a warp that has had `nj` of them; none if there are no more (or a wait was given up: ok is false).
-    // The warp reads what it needs and calls had_job.
-    auto next_job = [&](unsigned nj, bool& ok) -> const Job* {
-        ok = __all_sync(0xffffffffu, mbar_wait(&sh.job_full[nj % kJobs], (nj / kJobs) & 1, kWaitBudget));
-        if (!ok) return nullptr;
-        const Job* g = &sh.job[nj % kJobs];
-        return g->s >= 0 ? g : nullptr;
-    };
-    auto had_job = [&](unsigned& nj) {
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.job_empty[nj % kJobs]);
-        ++nj;
-    };
+    // of a split job's streams, row maxima and sums: where the second query tile is otherwise
+    float2 (*const row)[kTileM] = reinterpret_cast<float2 (*)[kTileM]>(smem + S::q_bytes);
     // whether a job's rows are one stream's: then both take them, and every other key tile
     auto is_split = [&](const Job& g) { return g.t * 2 * p.tokens + p.tokens >= g.B; };
 
@@ -350,12 +667,12 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
         const uint32_t s_addr = lanes + i * 128;  // P comes over the scores
         const int my_tok = r / G;
         const int box_shift = min(7, p.page_shift);
-        unsigned ns = 0, no = 0, x0 = 0;  // scores and accumulators waited for; key tiles of the jobs before
+        unsigned ns = 0, no = 0, batch0 = 0;  // scores and accumulators waited for; batches of the jobs before
         bool failed = false;
         unsigned nj = 0;
         for (;;) {
             bool ok = false;
-            const Job* g = failed ? nullptr : next_job(nj, ok);
+            const Job* g = failed ? nullptr : next_job(sh, nj, ok);
             // (a warp that gave up a wait takes the other stream's of its rows along, here and at a split job's end)
             if (named_barrier_or(1 + quad, 64, !ok)) {
                 failed = true;
@@ -379,9 +696,9 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                 uint32_t top = 0;
                 if (mine == i) top = split_queries<D>(fp.q, at, smem + i * S::q_bytes + quad * 32 * 128);
                 if (split) {  // (the other stream's threads learn of it)
-                    if (i == 0) sh.row[0][r].x = __uint_as_float(top);
+                    if (i == 0) row[0][r].x = __uint_as_float(top);
                     named_barrier(1 + quad, 64);
-                    if (i == 1) top = __float_as_uint(sh.row[0][r].x);
+                    if (i == 1) top = __float_as_uint(row[0][r].x);
                 }
                 // the row times 2^(7 - e) is below 256; 2^(e - 7) of it is put back with the softmax's scale
                 row_scale = p.scale_log2 * __uint_as_float((max(top >> 7, 8u) - 7) << 23);
@@ -394,10 +711,9 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
             }
             const int step = split ? 2 : 1, from_j = split ? a + i : a;  // (a split job's a is its j0)
             int from = lo - from_j * kKeys, to = hi - from_j * kKeys;    // columns that the row sees
-            unsigned xt = x0 + from_j - j0;
             int ref = 0;  // the largest power of two of the stream's values so far, biased (0: none yet)
 #pragma unroll 1
-            for (int j = from_j; j < b; j += step, ++ns, xt += step, from -= step * kKeys, to -= step * kKeys) {
+            for (int j = from_j; j < b; j += step, ++ns, from -= step * kKeys, to -= step * kKeys) {
                 failed = !__all_sync(0xffffffffu, mbar_wait(&sh.s[i], ns & 1, kWaitBudget));
                 if (failed) break;
                 tc_fence_after();
@@ -405,56 +721,26 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                     const bool full = __all_sync(0xffffffffu, from <= 0 && to >= kKeys);
                     // the factors of the scores, of kKeys / FACTORS keys each; finite and above 0, so that a hidden column's
                     // -inf stays one
+                    const unsigned batch = (batch0 + batch_of(j - j0, box_shift)) % kBatches;
                     float f[FACTORS];
 #pragma unroll
                     for (int c = 0; c < FACTORS; ++c)
-                        f[c] = fmaxf(fminf(row_scale * sh.k_power[xt % S::notes][c * (kKeys / FACTORS) >> box_shift], 3.4e38f), 1.2e-38f);
-                    uint32_t x[8][16];
-                    float mx[8];
-                    if (full) {
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) tmem_ld16_max(s_addr + c * 16, x[c], mx[c]);
-                        tmem_ld_wait();
-                    } else {
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) tmem_ld16(s_addr + c * 16, x[c]);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) {
-                            mx[c] = -INFINITY;
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                if (c * 16 + e < from || c * 16 + e >= to) x[c][e] = 0xff800000u;  // -inf
-                                mx[c] = fmaxf(mx[c], __uint_as_float(x[c][e]));
-                            }
-                        }
-                    }
-                    float top = -INFINITY;
-#pragma unroll
-                    for (int c = 0; c < FACTORS; ++c) {
-                        float y = mx[c * (8 / FACTORS)];
-#pragma unroll
-                        for (int e = 1; e < 8 / FACTORS; ++e) y = fmaxf(y, mx[c * (8 / FACTORS) + e]);
-                        top = fmaxf(top, y * f[c]);
-                    }
+                        f[c] = fmaxf(fminf(row_scale * power_of(sh.k_exp[batch][in_batch(j - j0, c * (kKeys / FACTORS) >> box_shift, box_shift)]), 3.4e38f), 1.2e-38f);
+                    uint32_t lower[4][16], upper[4][16];
+                    float mx[2][4];
+                    take_scores(s_addr, 0, full, from, to, lower, mx[0]);
+                    take_scores(s_addr, 1, full, from, to, upper, mx[1]);
+                    const float top = top_score<FACTORS>(mx[0], mx[1], f);
                     // (with this m, 2^(score - m) stays below 2^8)
                     const bool grew = top > m + 8.f;
-                    const int tile_ref = sh.v_ref[xt % S::notes];
+                    const int tile_ref = sh.v_ref[batch][in_batch(j - j0, 0, box_shift)];
                     if (__any_sync(0xffffffffu, grew) || tile_ref > ref) {
                         float alpha = grew ? chunk_exp2(m - top) : 1.f;
                         if (grew) l *= alpha;
                         // (this tile's scores are complete, so the stream's MMAs before them, the last P V among them, are too)
                         if (j > from_j) {
                             if (tile_ref > ref) alpha *= power_of((uint32_t)max(127 + ref - tile_ref, 0));
-#pragma unroll 1
-                            for (int c = 0; c < D / 16; ++c) {
-                                uint32_t v[16];
-                                tmem_ld16(lanes + S::col_o + i * D + c * 16, v);
-                                tmem_ld_wait();
-#pragma unroll
-                                for (int e = 0; e < 16; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * alpha);
-                                tmem_st16(lanes + S::col_o + i * D + c * 16, v);
-                            }
+                            rescale<D>(lanes + kColO + i * D, alpha);
                         }
                         if (grew) m = top;
                         ref = max(ref, tile_ref);
@@ -462,25 +748,9 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                     // weights 2^(f * score - m) times the values' power and 2^7, packed in pairs over the scores; their sum
                     const int power = max(tile_ref - ref + 7, -60);
                     const float negm = (m == -INFINITY ? 0.f : -m) + (float)power;
-                    const uint64_t negm2 = pack_f32x2(negm, negm);
                     uint64_t sum2[2] = {0ull, 0ull};
-#pragma unroll
-                    for (int c = 0; c < 8; c += 2) {
-                        uint32_t pk[16];
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const int h = c + (e >> 3);
-                            const float factor = f[h * FACTORS / 8];
-                            float u, w;
-                            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[h][2 * (e & 7)]), __uint_as_float(x[h][2 * (e & 7) + 1])),
-                                                   pack_f32x2(factor, factor), negm2), u, w);
-                            u = chunk_exp2(u);
-                            w = chunk_exp2(w);
-                            sum2[e & 1] = add_f32x2(sum2[e & 1], pack_f32x2(u, w));
-                            pk[e] = pack_f16x2(u, w);  // fp16, as the converted values are: 11 bits
-                        }
-                        tmem_st16(s_addr + c * 8, pk);
-                    }
+                    weigh<FACTORS>(lower, f, 0, negm, sum2, s_addr);
+                    weigh<FACTORS>(upper, f, 1, negm, sum2, s_addr);
                     float u, w;
                     unpack_f32x2(add_f32x2(sum2[0], sum2[1]), u, w);
                     l = fmaf(u + w, __uint_as_float((uint32_t)(127 - power) << 23), l);
@@ -501,21 +771,21 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                     for (int j = from_j; j < b; j += step)
                         if (sees_nan<D>(fp, *g, j * kKeys, lo, hi)) l = __uint_as_float(0x7fc00000u);
             }
-            x0 += j1 - j0;
+            batch0 += batches_of(max(0, j1 - j0), box_shift);
             if (!split && failed) continue;
             // the weights of the streams' accumulators, which are in units of 2^(ref - 134)
             float w_mine = some ? power_of((uint32_t)(ref - 7)) : 0.f, w_other = 0.f;
             bool others_some = false;
             if (split) {
                 // ---- the other stream's part of these rows, merged as the second kernel merges CTAs' parts
-                sh.row[i][r] = make_float2(m, l);
+                row[i][r] = make_float2(m, l);
                 if (lane == 0) sh.row_ref[i][quad] = some ? ref : 0;
                 if (named_barrier_or(1 + quad, 64, failed)) {
                     failed = true;
                     continue;
                 }
                 others_some = a + (i ^ 1) < b;
-                const float2 o = sh.row[i ^ 1][r];
+                const float2 o = row[i ^ 1][r];
                 const float top = fmaxf(m, o.x);
                 const float u = m == top ? 1.f : chunk_exp2(m - top), v = o.x == top ? 1.f : chunk_exp2(o.x - top);
                 l = i == 0 ? l * u + o.y * v : o.y * v + l * u;
@@ -526,14 +796,14 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
             const bool first = g->first, whole = first && g->last;
             // the query row's number among all, in the output (-1: none)
             const long long orow = active ? (long long)(g->q0 + tok) * p.num_q_heads + g->h * G + r - my_tok * G : -1;
-            had_job(nj);
+            had_job(sh, nj);
             const float inv = whole ? row_inverse(m, l) : 1.f;
             w_mine *= inv;
             w_other *= inv;
             const size_t slot = (size_t)blockIdx.x * 2 + (first ? 1 : 0);
             if (!idle) {
                 // (a split job's two warps have half of the columns each)
-                const uint32_t o_addr = lanes + S::col_o;
+                const uint32_t o_addr = lanes + kColO;
                 write_rows<D>(p, some ? o_addr + i * D : 0, others_some ? o_addr + (i ^ 1) * D : 0, w_mine, w_other,
                               split ? i * (D / 2) : 0, split ? (i + 1) * (D / 2) : D, whole, orow, slot, mine * kTileM + r);
             }
@@ -546,54 +816,8 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
         if (failed && lane == 0) raise_error(p.err, kErrTimeout);
     } else {
         regs_dec<kOtherRegs>();
-        if (warp == kProducerWarp) {
-            // ================= this CTA's part of the line, laid out in jobs; K and V tiles of codes through their rings
-            Place place[2];
-            find_places(p, lane, place);
-            Walk walk{p, place[0], place[1], -1, Seq{}, 0};
-            unsigned nj = 0;
-            bool ok = true;
-            // lays out the next job, or the end of them
-            auto lay_out = [&](Job& g) {
-                if (!walk.next(g)) g.s = -1;
-                const int e = nj % kJobs;
-                if (nj >= kJobs && !__all_sync(0xffffffffu, mbar_wait(&sh.job_empty[e], ((nj / kJobs) - 1) & 1, kWaitBudget))) {
-                    ok = false;
-                    return;
-                }
-                if (lane == 0) {
-                    sh.job[e] = g;
-                    sh.job_nan[e] = 0;
-                    mbar_arrive(&sh.job_full[e]);
-                }
-                ++nj;
-            };
-            unsigned x = 0;  // tiles asked for
-            Job g, after;
-            for (bool have = false; ; have = true) {
-                lay_out(after);  // one ahead of the copies
-                if (!ok) break;
-                if (have && g.j1 > g.j0) {
-                    Boxes box(p, fp.k_scale, g);
-                    for (int j = g.j0; j < g.j1; ++j, ++x) {
-                        const int slot = x % S::k_slots;
-                        ok = x < (unsigned)S::k_slots || __all_sync(0xffffffffu, mbar_wait(&sh.k_empty[slot], (x / S::k_slots - 1) & 1, kWaitBudget));
-                        if (!ok) break;
-                        const int row = box.next(j);
-                        // (a slot is full when lane 0 has said how many bytes it takes)
-                        if (row >= 0) tma_load_3d(smem + S::at_k + slot * S::code_bytes + lane * box.rows * D, &kmap, &sh.k_full[slot], 0, g.h, row);
-                        if (lane < box.of_tile) sh.k_power[x % S::notes][lane] = power_of(box.exponent);
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive_expect_tx(&sh.k_full[slot], box.keys(j) * D);
-                    }
-                }
-                if (!ok || after.s < 0) break;
-                g = after;
-            }
-            if (!ok && lane == 0) raise_error(p.err, kErrTimeout);
-            // no copy may still be in flight when the CTA leaves
-            for (unsigned y = x > (unsigned)S::k_slots ? x - S::k_slots : 0; y < x; ++y)
-                if (!mbar_wait(&sh.k_full[y % S::k_slots], (y / S::k_slots) & 1, kDrainBudget) && lane == 0) raise_error(p.err, kErrTimeout);
+        if (warp == kKeyWarp) {
+            bring_keys<D, false>(fp, &kmap, sh, smem);
         } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
             // ================= MMA issuer of stream i.  The streams take turns, a P V and a Q K^T at a time, each from a
             // warp of its own: one waits for its operands and commits while the other's MMAs are issued
@@ -607,7 +831,7 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
             const uint32_t q_lo = (uint32_t)smem_desc(smem_addr(smem), 16, 0, 0);
             const uint32_t k_lo = (uint32_t)smem_desc(smem_addr(smem + S::at_k), 16, 0, 0);
             const uint32_t v_lo = (uint32_t)smem_desc(smem_addr(smem + S::at_v), kHalfBytes, 0, 0);
-            const uint32_t t_s = tmem + i * 128, t_o = tmem + S::col_o + i * D;
+            const uint32_t t_s = tmem + i * 128, t_o = tmem + kColO + i * D;
             // this stream's arrivals on `bar`: when its MMAs so far are done, or at once if it had none there; a split job's
             // tiles are one stream's, which arrives for the other one too
             auto release = [&](uint64_t* bar, bool used, bool both) {
@@ -617,11 +841,11 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
             unsigned x = 0;  // key tiles of the jobs before
             unsigned nj = 0, np = 0, turn = 0, nq0 = 0, nq1 = 0;
             bool ok, fine = true, any = false;
-            while (const Job* g = next_job(nj, ok)) {
+            while (const Job* g = next_job(sh, nj, ok)) {
                 const bool split = is_split(*g);
                 const int mine = split ? 0 : i;
                 const int a = g->a[mine], b = g->b[mine], j0 = g->j0, j1 = g->j1;
-                had_job(nj);
+                had_job(sh, nj);
                 if (j1 <= j0) continue;
                 const int step = split ? 2 : 1, f = split ? j0 + i : j0;
                 const int turns = (split ? (j1 - j0 + 1) / 2 : j1 - j0) + 1;
@@ -687,118 +911,10 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                 if (!mbar_wait(&sh.drain[i], 0, kDrainBudget)) raise_error(p.err, kErrTimeout);
             }
             __syncwarp();
-        } else if (warp >= kConvertWarp) {
-            // ================= V from codes to fp16: keys [32 w, 32 w + 32) of every tile
-            // Eight lanes read all banks, and write them: a key's lower pieces of 16 codes with the next key's upper ones (form
-            // 0; 1: the other way round; of 64 columns: the two keys' pieces all together).  From one piece of a lane to the
-            // next of its form it is 8 keys, which the swizzle does not tell apart.
-            constexpr int kForms = D == 128 ? 2 : 1, kPieces = 2 * kForms;  // pieces of 16 keys
-            const int w = warp - kConvertWarp, e = lane & 7;
-            const int key0 = w * 32 + (lane >> 3) * 2 + (e >> 2);
-            int from[kForms], to[kForms];
-#pragma unroll
-            for (int form = 0; form < kForms; ++form) {
-                const int piece = (e & 3) + (D == 128 ? 4 * ((e >> 2) ^ form) : 0);
-                from[form] = key0 * D + piece * 16;
-                to[form] = (piece >> 2) * kHalfBytes + key0 * 128 + (((2 * (piece & 3)) ^ (key0 & 7)) << 4);
-            }
-            const int box_shift = min(7, p.page_shift);
-            unsigned x = 0, nj = 0;
-            bool ok, fine = true;
-            while (const Job* g = next_job(nj, ok)) {
-                const int j0 = g->j0, j1 = g->j1, n = g->n;
-                int* const nan = &sh.job_nan[nj % kJobs];
-                had_job(nj);
-                for (int j = j0; j < j1; ++j, ++x) {
-                    const int rs = x % S::raw_slots, vs = x % S::v_slots;
-                    fine = mbar_wait(&sh.raw_full[rs], (x / S::raw_slots) & 1, kWaitBudget);
-                    if (fine && x >= (unsigned)S::v_slots) fine = mbar_wait(&sh.v_empty[vs], (x / S::v_slots - 1) & 1, kWaitBudget);
-                    fine = __all_sync(0xffffffffu, fine);
-                    if (!fine) break;
-                    const uint8_t* raw = smem + S::at_raw + rs * S::code_bytes;
-                    uint8_t* out = smem + S::at_v + vs * S::v_bytes;
-                    const int left = n - j * kKeys;  // keys from this one on are none: zeros
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {  // 16 keys at a time: boxes are no smaller
-                        uint32_t v[kPieces][4];
-#pragma unroll
-                        for (int k = 0; k < kPieces; ++k) {
-                            const uint4 c = *reinterpret_cast<const uint4*>(raw + from[k % kForms] + (h * kPieces + k) / kForms * 8 * D);
-                            v[k][0] = c.x; v[k][1] = c.y; v[k][2] = c.z; v[k][3] = c.w;
-                        }
-                        if (left < kKeys) {
-#pragma unroll
-                            for (int k = 0; k < kPieces; ++k)
-                                if (key0 + (h * kPieces + k) / kForms * 8 >= left) v[k][0] = v[k][1] = v[k][2] = v[k][3] = 0;
-                        }
-                        uint32_t found = 0;  // bit 7 of a byte: a code is 0x7f or 0xff
-#pragma unroll
-                        for (int k = 0; k < kPieces; ++k)
-#pragma unroll
-                            for (int c = 0; c < 4; ++c) found |= (v[k][c] & 0x7f7f7f7fu) + 0x01010101u;
-                        if (__any_sync(0xffffffffu, found & 0x80808080u)) {
-                            *nan = 1;  // (the softmax warps look once all of the job's values have been used)
-#pragma unroll
-                            for (int k = 0; k < kPieces; ++k)
-#pragma unroll
-                                for (int c = 0; c < 4; ++c) {
-                                    const uint32_t at = ((v[k][c] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-                                    v[k][c] &= ~((at >> 7) * 255u);
-                                }
-                        }
-                        const int below = sh.v_below[rs][(w * 32 + h * 16) >> box_shift];
-                        const uint32_t mul = (below < 15 ? (15 - below) << 10 : below < 25 ? 1 << (24 - below) : 0) * 0x10001u;
-#pragma unroll
-                        for (int k = 0; k < kPieces; ++k) {
-                            uint32_t y[8];
-#pragma unroll
-                            for (int c = 0; c < 8; ++c) y[c] = mul_f16x2(e4m3x2_to_f16x2(c & 1 ? v[k][c >> 1] >> 16 : v[k][c >> 1]), mul);
-                            uint8_t* const at = out + (h * kPieces + k) / kForms * 1024;
-                            *reinterpret_cast<uint4*>(at + to[k % kForms]) = make_uint4(y[0], y[1], y[2], y[3]);
-                            *reinterpret_cast<uint4*>(at + (to[k % kForms] ^ 16)) = make_uint4(y[4], y[5], y[6], y[7]);
-                        }
-                    }
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) {
-                        mbar_arrive(&sh.v_full[vs]);
-                        mbar_arrive(&sh.raw_empty[rs]);
-                    }
-                }
-                if (!fine) break;
-            }
-            if ((!fine || !ok) && lane == 0) raise_error(p.err, kErrTimeout);
+        } else if (warp == kValueWarp) {
+            bring_values<D, false>(fp, &vmap, sh, smem);
         } else {
-            // ================= V tiles of codes through their ring; what this CTA leaves to the merge
-            unsigned x = 0, nj = 0;
-            int4 left = make_int4(0, 0, 0, 0);
-            bool ok, fine = true;
-            while (const Job* job = next_job(nj, ok)) {
-                const Job g = *job;
-                had_job(nj);
-                if (!g.first) left.x |= kHasHead | (g.last ? kHeadEnds : 0);
-                if (g.first && !g.last)
-                    left = make_int4(left.x | kHasTail, g.q0 + g.t * 2 * p.tokens, min(2 * p.tokens, g.B - g.t * 2 * p.tokens), g.h);
-                if (g.j1 <= g.j0) continue;
-                Boxes box(p, fp.v_scale, g);
-                for (int j = g.j0; j < g.j1; ++j, ++x) {
-                    const int slot = x % S::raw_slots;
-                    fine = x < (unsigned)S::raw_slots || __all_sync(0xffffffffu, mbar_wait(&sh.raw_empty[slot], (x / S::raw_slots - 1) & 1, kWaitBudget));
-                    if (!fine) break;
-                    const int row = box.next(j);
-                    if (row >= 0) tma_load_3d(smem + S::at_raw + slot * S::code_bytes + lane * box.rows * D, &vmap, &sh.raw_full[slot], 0, g.h, row);
-                    const uint32_t ref = max(__reduce_max_sync(0xffffffffu, row >= 0 ? box.exponent : 0u), kLeastRef);
-                    if (lane < box.of_tile) sh.v_below[slot][lane] = (uint8_t)(row >= 0 ? ref - box.exponent : 0u);
-                    if (lane == 0) sh.v_ref[x % S::notes] = (int)ref;
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_expect_tx(&sh.raw_full[slot], box.keys(j) * D);
-                }
-                if (!fine) break;
-            }
-            if ((!ok || !fine) && lane == 0) raise_error(p.err, kErrTimeout);
-            for (unsigned y = x > (unsigned)S::raw_slots ? x - S::raw_slots : 0; y < x; ++y)
-                if (!mbar_wait(&sh.raw_full[y % S::raw_slots], (y / S::raw_slots) & 1, kDrainBudget) && lane == 0) raise_error(p.err, kErrTimeout);
-            if (lane == 0) p.info[blockIdx.x] = left;
+            convert_values<D, false>(p, sh, smem, warp - kConvertWarp);
         }
     }
     tc_fence_before();
@@ -807,6 +923,322 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
         tc_fence_after();
         tmem_dealloc(tmem, kChunkTmem);
     }
+}
+
+// Shared memory of block_attention_fp8_kernel behind the tiles.
+template <int D>
+struct BlockShared : Common<D, true> {
+    uint64_t q_ready, drain, o;
+    uint64_t s[3], p[3];                             // of a score buffer: scores, weights
+    uint64_t decided[4][2];                          // of 32 rows, by the tile's parity: what follows is as after it
+    float top[kTileM];                               // of a row: its maximum so far
+    int ref[4];                                      // the values' power so far (the same in all of them)
+    float row[2][kTileM];                            // of the two groups of warps: at the end row sums
+    __device__ void init() {
+        mbar_init(&q_ready, 4);
+        mbar_init(&drain, 1);
+        mbar_init(&o, 1);
+        for (int i = 0; i < 3; ++i) {
+            mbar_init(&s[i], 1);
+            mbar_init(&p[i], 4);
+        }
+        for (int i = 0; i < 8; ++i) mbar_init(&decided[i >> 1][i & 1], 1);
+    }
+};
+template <int D>
+constexpr int block_smem() { return whole_sm(Shape<D, true>::tiles + (int)sizeof(BlockShared<D>)); }
+static_assert(block_smem<128>() <= 227 * 1024 && block_smem<64>() <= 227 * 1024, "a block's shared memory");
+
+// The same where every work tile has the rows of one stream: blocks and single tokens, whose keys' bytes are what counts.  One
+// accumulator; scores in three buffers, so that a tile's are there before the softmax has done with the two before it.  The
+// softmax's two groups of warps take the tiles in turn, each row's maximum handed from one tile's thread to the next one's
+// (rarely another: it is moved only where a score has outgrown it by 2^8, and the accumulator with it).
+template <int D, int FACTORS>
+__global__ void __launch_bounds__(kThreads, 1)
+block_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_constant__ CUtensorMap kmap,
+                           const __grid_constant__ CUtensorMap vmap) {
+    using S = Shape<D, true>;
+    constexpr uint32_t kColO = 384;  // behind the score buffers
+    const ChunkParams& p = fp.c;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    BlockShared<D>& sh = *reinterpret_cast<BlockShared<D>*>(smem + S::tiles);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int G = p.group;
+    if (!begin<D, true>(p, &kmap, &vmap, sh, smem, 1)) return;
+    const uint32_t tmem = sh.tmem;
+
+    if (warp < kSoftmaxWarps) {
+        regs_inc<kSoftmaxRegs>();
+        // ================= softmax of the tiles of parity i: a thread a row
+        const int i = warp >> 2, quad = warp & 3, r = quad * 32 + lane;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+        const int my_tok = r / G;
+        const int box_shift = min(7, p.page_shift);
+        unsigned x0 = 0, no = 0, batch0 = 0;  // key tiles of the jobs before; accumulators waited for; batches before
+        unsigned nd[2] = {0, 0};              // decisions of either group before
+        bool failed = false;
+        unsigned nj = 0;
+        for (;;) {
+            bool ok = false;
+            const Job* g = failed ? nullptr : next_job(sh, nj, ok);
+            // (a warp that gave up a wait takes the other group's of its rows along, here and at a job's end)
+            if (named_barrier_or(1 + quad, 64, !ok)) {
+                failed = true;
+                break;
+            }
+            if (!g) break;
+            const int j0 = g->j0, tiles = max(0, g->j1 - j0);
+            const int tok = g->t * 2 * p.tokens + my_tok;
+            const bool active = my_tok < p.tokens && tok < g->B;
+            const int pos = g->n - g->B + tok;  // (what the end needs of the job is read again there)
+            // (rows of none count as seeing all: their warps' tiles are not masked for their sake)
+            const int hi = !active ? 0x7fffffff : p.causal ? max(0, pos + 1) : g->n;
+            const int lo = active && p.window > 0 ? max(0, pos + 1 - p.window) : 0;
+            const bool idle = !__any_sync(0xffffffffu, active);  // the same in both warps of these rows
+            float m = -INFINITY, l = 0.f, row_scale = 1.f;
+            if (tiles > 0) {
+                if (!idle) {
+                    // ---- the queries of these rows, two parts each, to shared memory; the other group learns of their size
+                    uint32_t top = 0;
+                    if (i == 0) {
+                        const int64_t at = active ? (int64_t)(g->q0 + tok) * fp.q_stride + (g->h * G + r - my_tok * G) * D : -1;
+                        top = split_queries<D>(fp.q, at, smem + quad * 32 * 128);
+                        sh.row[0][r] = __uint_as_float(top);
+                    }
+                    named_barrier(1 + quad, 64);
+                    if (i == 1) top = __float_as_uint(sh.row[0][r]);
+                    // the row times 2^(7 - e) is below 256; 2^(e - 7) of it is put back with the softmax's scale
+                    row_scale = p.scale_log2 * __uint_as_float((max(top >> 7, 8u) - 7) << 23);
+                    if (top >= 0x7f80u && hi > lo) l = __uint_as_float(0x7fc00000u);  // a NaN or an infinity: the row is none
+                }
+                if (i == 0) {
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.q_ready);
+                }
+            }
+            int from = lo - (j0 + i) * kKeys, to = hi - (j0 + i) * kKeys;  // columns that the row sees
+            int ref = 0;  // the largest power of two of the values so far, biased (0: none yet)
+#pragma unroll 1
+            for (int t = i; t < tiles; t += 2, from -= 2 * kKeys, to -= 2 * kKeys) {
+                const unsigned x = x0 + t;
+                const uint32_t s_addr = lanes + x % 3 * 128;  // P comes over the scores
+                failed = !__all_sync(0xffffffffu, mbar_wait(&sh.s[x % 3], (x / 3) & 1, kWaitBudget));
+                if (failed) break;
+                tc_fence_after();
+                if (!idle) {
+                    const bool full = __all_sync(0xffffffffu, from <= 0 && to >= kKeys);
+                    // the factors of the scores, of kKeys / FACTORS keys each; finite and above 0, so that a hidden column's
+                    // -inf stays one
+                    const unsigned batch = (batch0 + batch_of(t, box_shift)) % kBatches;
+                    float f[FACTORS];
+#pragma unroll
+                    for (int c = 0; c < FACTORS; ++c)
+                        f[c] = fmaxf(fminf(row_scale * power_of(sh.k_exp[batch][in_batch(t, c * (kKeys / FACTORS) >> box_shift, box_shift)]), 3.4e38f), 1.2e-38f);
+                    uint32_t lower[4][16], upper[4][16];
+                    float mx[2][4];
+                    take_scores(s_addr, 0, full, from, to, lower, mx[0]);
+                    take_scores(s_addr, 1, full, from, to, upper, mx[1]);
+                    const float top = top_score<FACTORS>(mx[0], mx[1], f);
+                    const int tile_ref = sh.v_ref[batch][in_batch(t, 0, box_shift)];
+                    // ---- (m, ref) as the tile before left them
+                    float m_old = -INFINITY;
+                    int ref_old = 0;
+                    if (t > 0) {
+                        failed = !__all_sync(0xffffffffu, mbar_wait(&sh.decided[quad][i ^ 1], (nd[i ^ 1] + ((t - 1) >> 1)) & 1, kWaitBudget));
+                        if (failed) break;
+                        m_old = sh.top[r];
+                        ref_old = sh.ref[quad];
+                        __syncwarp();
+                    }
+                    // (with this m, 2^(score - m) stays below 2^8)
+                    const bool grew = top > m_old + 8.f;
+                    const float m_new = grew ? top : m_old;
+                    ref = max(ref_old, tile_ref);
+                    const bool moves = t > 0 && __any_sync(0xffffffffu, (grew && m_old != -INFINITY) || ref > ref_old);
+                    if (t == 0 || grew) sh.top[r] = m_new;
+                    if (lane == 0 && (t == 0 || ref > ref_old)) sh.ref[quad] = ref;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.decided[quad][i]);
+                    if (moves) {  // the accumulator with them, once the tile before is in it
+                        failed = !__all_sync(0xffffffffu, mbar_wait(&sh.v_empty[(x - 1) % S::v_slots], ((x - 1) / S::v_slots) & 1, kWaitBudget));
+                        if (failed) break;
+                        tc_fence_after();
+                        rescale<D>(lanes + kColO, (grew ? chunk_exp2(m_old - m_new) : 1.f) * power_of((uint32_t)max(127 + ref_old - ref, 0)));
+                    }
+                    if (m != m_new) {
+                        l *= chunk_exp2(m - m_new);
+                        m = m_new;
+                    }
+                    // weights 2^(f * score - m) times the values' power and 2^7, over the scores; their sum
+                    const int power = max(tile_ref - ref + 7, -60);
+                    const float negm = (m == -INFINITY ? 0.f : -m) + (float)power;
+                    uint64_t sum2[2] = {0ull, 0ull};
+                    weigh<FACTORS>(lower, f, 0, negm, sum2, s_addr);
+                    weigh<FACTORS>(upper, f, 1, negm, sum2, s_addr);
+                    float u, w;
+                    unpack_f32x2(add_f32x2(sum2[0], sum2[1]), u, w);
+                    l = fmaf(u + w, __uint_as_float((uint32_t)(127 - power) << 23), l);
+                    tmem_st_wait();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.p[x % 3]);
+            }
+            if (!failed && tiles > 0) {
+                failed = !__all_sync(0xffffffffu, mbar_wait(&sh.o, no & 1, kWaitBudget));
+                ++no;
+                tc_fence_after();
+                // A value that is none, in a key that the row sees, makes the row none (the tiles' weights of it are 0, and its
+                // values too).  Rare: the codes are read again to find which keys have one.
+                if (*const_cast<volatile int*>(&sh.job_nan[nj % kJobs]) && !idle)
+                    for (int t = i; t < tiles; t += 2)
+                        if (sees_nan<D>(fp, *g, (j0 + t) * kKeys, lo, hi)) l = __uint_as_float(0x7fc00000u);
+            }
+            x0 += tiles;
+            batch0 += batches_of(tiles, box_shift);
+            if (!idle) {  // (idle warps decide nothing)
+                nd[0] += (tiles + 1) >> 1;
+                nd[1] += tiles >> 1;
+            }
+            // ---- the sums of both groups' tiles, for the last tile's maximum; the accumulator is in units of 2^(ref - 134)
+            if (tiles > 0 && !idle) {
+                const float top = sh.top[r];
+                if (m != top) l *= chunk_exp2(m - top);
+                m = top;
+                ref = sh.ref[quad];
+            }
+            sh.row[i][r] = l;
+            if (named_barrier_or(1 + quad, 64, failed)) {
+                failed = true;
+                continue;
+            }
+            l = sh.row[0][r] + sh.row[1][r];
+            const bool first = g->first, whole = first && g->last;
+            // the query row's number among all, in the output (-1: none)
+            const long long orow = active ? (long long)(g->q0 + tok) * p.num_q_heads + g->h * G + r - my_tok * G : -1;
+            had_job(sh, nj);
+            const float weight = (tiles > 0 ? power_of((uint32_t)(ref - 7)) : 0.f) * (whole ? row_inverse(m, l) : 1.f);
+            const size_t slot = (size_t)blockIdx.x * 2 + (first ? 1 : 0);
+            if (!idle)  // (each group has half of the columns)
+                write_rows<D>(p, tiles > 0 ? lanes + kColO : 0, 0, weight, 0.f, i * (D / 2), (i + 1) * (D / 2), whole, orow, slot, r);
+            if (active && i == 0) {
+                if (!whole) p.part_ml[slot * (2 * kTileM) + r] = make_float2(m, l);
+                else if (p.lse) p.lse[orow] = row_lse(m, l);
+            }
+            tc_fence_before();
+        }
+        if (failed && lane == 0) raise_error(p.err, kErrTimeout);
+    } else {
+        regs_dec<kOtherRegs>();
+        if (warp == kKeyWarp) {
+            bring_keys<D, true>(fp, &kmap, sh, smem);
+        } else if (warp == kMmaWarp) {
+            // ================= MMA issuer: a tile's P V, then Q K^T of the tile that has its score buffer next
+            const uint32_t id_s = idesc_e4m3_f32(kTileM, kKeys);
+            const uint32_t id_o = idesc_f16_f32(kTileM, D, false, true);
+            // descriptors of the query tile, of the rings' first slots as K and as V: their upper halves are constant, an
+            // offset adds its 16-byte units to the lower ones
+            const uint64_t upper = smem_desc(0, 0, 1024, kSwizzle128B);
+            const uint64_t k_upper = D == 128 ? upper : smem_desc(0, 0, 512, kSwizzle64B);
+            const uint32_t q_lo = (uint32_t)smem_desc(smem_addr(smem), 16, 0, 0);
+            const uint32_t k_lo = (uint32_t)smem_desc(smem_addr(smem + S::at_k), 16, 0, 0);
+            const uint32_t v_lo = (uint32_t)smem_desc(smem_addr(smem + S::at_v), kHalfBytes, 0, 0);
+            unsigned x0 = 0, nj = 0, nq = 0;  // key tiles of the jobs before; jobs; those with queries
+            bool ok, fine = true;
+            while (const Job* g = next_job(sh, nj, ok)) {
+                const int tiles = max(0, g->j1 - g->j0);
+                had_job(sh, nj);
+                if (tiles == 0) continue;
+                if (elect_one()) {  // one thread throughout: its waits need no votes
+                    fine = mbar_wait(&sh.q_ready, nq & 1, kWaitBudget);
+                    for (int t = -3; t < tiles && fine; ++t) {  // P V of tile t, Q K^T of tile t + 3
+                        if (t >= 0) {
+                            const unsigned x = x0 + t;
+                            const int slot = x % S::v_slots;
+                            fine = mbar_wait(&sh.v_full[slot], (x / S::v_slots) & 1, kWaitBudget) &&
+                                   mbar_wait(&sh.p[x % 3], (x / 3) & 1, kWaitBudget);
+                            if (!fine) break;
+                            tc_fence_after();
+                            const uint32_t vl = v_lo + slot * (S::v_bytes >> 4), t_p = tmem + x % 3 * 128;
+                            uint32_t on = t > 0 ? 1u : 0u;
+#pragma unroll
+                            for (int kk = 0; kk < kKeys / 16; ++kk) {
+                                umma_ts(tmem + kColO, t_p + kk * 8, upper | (vl + kk * (2048 >> 4)), id_o, on);
+                                on = 1;
+                            }
+                            umma_commit(&sh.v_empty[slot]);
+                            if (t == tiles - 1) umma_commit(&sh.o);
+                        }
+                        if (t + 3 < tiles) {
+                            const unsigned x = x0 + t + 3;
+                            const int slot = x % S::k_slots;
+                            fine = mbar_wait(&sh.k_full[slot], (x / S::k_slots) & 1, kWaitBudget);
+                            if (!fine) break;
+                            tc_fence_after();
+                            // both parts of Q, 32 columns at a time
+                            const uint32_t kl = k_lo + slot * (S::code_bytes >> 4), t_s = tmem + x % 3 * 128;
+                            uint32_t on = 0;
+#pragma unroll
+                            for (int kk = 0; kk < D / 16; ++kk) {
+                                const int part = kk / (D / 32), c = kk % (D / 32);
+                                const uint32_t off = ((D == 128 ? part * kHalfBytes : part * 64) + c * 32) >> 4;
+                                umma_ss_f8(t_s, upper | (q_lo + off), k_upper | (kl + c * 2), id_s, on);
+                                on = 1;
+                            }
+                            umma_commit(&sh.s[x % 3]);
+                            umma_commit(&sh.k_empty[slot]);
+                        }
+                    }
+                }
+                x0 += tiles;
+                ++nq;
+                fine = __all_sync(0xffffffffu, fine);
+                if (!fine) break;
+            }
+            if ((!fine || !ok) && lane == 0) raise_error(p.err, kErrTimeout);
+            if (nq > 0 && elect_one()) {
+                umma_commit(&sh.drain);
+                if (!mbar_wait(&sh.drain, 0, kDrainBudget)) raise_error(p.err, kErrTimeout);
+            }
+            __syncwarp();
+        } else if (warp == kValueWarp) {
+            bring_values<D, true>(fp, &vmap, sh, smem);
+        } else if (warp >= kConvertWarp) {
+            convert_values<D, true>(p, sh, smem, warp - kConvertWarp);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        tc_fence_after();
+        tmem_dealloc(tmem, kChunkTmem);
+    }
+}
+
+template <typename Kernel>
+int launch(Kernel kernel, bool (&configured)[64], int threads, int smem, const Fp8Params& p, const CUtensorMap& kmap,
+           const CUtensorMap& vmap, int grid, int device, cudaStream_t stream) {
+    static std::mutex mu;
+    if (device < 0 || device >= 64) return BP_ERR_UNSUPPORTED;
+    {
+        std::lock_guard<std::mutex> lock(mu);
+        if (!configured[device]) {
+            if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return BP_ERR_CUDA;
+            configured[device] = true;
+        }
+    }
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3((unsigned)grid, 1, 1);
+    cfg.blockDim = dim3((unsigned)threads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, p, kmap, vmap) == cudaSuccess ? BP_OK : BP_ERR_CUDA;
 }
 
 template <int D, int FACTORS>
@@ -833,28 +1265,12 @@ int run(const ChunkAttentionFp8Args& a, const DeviceInfo& dev, cudaStream_t stre
                            CU_TENSOR_MAP_SWIZZLE_NONE, promotion);
     if (rc != BP_OK) return rc;
 
-    static std::mutex mu;
-    static bool configured[64] = {};
-    if (dev.device < 0 || dev.device >= 64) return BP_ERR_UNSUPPORTED;
-    {
-        std::lock_guard<std::mutex> lock(mu);
-        if (!configured[dev.device]) {
-            if (cudaFuncSetAttribute(chunk_attention_fp8_kernel<D, FACTORS>, cudaFuncAttributeMaxDynamicSharedMemorySize, fp8_smem<D>()) != cudaSuccess)
-                return BP_ERR_CUDA;
-            configured[dev.device] = true;
-        }
-    }
-    cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3((unsigned)grid, 1, 1);
-    cfg.blockDim = dim3(kFp8Threads, 1, 1);
-    cfg.dynamicSmemBytes = fp8_smem<D>();
-    cfg.stream = stream;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, chunk_attention_fp8_kernel<D, FACTORS>, p, kmap, vmap) != cudaSuccess) return BP_ERR_CUDA;
+    static bool chunk_configured[64] = {}, block_configured[64] = {};
+    if (a.max_q_len <= p.c.tokens)  // one stream's rows have any sequence's new tokens
+        rc = launch(block_attention_fp8_kernel<D, FACTORS>, block_configured, kThreads, block_smem<D>(), p, kmap, vmap, grid, dev.device, stream);
+    else
+        rc = launch(chunk_attention_fp8_kernel<D, FACTORS>, chunk_configured, kThreads, chunk_smem<D>(), p, kmap, vmap, grid, dev.device, stream);
+    if (rc != BP_OK) return rc;
     if (a.max_kv_len <= (2 * kLeastCut - 1) * kKeys) return BP_OK;  // too short to be cut: nothing to merge
     return launch_chunk_merge(p.c, D, grid, a.max_q_len, stream);
 }

@@ -1,6 +1,7 @@
 // How the work of a chunk attention is laid out: what chunk_attention.cu (a bf16 cache) and chunk_attention_fp8.cu (a cache
 // in 8 bits) share.  The work tiles of all sequences and heads lie on one line, measured in keys; every CTA takes an equal
 // stretch of it, and what a cut leaves in parts is merged by a second kernel (chunk_merge_kernel, in chunk_attention.cu).
+// Whoever includes this has defined bp::kTileCost, a work tile's fixed cost (queries in, output out) in keys.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -13,9 +14,6 @@ namespace bp {
 constexpr int kTileM = 128;                      // rows of one stream's query tile
 constexpr int kKeys = 128;                       // keys per K/V tile
 
-// A work tile's fixed cost (queries in, output out), in keys: a prompt of 8192 takes 399 us with 192, 372 with 320, 368
-// with 448, 374 with 640.  Heads of 64 and tiles of one stream take the same number; it was not fitted to them.
-constexpr int kTileCost = 400;
 constexpr int kLeastCost = 2 * kKeys;            // of a CTA's stretch: below it, fewer CTAs take part
 constexpr int kLeastCut = 2;                     // key tiles on either side of a cut
 

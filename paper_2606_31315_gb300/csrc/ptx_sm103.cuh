@@ -358,16 +358,23 @@ __device__ __forceinline__ void unpack_e4m3x2(uint32_t v, float& lo, float& hi) 
         : "=f"(lo), "=f"(hi)
         : "h"(static_cast<uint16_t>(v)));
 }
-// Two e4m3 numbers, in the lower 16 bits, as fp16 ones (exact).
-__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t v) {
-    uint32_t r;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(static_cast<uint16_t>(v)));
-    return r;
+// Four e4m3 numbers as fp16 ones (exact; of 0x7f and 0xff 0x7fff and 0xffff).
+__device__ __forceinline__ void e4m3x4_to_f16x4(uint32_t v, uint32_t& lo, uint32_t& hi) {
+    asm("{\n\t.reg .b16 x, y;\n\t"
+        "mov.b32 {x, y}, %2;\n\t"
+        "cvt.rn.f16x2.e4m3x2 %0, x;\n\t"
+        "cvt.rn.f16x2.e4m3x2 %1, y;\n\t}"
+        : "=r"(lo), "=r"(hi)
+        : "r"(v));
 }
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
+}
+// Two fp16 numbers with 0 in the place of what is none.
+__device__ __forceinline__ uint32_t drop_nan_f16x2(uint32_t a) {
+    return ((a & 0x7fffu) > 0x7c00u ? 0u : a & 0xffffu) | ((a >> 16 & 0x7fffu) > 0x7c00u ? 0u : a & 0xffff0000u);
 }
 __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
     uint32_t r;
