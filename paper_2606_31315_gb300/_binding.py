@@ -542,8 +542,12 @@ def pages_update(block_table, old_lens, new_lens, free_pages, num_free, page_siz
     the device; the table, the list and its length are updated in place.  total_new: how many new tokens positions (int32) and
     slots (int64) have room for; None: neither is wanted.  Returns (positions, slots, cu_new, cu_kv, missing)."""
     lib = load()
-    _int32("block_table old_lens new_lens free_pages num_free positions cu_new cu_kv missing", block_table, old_lens, new_lens,
-           free_pages, num_free, positions, cu_new, cu_kv, missing)
+    i32 = torch.int32  # (written out: a helper's loop over these took 1.5 us of a call's 10)
+    if not (block_table.dtype is i32 and old_lens.dtype is i32 and new_lens.dtype is i32 and free_pages.dtype is i32 and
+            num_free.dtype is i32 and block_table.is_cuda and old_lens.is_cuda and new_lens.is_cuda and free_pages.is_cuda and
+            num_free.is_cuda and block_table.is_contiguous() and old_lens.is_contiguous() and new_lens.is_contiguous() and
+            free_pages.is_contiguous()):
+        _int32("block_table old_lens new_lens free_pages num_free", block_table, old_lens, new_lens, free_pages, num_free)
     s, per = block_table.shape
     dev = block_table.device
     if old_lens.numel() != s or new_lens.numel() != s or num_free.numel() != 1:
@@ -555,23 +559,27 @@ def pages_update(block_table, old_lens, new_lens, free_pages, num_free, page_siz
         total_new = 0
     else:
         if positions is None:
-            positions = _empty(total_new, torch.int32, dev, stream)
+            positions = _empty(total_new, i32, dev, stream)
+        elif positions.dtype is not i32 or positions.numel() != total_new or not (positions.is_cuda and positions.is_contiguous()):
+            raise ValueError("positions must be a contiguous int32 CUDA tensor of total_new entries")
         if slots is None:
             slots = _empty(total_new, torch.int64, dev, stream)
-        elif slots.dtype is not torch.int64 or not (slots.is_cuda and slots.is_contiguous()):
-            raise ValueError("slots must be a contiguous int64 CUDA tensor")
-        if positions.numel() != total_new or slots.numel() != total_new:
-            raise ValueError("positions and slots must hold total_new entries")
+        elif slots.dtype is not torch.int64 or slots.numel() != total_new or not (slots.is_cuda and slots.is_contiguous()):
+            raise ValueError("slots must be a contiguous int64 CUDA tensor of total_new entries")
         if total_new:  # (an empty tensor has no address)
             pp, sp = positions.data_ptr(), slots.data_ptr()
     if cu_new is None:
-        cu_new = _empty(s + 1, torch.int32, dev, stream)
+        cu_new = _empty(s + 1, i32, dev, stream)
+    elif cu_new.dtype is not i32 or cu_new.numel() != s + 1 or not (cu_new.is_cuda and cu_new.is_contiguous()):
+        raise ValueError("cu_new must be a contiguous int32 CUDA tensor with one more entry than block_table has rows")
     if cu_kv is None:
-        cu_kv = _empty(s + 1, torch.int32, dev, stream)
+        cu_kv = _empty(s + 1, i32, dev, stream)
+    elif cu_kv.dtype is not i32 or cu_kv.numel() != s + 1 or not (cu_kv.is_cuda and cu_kv.is_contiguous()):
+        raise ValueError("cu_kv must be a contiguous int32 CUDA tensor with one more entry than block_table has rows")
     if missing is None:
-        missing = _empty(1, torch.int32, dev, stream)
-    if cu_new.numel() != s + 1 or cu_kv.numel() != s + 1 or missing.numel() != 1:
-        raise ValueError("cu_new and cu_kv must hold one more entry than block_table has rows, missing one")
+        missing = _empty(1, i32, dev, stream)
+    elif missing.dtype is not i32 or missing.numel() != 1 or not missing.is_cuda:
+        raise ValueError("missing must be an int32 CUDA tensor of one entry")
     if ws is None:
         ws = workspace(256, dev, stream)
     rc = lib.bp_pages_update(block_table.data_ptr(), old_lens.data_ptr(), new_lens.data_ptr(), free_pages.data_ptr(),

@@ -13,7 +13,7 @@
 // A page's new rows are a unit, which has one owner: nothing is summed or ordered by atomics.  A block has a few tokens of
 // one head of K or V; its threads look which of them begin a unit (a sequence's first new token, or a page's first row), then
 // units of many rows are the whole block's, others a warp's.  A thread keeps its rows' pieces in registers between the
-// maximum and the rounding, four of 16 elements; what is more (pages above 64 rows of 128) is read again, from L2.
+// maximum and the rounding, four of 16 elements (two of fp32); what is more (pages above 64 rows of 128) is read again, from L2.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -27,14 +27,16 @@ namespace {
 constexpr int kAppendThreads = 128;
 constexpr int kAppendTokens = 64;  // of a block, at most
 constexpr int kWarpRows = 8;       // a unit of up to so many rows is a warp's
-constexpr int kKept = 4;           // pieces that a thread keeps
+template <typename T>
+constexpr int kKept = sizeof(T) == 2 ? 4 : 2;  // pieces that a thread keeps
 
 struct AppendParams {
     KvAppendFp8Args a;
     int page_shift, tokens;  // tokens of a block
+    unsigned piece_inverse;  // 2^32 / (pieces of a row), rounded up
 };
 struct Unit {
-    int token, rows, page, off;  // first new token, its rows; the page, and the first one's row in it
+    int token, rows, seq, key;  // first new token, its rows; its sequence, and its key's number
 };
 
 // 16 elements of a row.
@@ -83,22 +85,32 @@ __device__ __forceinline__ float power_of(int e) { return __uint_as_float(e > 0 
 template <typename T, int THREADS, typename Reduce>
 __device__ __forceinline__ void append_unit(const AppendParams& p, const Unit& u, int head, int kv, int t, Reduce reduce) {
     const int D = p.a.head_dim, pieces = D / 16, n = u.rows * pieces, H = p.a.num_kv_heads;
-    const T* from = static_cast<const T*>(p.a.fresh[kv]) + (int64_t)u.token * p.a.stride[kv] + (int64_t)head * D;
-    const int64_t row0 = (int64_t)u.page << p.page_shift;
-    uint8_t* const to = p.a.cache[kv] + (row0 * H + head) * D;  // the page's first row
-    uint8_t* const scale = p.a.scale[kv] + (int64_t)u.page * H + head;
-    const int was = u.off > 0 ? min((int)*scale, 254) : 0;
-    Piece<T> kept[kKept];
+    auto row_of = [&](int i) { return pieces == 1 ? i : (int)__umulhi((unsigned)i, p.piece_inverse); };  // i / pieces, below 2^28
+    auto source = [&](int i) {
+        const int row = row_of(i);
+        return static_cast<const T*>(p.a.fresh[kv]) + (int64_t)(u.token + row) * p.a.stride[kv] + (int64_t)head * D + (i - row * pieces) * 16;
+    };
+    Piece<T> kept[kKept<T>];
     float top = 0.f;
 #pragma unroll
-    for (int k = 0; k < kKept; ++k)
-        if (t + k * THREADS < n) kept[k].load(from + (int64_t)((t + k * THREADS) / pieces) * p.a.stride[kv] + (t + k * THREADS) % pieces * 16);
+    for (int k = 0; k < kKept<T>; ++k)
+        if (t + k * THREADS < n) kept[k].load(source(t + k * THREADS));
+    // the page is looked up while the rows are on their way
+    const int index = u.key >> p.page_shift, off = u.key & ((1 << p.page_shift) - 1);
+    const int page = u.key >= 0 && index < p.a.pages_per_seq ? __ldg(p.a.block_table + (size_t)u.seq * p.a.pages_per_seq + index) : -1;
+    if ((unsigned)page >= (unsigned)p.a.num_pages) {
+        if (t == 0) raise_error(p.a.err_word, kErrDeviceArg);
+        return;  // (all of the unit's threads)
+    }
+    uint8_t* const to = p.a.cache[kv] + ((((int64_t)page << p.page_shift) * H) + head) * D;  // the page's first row
+    uint8_t* const scale = p.a.scale[kv] + (int64_t)page * H + head;
+    const int was = off > 0 ? min((int)*scale, 254) : 0;
 #pragma unroll
-    for (int k = 0; k < kKept; ++k)
+    for (int k = 0; k < kKept<T>; ++k)
         if (t + k * THREADS < n) top = kept[k].top(top);
-    for (int i = t + kKept * THREADS; i < n; i += THREADS) {
+    for (int i = t + kKept<T> * THREADS; i < n; i += THREADS) {
         Piece<T> x;
-        x.load(from + (int64_t)(i / pieces) * p.a.stride[kv] + i % pieces * 16);
+        x.load(source(i));
         top = x.top(top);
     }
     const uint32_t bits = __float_as_uint(reduce(top));
@@ -106,10 +118,11 @@ __device__ __forceinline__ void append_unit(const AppendParams& p, const Unit& u
     const int least = bits == 0 ? 1 : max(1, (int)(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0));
     const int b = max(least, was);
     if (t == 0 && b != was) *scale = (uint8_t)b;
-    if (u.off > 0 && b > was) {
+    if (off > 0 && b > was) {
         const float down = power_of(127 + was - b);  // (0 from 2^-127 on: every code becomes 0)
-        for (int i = t; i < u.off * pieces; i += THREADS) {
-            uint4* at = reinterpret_cast<uint4*>(to + (int64_t)(i / pieces) * H * D + i % pieces * 16);
+        for (int i = t; i < off * pieces; i += THREADS) {
+            const int row = row_of(i);
+            uint4* at = reinterpret_cast<uint4*>(to + (int64_t)row * H * D + (i - row * pieces) * 16);
             uint4 c = *at;
             uint32_t* w = reinterpret_cast<uint32_t*>(&c);
 #pragma unroll
@@ -124,14 +137,15 @@ __device__ __forceinline__ void append_unit(const AppendParams& p, const Unit& u
     }
     const float up = power_of(254 - b);
     auto store = [&](const Piece<T>& x, int i) {
-        *reinterpret_cast<uint4*>(to + (int64_t)(u.off + i / pieces) * H * D + i % pieces * 16) = x.codes(up);
+        const int row = row_of(i);
+        *reinterpret_cast<uint4*>(to + (int64_t)(off + row) * H * D + (i - row * pieces) * 16) = x.codes(up);
     };
 #pragma unroll
-    for (int k = 0; k < kKept; ++k)
+    for (int k = 0; k < kKept<T>; ++k)
         if (t + k * THREADS < n) store(kept[k], t + k * THREADS);
-    for (int i = t + kKept * THREADS; i < n; i += THREADS) {
+    for (int i = t + kKept<T> * THREADS; i < n; i += THREADS) {
         Piece<T> x;
-        x.load(from + (int64_t)(i / pieces) * p.a.stride[kv] + i % pieces * 16);
+        x.load(source(i));
         store(x, i);
     }
 }
@@ -145,12 +159,10 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_fp8_kernel(const __g
     griddep_wait();
     const KvAppendFp8Args& a = p.a;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, head = blockIdx.y, kv = blockIdx.z;
-    const int t0 = blockIdx.x * p.tokens, all = min(a.total_new, __ldg(a.cu_new + a.num_seqs));
-    if (t0 >= all) return;
     if (tid == 0) count = 0;
     __syncthreads();
-    if (tid < p.tokens && t0 + tid < all) {
-        const int t = t0 + tid;
+    if (tid < p.tokens) {
+        const int t = blockIdx.x * p.tokens + tid, all = min(a.total_new, __ldg(a.cu_new + a.num_seqs));
         int s = 0;
         for (int hi = a.num_seqs; hi - s > 1;) {  // the last sequence that begins at or before t
             const int mid = (s + hi) >> 1;
@@ -159,15 +171,8 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_fp8_kernel(const __g
         const int first = __ldg(a.cu_new + s), end = __ldg(a.cu_new + s + 1);
         const int len = __ldg(a.cu_kv + s + 1) - __ldg(a.cu_kv + s), pos = len - (end - first) + t - first;
         const int off = pos & ((1 << p.page_shift) - 1);
-        if (t == first || off == 0) {
-            const int index = pos >> p.page_shift;
-            const int page = len >= end - first && index >= 0 && index < a.pages_per_seq
-                                 ? __ldg(a.block_table + (size_t)s * a.pages_per_seq + index) : -1;
-            if ((unsigned)page >= (unsigned)a.num_pages)
-                raise_error(a.err_word, kErrDeviceArg);
-            else
-                units[atomicAdd(&count, 1)] = Unit{t, min((1 << p.page_shift) - off, min(end, all) - t), page, off};
-        }
+        if (t < all && (t == first || off == 0))
+            units[atomicAdd(&count, 1)] = Unit{t, min((1 << p.page_shift) - off, min(end, all) - t), s, len >= end - first ? pos : -1};
     }
     __syncthreads();
     const int n = count;  // (their order is that of arrival: each is by itself)
@@ -181,7 +186,10 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_fp8_kernel(const __g
                 __syncthreads();  // (the unit before is done with tops)
                 if (lane == 0) tops[warp] = top;
                 __syncthreads();
-                return fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+                float all = tops[0];
+#pragma unroll
+                for (int w = 1; w < kAppendThreads / 32; ++w) all = fmaxf(all, tops[w]);
+                return all;
             });
         } else if (mine++ % (kAppendThreads / 32) == warp) {
             append_unit<T, 32>(p, u, head, kv, lane, [&](float top) {
@@ -201,6 +209,7 @@ int launch_kv_append_fp8(const KvAppendFp8Args& a, cudaStream_t stream) {
     p.a = a;
     p.page_shift = 0;
     while ((1 << p.page_shift) < a.page_size) ++p.page_shift;
+    p.piece_inverse = (unsigned)(((1ull << 32) + a.head_dim / 16 - 1) / (a.head_dim / 16));
     // as many tokens a block as a sequence brings, so that neither units wait for one another nor blocks find none
     p.tokens = 4;
     while (p.tokens < std::min(kAppendTokens, a.page_size) && p.tokens * 2 * (long long)a.num_seqs <= a.total_new) p.tokens *= 2;

@@ -23,12 +23,17 @@
 namespace bp {
 namespace {
 
-constexpr int kPagesThreads = 512;
 constexpr int kPerThread = 4;  // tokens in a row
+constexpr int kCopied = 12288; // of up to so many sequences the old lengths are in shared memory too
+constexpr int pages_smem(int seqs) { return ((seqs <= kCopied ? 4 : 3) * seqs + 3) * (int)sizeof(int); }
+constexpr int kMostSmem = pages_smem(kCopied) > pages_smem(kPagesMaxSeqs) ? pages_smem(kCopied) : pages_smem(kPagesMaxSeqs);
+static_assert(kMostSmem <= 226 * 1024, "a block's shared memory");
 
 struct PagesParams {
     PagesUpdateArgs a;
     int page_shift;
+    int may_overflow;  // the lengths' sum may pass 31 bits
+    int wide;  // positions and slots may be written by 16 bytes
 };
 
 // The last i of [0, n) with sums[i] <= x (sums[0] <= x).
@@ -41,9 +46,13 @@ __device__ __forceinline__ int place_of(const int* sums, int n, int x) {
     return i;
 }
 
-__global__ void __launch_bounds__(kPagesThreads) pages_update_kernel(const __grid_constant__ PagesParams p) {
-    extern __shared__ int sums[];  // [3][num_seqs + 1]: new tokens, taken pages, given pages of the sequences before
-    __shared__ int warp_sums[4][kPagesThreads / 32];
+// THREADS: 128 for a few sequences and tokens, whose time is that of the steps below one after the other; else 512.
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) pages_update_kernel(const __grid_constant__ PagesParams p) {
+    constexpr int kWarps = THREADS / 32;
+    // [3][num_seqs + 1]: new tokens, taken pages, given pages of the sequences before; where there is room, old_lens
+    extern __shared__ int sums[];
+    __shared__ int warp_sums[4][kWarps], warps_before[4][kWarps + 1];
     griddep_launch_dependents();
     griddep_wait();
     const PagesUpdateArgs& a = p.a;
@@ -51,19 +60,22 @@ __global__ void __launch_bounds__(kPagesThreads) pages_update_kernel(const __gri
     int* const tokens = sums;
     int* const taken = sums + n + 1;
     int* const given = sums + 2 * (n + 1);
+    int* const copy = n <= kCopied ? sums + 3 * (n + 1) : nullptr;
+    const int* const olds = copy ? copy : a.old_lens;
     auto pages_of = [&](int len) { return (int)(((unsigned)len + P - 1) >> p.page_shift); };
 
-    // ---- prefix sums over the sequences, kPagesThreads at a time
+    // ---- prefix sums over the sequences, THREADS at a time
     const int num_free = *a.num_free;
     int carry[4] = {0, 0, 0, 0};  // tokens, taken, given; keys after the step
     bool bad = num_free < 0 || num_free > a.num_pages;
-    long long all_tokens = 0, all_keys = 0, all_given = 0;
+    long long all_keys = 0, all_given = 0;
     const bool writes = blockIdx.x == 0;
-    for (int base = 0; base < n; base += kPagesThreads) {
+    for (int base = 0; base < n; base += THREADS) {
         const int s = base + tid;
         int v[4] = {0, 0, 0, 0};
         if (s < n) {
             const int o = __ldg(a.old_lens + s), w = __ldg(a.new_lens + s);
+            if (copy) copy[s] = o;
             if (o < 0 || w < 0 || pages_of(o) > a.pages_per_seq || pages_of(w) > a.pages_per_seq) {
                 bad = true;
             } else {
@@ -71,7 +83,6 @@ __global__ void __launch_bounds__(kPagesThreads) pages_update_kernel(const __gri
                 v[1] = max(0, pages_of(w) - pages_of(o));
                 v[2] = max(0, pages_of(o) - pages_of(w));
                 v[3] = w;
-                all_tokens += v[0];
                 all_keys += w;
                 all_given += v[2];
             }
@@ -86,24 +97,23 @@ __global__ void __launch_bounds__(kPagesThreads) pages_update_kernel(const __gri
                 if (lane >= o) sum[k] += y;
             }
         }
-        __syncthreads();  // the sequences before are done with warp_sums
         if (lane == 31)
 #pragma unroll
             for (int k = 0; k < 4; ++k) warp_sums[k][warp] = sum[k];
         __syncthreads();
-        int total[4];
+        if (tid < 4) {  // (a few numbers: one after the other)
+            int before = 0;
+            for (int w = 0; w < kWarps; ++w) {
+                warps_before[tid][w] = before;
+                before += warp_sums[tid][w];
+            }
+            warps_before[tid][kWarps] = before;
+        }
+        __syncthreads();  // (and the sums before are written again only behind the next one)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const int w = lane < kPagesThreads / 32 ? warp_sums[k][lane] : 0;
-            int before = lane < warp ? w : 0;
-            total[k] = w;
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                before += __shfl_xor_sync(0xffffffffu, before, o);
-                total[k] += __shfl_xor_sync(0xffffffffu, total[k], o);
-            }
-            sum[k] += carry[k] + before;
-            carry[k] += total[k];
+            sum[k] += carry[k] + warps_before[k][warp];
+            carry[k] += warps_before[k][kWarps];
         }
         if (s < n) {
             tokens[s + 1] = sum[0];
@@ -111,30 +121,24 @@ __global__ void __launch_bounds__(kPagesThreads) pages_update_kernel(const __gri
             given[s + 1] = sum[2];
             if (writes && a.cu_kv) a.cu_kv[s + 1] = sum[3];  // (rewritten below where the step does not take place)
         }
+        if (base + THREADS < n) __syncthreads();
     }
     if (tid == 0) tokens[0] = taken[0] = given[0] = 0;
-    // (the sums above may pass 31 bits; these tell)
+    if (p.may_overflow) {  // the sums above may pass 31 bits: these tell
+        __shared__ long long long_sums[2][kWarps];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        all_tokens += __shfl_xor_sync(0xffffffffu, all_tokens, o);
-        all_keys += __shfl_xor_sync(0xffffffffu, all_keys, o);
-        all_given += __shfl_xor_sync(0xffffffffu, all_given, o);
-    }
-    __shared__ long long long_sums[3][kPagesThreads / 32];
-    if (lane == 0) {
-        long_sums[0][warp] = all_tokens;
-        long_sums[1][warp] = all_keys;
-        long_sums[2][warp] = all_given;
-    }
-    __syncthreads();
-    all_tokens = all_keys = all_given = 0;
-    for (int w = 0; w < kPagesThreads / 32; ++w) {
-        all_tokens += long_sums[0][w];
-        all_keys += long_sums[1][w];
-        all_given += long_sums[2][w];
+        for (int o = 16; o > 0; o >>= 1) {
+            all_keys += __shfl_xor_sync(0xffffffffu, all_keys, o);
+            all_given += __shfl_xor_sync(0xffffffffu, all_given, o);
+        }
+        if (lane == 0) long_sums[0][warp] = all_keys, long_sums[1][warp] = all_given;
+        __syncthreads();
+        all_keys = all_given = 0;
+        for (int w = 0; w < kWarps; ++w) all_keys += long_sums[0][w], all_given += long_sums[1][w];
+        bad = bad || all_keys > INT_MAX || all_given > a.num_pages;
     }
     const int A = carry[1], R = carry[2];
-    bad = __syncthreads_or(bad) || all_keys > INT_MAX || all_given > a.num_pages || ((a.positions || a.slots) && all_tokens > a.total_new) ||
+    bad = __syncthreads_or(bad) || R > a.num_pages || ((a.positions || a.slots) && carry[0] > a.total_new) ||
           (long long)num_free + R - A > a.num_pages;
     const int missing = bad ? 0 : max(0, A - R - num_free);
     const bool done = !bad && missing == 0;
@@ -143,18 +147,19 @@ __global__ void __launch_bounds__(kPagesThreads) pages_update_kernel(const __gri
     // the page that is taken as number i, and the one that is given back as number i
     auto given_page = [&](int i) {
         const int s = place_of(given, n, i);
-        return a.block_table[(size_t)s * a.pages_per_seq + pages_of(__ldg(a.new_lens + s)) + i - given[s]];
+        return a.block_table[(size_t)s * a.pages_per_seq + pages_of(olds[s]) + i - given[s + 1]];  // (the last of its pages)
     };
     auto taken_page = [&](int i) { return i < R ? given_page(i) : a.free_pages[num_free - 1 - (i - R)]; };
-    const int t0 = blockIdx.x * kPagesThreads + tid, stride = gridDim.x * kPagesThreads;
+    // (pages by the last threads first, tokens by the first: few of both are moved at the same time)
+    const int t0 = blockIdx.x * THREADS + tid, stride = gridDim.x * THREADS, back = stride - 1 - t0;
     if (done) {
-        for (int i = t0; i < A; i += stride) {
+        for (int i = back; i < A; i += stride) {
             const int s = place_of(taken, n, i);
             const int page = taken_page(i);
             if ((unsigned)page >= (unsigned)a.num_pages) raise_error(a.err_word, kErrDeviceArg);
-            a.block_table[(size_t)s * a.pages_per_seq + pages_of(__ldg(a.old_lens + s)) + i - taken[s]] = page;
+            a.block_table[(size_t)s * a.pages_per_seq + pages_of(olds[s]) + i - taken[s]] = page;
         }
-        for (int i = A + t0; i < R; i += stride) {
+        for (int i = A + back; i < R; i += stride) {
             const int page = given_page(i);
             if ((unsigned)page >= (unsigned)a.num_pages) raise_error(a.err_word, kErrDeviceArg);
             a.free_pages[num_free + R - 1 - i] = page;
@@ -165,31 +170,44 @@ __global__ void __launch_bounds__(kPagesThreads) pages_update_kernel(const __gri
         for (int t = t0 * kPerThread; t < a.total_new; t += stride * kPerThread) {
             int s = t < real ? place_of(tokens, n, t) : 0, old = 0, held = 0, at = -1, page = 0;
             bool fresh = true;
+            int pos[kPerThread];
+            int64_t slot[kPerThread];
 #pragma unroll
             for (int k = 0; k < kPerThread; ++k) {
                 const int x = t + k;
-                if (x >= a.total_new) break;
-                int pos = -1;
-                int64_t slot = -1;
+                pos[k] = -1;
+                slot[k] = -1;
                 if (x < real) {
                     while (x >= tokens[s + 1]) ++s, fresh = true;
-                    if (fresh) old = __ldg(a.old_lens + s), held = pages_of(old), at = -1, fresh = false;
-                    pos = old + x - tokens[s];
-                    const int j = pos >> p.page_shift;
+                    if (fresh) old = olds[s], held = pages_of(old), at = -1, fresh = false;
+                    pos[k] = old + x - tokens[s];
+                    const int j = pos[k] >> p.page_shift;
                     if (j != at) {
                         at = j;
                         page = j < held ? a.block_table[(size_t)s * a.pages_per_seq + j] : taken_page(taken[s] + j - held);
                     }
-                    slot = ((int64_t)page << p.page_shift) + (pos & (P - 1));
+                    slot[k] = ((int64_t)page << p.page_shift) + (pos[k] & (P - 1));
                 }
-                if (a.positions) a.positions[x] = pos;
-                if (a.slots) a.slots[x] = slot;
+            }
+            if (p.wide && t + kPerThread <= a.total_new) {
+                if (a.positions) *reinterpret_cast<int4*>(a.positions + t) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+                if (a.slots) {
+                    *reinterpret_cast<longlong2*>(a.slots + t) = make_longlong2(slot[0], slot[1]);
+                    *reinterpret_cast<longlong2*>(a.slots + t + 2) = make_longlong2(slot[2], slot[3]);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < kPerThread; ++k) {
+                    if (t + k >= a.total_new) break;
+                    if (a.positions) a.positions[t + k] = pos[k];
+                    if (a.slots) a.slots[t + k] = slot[k];
+                }
             }
         }
     }
     if (writes) {
         if (a.cu_new)
-            for (int s = tid; s <= n; s += kPagesThreads) a.cu_new[s] = done ? tokens[s] : 0;
+            for (int s = tid; s <= n; s += THREADS) a.cu_new[s] = done ? tokens[s] : 0;
         if (a.cu_kv && tid == 0) {
             a.cu_kv[0] = 0;
             if (!done)  // the lengths stay (rare: by one thread)
@@ -197,14 +215,16 @@ __global__ void __launch_bounds__(kPagesThreads) pages_update_kernel(const __gri
         }
         if (a.missing && tid == 0) *a.missing = missing;
     }
-    // every block has read the list's length: the last one writes the new one
+    // the list's new length, by the last block to finish: every one has read it then
     __syncthreads();
     if (tid == 0) {
-        __threadfence();
-        if (atomicAdd(a.ticket, 1u) == gridDim.x - 1) {
-            *a.ticket = 0;
-            if (done) *a.num_free = num_free + R - A;
+        bool last = gridDim.x == 1;
+        if (!last) {
+            __threadfence();
+            last = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
+            if (last) *a.ticket = 0;
         }
+        if (last && done) *a.num_free = num_free + R - A;
     }
 }
 
@@ -215,32 +235,34 @@ int launch_pages_update(const PagesUpdateArgs& a, const DeviceInfo& dev, cudaStr
     p.a = a;
     p.page_shift = 0;
     while ((1 << p.page_shift) < a.page_size) ++p.page_shift;
-    const int smem = 3 * (a.num_seqs + 1) * (int)sizeof(int);
+    p.wide = reinterpret_cast<uintptr_t>(a.positions) % 16 == 0 && reinterpret_cast<uintptr_t>(a.slots) % 16 == 0;
+    p.may_overflow = (long long)a.num_seqs * a.pages_per_seq * a.page_size > INT_MAX;
+    const long long tokens = a.positions || a.slots ? a.total_new : 0, work = (tokens + 8ll * a.num_seqs) / kPerThread;
+    const bool small = a.num_seqs <= 128 && work <= 1024;
+    const auto kernel = small ? pages_update_kernel<128> : pages_update_kernel<512>;
+    const int threads = small ? 128 : 512;
     static std::mutex mu;
     static bool configured[64] = {};
     if (dev.device < 0 || dev.device >= 64) return BP_ERR_UNSUPPORTED;
     {
         std::lock_guard<std::mutex> lock(mu);
         if (!configured[dev.device]) {
-            if (cudaFuncSetAttribute(pages_update_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                     3 * (kPagesMaxSeqs + 1) * (int)sizeof(int)) != cudaSuccess)
+            if (cudaFuncSetAttribute(pages_update_kernel<512>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem) != cudaSuccess)
                 return BP_ERR_CUDA;
             configured[dev.device] = true;
         }
     }
-    const long long tokens = a.positions || a.slots ? a.total_new : 0;
-    const long long blocks = (tokens + 8ll * a.num_seqs) / (kPagesThreads * kPerThread) + 1;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3((unsigned)std::min<long long>(blocks, dev.sm_count), 1, 1);
-    cfg.blockDim = dim3(kPagesThreads, 1, 1);
-    cfg.dynamicSmemBytes = smem;
+    cfg.gridDim = dim3((unsigned)std::min<long long>(work / threads + 1, dev.sm_count), 1, 1);
+    cfg.blockDim = dim3((unsigned)threads, 1, 1);
+    cfg.dynamicSmemBytes = pages_smem(a.num_seqs);
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, pages_update_kernel, p) == cudaSuccess ? BP_OK : BP_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess ? BP_OK : BP_ERR_CUDA;
 }
 
 }  // namespace bp
