@@ -250,3 +250,32 @@ def test_no_sequences_and_no_tokens():
     c, q, lens = make([100], [4], 8, 2, 128, 16)
     o, _ = bp.chunk_attention_paged_fp8(q[:0], c["k"], c["k_scale"], c["v"], c["v_scale"], offsets([0]), offsets([100]), c["table"], 16, 1, 100)
     assert o.shape == (0, 8, 128)
+
+
+@pytest.mark.parametrize("new", [16, 100])
+def test_a_cache_past_4_gib(new):
+    """Pages at the far end of pools of 4.6 GB each: append and attention by 64-bit offsets."""
+    hkv, dim, page = 8, 128, 64
+    pages = (4600 << 20) // (hkv * dim * page)
+    c = dict(page=page)
+    for name in "kv":
+        c[name] = torch.empty(pages * page, hkv, dim, dtype=torch.uint8, device="cuda")
+        c[name + "_scale"] = torch.full((pages, hkv), 120, dtype=torch.uint8, device="cuda")
+    c["table"] = torch.tensor([[pages - 1, 5, pages - 2, pages - 7]], dtype=torch.int32, device="cuda")
+    g = torch.Generator().manual_seed(9)
+    rows = torch.randn(200, 2 * hkv, dim, generator=g).to(torch.bfloat16).cuda()
+    ws = bp.workspace(256, "cuda")
+    bp.kv_append_fp8(c["k"], c["k_scale"], c["v"], c["v_scale"], rows[:, :hkv], rows[:, hkv:], offsets([200]), offsets([200]), c["table"],
+                     page, ws=ws)
+    assert bp.get_status(ws) == 0
+    small = dict(page=page, table=torch.arange(4, dtype=torch.int32, device="cuda")[None])
+    for name in "kv":
+        at = (c["table"][0].long()[:, None] * page + torch.arange(page, device="cuda")).flatten()
+        small[name], small[name + "_scale"] = c[name][at].clone(), c[name + "_scale"][c["table"][0].long()].clone()
+        near = rows[:, :hkv] if name == "k" else rows[:, hkv:]
+        value = small[name].view(torch.float8_e4m3fn)[:200].float() * torch.exp2(small[name + "_scale"].float() - 127).repeat_interleave(page, 0)[:200, :, None]
+        # (a code is off by half a step, 2^-4 of it, or by 2^-10 of a scale that takes the page's largest number below 448)
+        assert ((value - near.float()).abs() <= 2.0 ** -4 * near.float().abs() + 2.0 ** -10 * 2.0 ** -6).all()
+    q = torch.randn(new, 32, dim, generator=g).to(torch.bfloat16).cuda()
+    far, _, _ = run(c, q, [new], [200])
+    assert torch.equal(far, run(small, q, [new], [200])[0])
