@@ -13,6 +13,16 @@
 // query tile each (where a work tile has the rows of one only, both take them, and every other key tile, and add what they
 // have at the end), and block_attention_fp8_kernel for calls whose work tiles all are such: blocks and single tokens.
 //
+// What bounds them (32 query and 8 KV heads of 128; times with a cold L2; floors at 6.75 TB/s and 1.93 PFLOP/s):
+//   * a prompt of 8192, 520 us of 285: a stream's chain from tile to tile, softmax 1,700 to 2,000 cycles (scores out of tensor
+//     memory 450, maximum 200, weights 900 to 1,100), the turn's 16 MMAs 1,200 and the hand-overs; two streams in turn take
+//     3,300 a pair of key tiles, 2,048 of them MMAs (which read shared memory at its full rate: 128 bytes a cycle).  A job
+//     change is 17,000 cycles, half of it the queries' way in; the query rows of a work tile are all that shares a V tile's
+//     conversion.  (A bf16 cache: 369 us, without conversions and with 16 softmax warps.)
+//   * 8 blocks of 31 over 32768 keys, 156 us of 80 (3.5 TB/s): with conversions and MMAs left out 126 to 131, a plain read of
+//     the same rows of 128 bytes 94 to 106.  (A bf16 cache: 236 us, 217 with bp_block_attention_paged.)
+//   * one token over 2048 keys, 15 us in a graph: the plan, two copies, a tile, the merge, one after the other.
+//
 // Roles: warps 0-3 and 4-7 softmax of stream 0 and 1 (a thread a row; they read and split the queries too), warp 8 lays out
 // the jobs and issues K's TMA copies, 9 and 10 issue the streams' MMAs, 11 V's copies and what the merge has to know, 12-15
 // convert V.
@@ -23,7 +33,8 @@
 
 namespace bp {
 namespace {
-// A work tile's fixed cost (queries in, output out), in keys: a prompt of 8192 takes 607 us with 400, 552 with 800, 567 with 1200.
+// A work tile's fixed cost (queries in, output out), in keys: a prompt of 8192 takes 524 us with
+// 600, 520 with 800, 528 with 1000 (8 x 31 over 32768 keys 158, 154, 154).
 constexpr int kTileCost = 800;
 }  // namespace
 }  // namespace bp
@@ -623,11 +634,12 @@ __device__ __forceinline__ void rescale(uint32_t o_addr, float alpha) {
 template <int D>
 struct Shared : Common<D, false> {
     uint64_t q_ready[2], drain[2], turn[2];
-    uint64_t s[2], p[2], o[2];                       // of a stream: scores, weights, the accumulator
+    uint64_t s[2], half[2], p[2], o[2];              // of a stream: scores, a half of the weights, all of them, the accumulator
     int row_ref[2][4];                               // of a split job's streams: what their accumulators are in units of
     __device__ void init() {
         for (int i = 0; i < 2; ++i) {
             mbar_init(&q_ready[i], 4);
+            mbar_init(&half[i], 4);
             mbar_init(&s[i], 1);
             mbar_init(&p[i], 4);
             mbar_init(&o[i], 1);
@@ -750,11 +762,18 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                     const float negm = (m == -INFINITY ? 0.f : -m) + (float)power;
                     uint64_t sum2[2] = {0ull, 0ull};
                     weigh<FACTORS>(lower, f, 0, negm, sum2, s_addr);
+                    // (their P V begins: a prompt of 8192 520 us instead of 538)
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.half[i]);
                     weigh<FACTORS>(upper, f, 1, negm, sum2, s_addr);
                     float u, w;
                     unpack_f32x2(add_f32x2(sum2[0], sum2[1]), u, w);
                     l = fmaf(u + w, __uint_as_float((uint32_t)(127 - power) << 23), l);
                     tmem_st_wait();
+                } else if (lane == 0) {
+                    mbar_arrive(&sh.half[i]);
                 }
                 tc_fence_before();
                 __syncwarp();
@@ -865,8 +884,10 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                         const bool has_k = j < j1, has_v = k > 0 && jp < j1;
                         if (has_k) fine = mbar_wait(&sh.k_full[kslot], (xk / S::k_slots) & 1, kWaitBudget);
                         if (fine && has_v) fine = mbar_wait(&sh.v_full[vslot], (xv / S::v_slots) & 1, kWaitBudget);
-                        if (fine && pv) fine = mbar_wait(&sh.p[i], my_p++ & 1, kWaitBudget);
+                        // (the turn before the weights: a wait takes 100 to 200 cycles even where there is nothing to wait
+                        // for, and after the weights they are on the chain: 556 us instead of 538)
                         if (fine) fine = mbar_wait(&sh.turn[i], ((turn + k) & 1) ^ (i ^ 1), kWaitBudget);
+                        if (fine && pv) fine = mbar_wait(&sh.half[i], my_p & 1, kWaitBudget);
                         if (!fine) break;
                         tc_fence_after();
                         if (pv) {  // O += P V of tile jp
@@ -874,10 +895,16 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                             uint32_t on = jp > first ? 1u : 0u;
 #pragma unroll
                             for (int kk = 0; kk < kKeys / 16; ++kk) {
+                                if (kk == kKeys / 32) {
+                                    fine = mbar_wait(&sh.p[i], my_p++ & 1, kWaitBudget);
+                                    if (!fine) break;
+                                    tc_fence_after();
+                                }
                                 umma_ts(t_o, t_s + kk * 8, upper | (vl + kk * (2048 >> 4)), id_o, on);
                                 on = 1;
                             }
                         }
+                        if (!fine) break;
                         if (qk) {  // S = Q K^T of tile j: both parts of Q, 32 columns at a time
                             const uint32_t kl = k_lo + kslot * (S::code_bytes >> 4);
                             uint32_t on = 0;
@@ -949,7 +976,9 @@ template <int D>
 constexpr int block_smem() { return whole_sm(Shape<D, true>::tiles + (int)sizeof(BlockShared<D>)); }
 static_assert(block_smem<128>() <= 227 * 1024 && block_smem<64>() <= 227 * 1024, "a block's shared memory");
 
-// The same where every work tile has the rows of one stream: blocks and single tokens, whose keys' bytes are what counts.  One
+// The same where every work tile has the rows of one stream: blocks and single tokens, whose keys' bytes are what counts.
+// Against the kernel above, us with a cold L2: 32 x 1 token over 8192 keys in pages of 16 150 (171), 64 x 1 over 4096 147 (168),
+// 8 x 16 over 32768 142 (145), 32 x 16 over 2048 79 (86); 8 x 31 over 32768 157 (155), 1 x 31 54 (52).  One
 // accumulator; scores in three buffers, so that a tile's are there before the softmax has done with the two before it.  The
 // softmax's two groups of warps take the tiles in turn, each row's maximum handed from one tile's thread to the next one's
 // (rarely another: it is moved only where a score has outgrown it by 2^8, and the accumulator with it).
