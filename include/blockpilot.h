@@ -244,8 +244,8 @@ BP_API int bp_chunk_attention_paged(const void* q, int64_t q_stride, const void*
  * even; what is not finite becomes 0x7f.  Rows behind a sequence's last key keep what they hold, and so does the rest of
  * a page begun: they are not keys.  (After a rollback into a page its scale stays as the dropped rows left it.)
  *   k_new, v_new  rows of [num_kv_heads][head_dim] dtype (bf16 or fp32), *_stride elements from a token to the next
- * Limits: head_dim a multiple of 16; 16-byte aligned pointers and strides; num_kv_heads <= 65535.  A page that is to receive
- * rows and has no place in the table or the pool sets BP_ERR_DEVICE_FLAG and is not written; so do rows before key 0.
+ * Limits: head_dim a multiple of 16, page_size * (head_dim / 16)^2 < 2^32; 16-byte aligned pointers and strides;
+ * num_kv_heads <= 65535.  A page that is to receive rows and has no place in the table or the pool sets BP_ERR_DEVICE_FLAG and is not written; so do rows before key 0.
  * Rows from cu_new[num_seqs] on are padding.  A page may belong to one sequence of the call.  workspace: at least 256 bytes.
  *
  * bp_chunk_attention_paged_fp8 is bp_chunk_attention_paged over such a cache: the same arguments, limits, masks, workspace
@@ -285,8 +285,9 @@ BP_API int bp_chunk_attention_paged_fp8(const void* q, int64_t q_stride, const v
  * A length below 0 or past a row of the table, keys past 2^31 - 1, more new tokens than total_new (where positions or slots
  * are given), num_free outside [0, num_pages] or more pages free than there are set BP_ERR_DEVICE_FLAG and change nothing
  * either; so does, but for the change, a page id outside [0, num_pages) that is moved.
- * page_size as bp_block_attention_paged; num_seqs <= 16384 (else BP_ERR_UNSUPPORTED).  workspace: at least 256 bytes; it
- * keeps a counter there, which every call puts back at zero.  The arrays may not overlap, but old_lens and new_lens may.
+ * page_size as bp_block_attention_paged; num_seqs <= 16384, num_pages and total_new <= 2^30 (else BP_ERR_UNSUPPORTED).
+ * workspace: at least 256 bytes; it keeps a counter there, which every call puts back at zero.  The arrays may not overlap,
+ * but old_lens and new_lens may.
  * ------------------------------------------------------------------------------- */
 BP_API int bp_pages_update(int32_t* block_table, const int32_t* old_lens, const int32_t* new_lens, int32_t* free_pages,
                            int32_t* num_free, int num_seqs, int pages_per_seq, int page_size, int num_pages, int total_new,

@@ -325,6 +325,8 @@ int bp_kv_append_fp8(void* k_cache, void* k_scale, void* v_cache, void* v_scale,
     const int64_t row = (int64_t)num_kv_heads * head_dim, step = dtype == BP_BF16 ? 8 : 4;
     if (k_stride < row || v_stride < row) return BP_ERR_INVALID_ARG;
     if (head_dim % 16 != 0 || num_kv_heads > 65535) return BP_ERR_UNSUPPORTED;
+    const long long pieces = head_dim / 16;  // (the kernel divides the numbers of a page's pieces by them in 32 bits)
+    if (pieces >= 1 << 16 || pieces * pieces * page_size >= 1ll << 32) return BP_ERR_UNSUPPORTED;
     if (!aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) ||
         k_stride % step != 0 || v_stride % step != 0)
         return BP_ERR_INVALID_ARG;
@@ -356,7 +358,7 @@ int bp_pages_update(int32_t* block_table, const int32_t* old_lens, const int32_t
     if (!num_free || (num_pages > 0 && !free_pages) || pages_per_seq < (num_seqs > 0 ? 1 : 0) || !valid_page_size(page_size))
         return BP_ERR_INVALID_ARG;
     if ((long long)pages_per_seq * page_size > INT32_MAX) return BP_ERR_INVALID_ARG;
-    if (num_seqs > kPagesMaxSeqs) return BP_ERR_UNSUPPORTED;
+    if (num_seqs > kPagesMaxSeqs || num_pages > 1 << 30 || total_new > 1 << 30) return BP_ERR_UNSUPPORTED;
     int rc = check_workspace(workspace, workspace_bytes, sizeof(WorkspaceHeader));
     if (rc != BP_OK) return rc;
     DeviceInfo dev;

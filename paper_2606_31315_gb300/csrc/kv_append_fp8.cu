@@ -14,6 +14,9 @@
 // one head of K or V; its threads look which of them begin a unit (a sequence's first new token, or a page's first row), then
 // units of many rows are the whole block's, others a warp's.  A thread keeps its rows' pieces in registers between the
 // maximum and the rounding, four of 16 elements (two of fp32); what is more (pages above 64 rows of 128) is read again, from L2.
+//
+// Bound by memory: bf16 in, a byte an element out.  In graphs, 8 KV heads of 128: 8192 tokens 11.6 us (50 MB, 4.4 TB/s: the
+// units' chain, look-up, loads, maximum, stores, once a block), 32 x 16 tokens 4.5, one token 2.4, a launch and three round trips.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -85,7 +88,8 @@ __device__ __forceinline__ float power_of(int e) { return __uint_as_float(e > 0 
 template <typename T, int THREADS, typename Reduce>
 __device__ __forceinline__ void append_unit(const AppendParams& p, const Unit& u, int head, int kv, int t, Reduce reduce) {
     const int D = p.a.head_dim, pieces = D / 16, n = u.rows * pieces, H = p.a.num_kv_heads;
-    auto row_of = [&](int i) { return pieces == 1 ? i : (int)__umulhi((unsigned)i, p.piece_inverse); };  // i / pieces, below 2^28
+    // i / pieces: right for i * pieces below 2^32
+    auto row_of = [&](int i) { return pieces == 1 ? i : (int)__umulhi((unsigned)i, p.piece_inverse); };
     auto source = [&](int i) {
         const int row = row_of(i);
         return static_cast<const T*>(p.a.fresh[kv]) + (int64_t)(u.token + row) * p.a.stride[kv] + (int64_t)head * D + (i - row * pieces) * 16;
@@ -210,7 +214,8 @@ int launch_kv_append_fp8(const KvAppendFp8Args& a, cudaStream_t stream) {
     p.page_shift = 0;
     while ((1 << p.page_shift) < a.page_size) ++p.page_shift;
     p.piece_inverse = (unsigned)(((1ull << 32) + a.head_dim / 16 - 1) / (a.head_dim / 16));
-    // as many tokens a block as a sequence brings, so that neither units wait for one another nor blocks find none
+    // as many tokens a block as a sequence brings, so that neither units wait for one another nor blocks find none (us in graphs,
+    // against always 4 and always 64: 32 sequences of 16 tokens 4.5, 6.7, 10.4; 256 of 1 6.7, 6.6, 20.8; 1 of 8192 11.6, 35.7, 11.6)
     p.tokens = 4;
     while (p.tokens < std::min(kAppendTokens, a.page_size) && p.tokens * 2 * (long long)a.num_seqs <= a.total_new) p.tokens *= 2;
     cudaLaunchConfig_t cfg = {};

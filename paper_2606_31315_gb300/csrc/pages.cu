@@ -12,6 +12,10 @@
 // number alone, by a search in shared memory.  Tables and list are written in places that no block reads (a page that is taken
 // stands behind its sequence's old ones, one that is given back behind the list's old end, and only where none of the old list
 // is taken); the list's length is written by the last block to finish.
+//
+// What it has to move is small (1024 sequences with 370,000 new tokens: 4.5 MB, 0.7 us); what it takes are round trips: the
+// lengths, the scan, the searches, the list's pages, the table.  2.3 us a call for one sequence, of which a launch in a graph
+// is 1.5 and more; 8.4 for that large one.
 #include <limits.h>
 
 #include <algorithm>
@@ -46,7 +50,10 @@ __device__ __forceinline__ int place_of(const int* sums, int n, int x) {
     return i;
 }
 
-// THREADS: 128 for a few sequences and tokens, whose time is that of the steps below one after the other; else 512.
+// THREADS: 128 for up to 128 sequences whose tokens are one pass of the grid: the time is that of the steps below one after
+// the other, barriers among them (us a call in graphs, against 512: 1 sequence of 1 token 2.3 and 2.7, of 8192 tokens 2.9 and
+// 3.4, 8 of 16 2.7 and 3.0, 64 of 16 3.4 and 3.2, 128 of 16 3.5 and 3.8).  512 beyond: 256 of 16 5.7 against 6.4, 1024
+// sequences of up to 2000 tokens 8.4 against 12.6.
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS) pages_update_kernel(const __grid_constant__ PagesParams p) {
     constexpr int kWarps = THREADS / 32;
@@ -238,7 +245,7 @@ int launch_pages_update(const PagesUpdateArgs& a, const DeviceInfo& dev, cudaStr
     p.wide = reinterpret_cast<uintptr_t>(a.positions) % 16 == 0 && reinterpret_cast<uintptr_t>(a.slots) % 16 == 0;
     p.may_overflow = (long long)a.num_seqs * a.pages_per_seq * a.page_size > INT_MAX;
     const long long tokens = a.positions || a.slots ? a.total_new : 0, work = (tokens + 8ll * a.num_seqs) / kPerThread;
-    const bool small = a.num_seqs <= 128 && work <= 1024;
+    const bool small = a.num_seqs <= 128 && work <= 128ll * dev.sm_count;
     const auto kernel = small ? pages_update_kernel<128> : pages_update_kernel<512>;
     const int threads = small ? 128 : 512;
     static std::mutex mu;

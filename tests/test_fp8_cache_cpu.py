@@ -58,6 +58,17 @@ def test_append_refusals(lib, change, status):
     assert _append(lib, **change) == status
 
 
+@pytest.mark.parametrize("change", [dict(d=1 << 19, hk=1, kst=1 << 19, vst=1 << 19, page=16), dict(d=1 << 20, hk=1, kst=1 << 20, vst=1 << 20, page=16),
+                                    dict(d=1 << 18, hk=1, kst=1 << 18, vst=1 << 18, page=16), dict(d=1024, kst=8192, vst=8192, page=1 << 20)])
+def test_append_refuses_pages_of_too_many_pieces(lib, change):
+    assert _append(lib, **change) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("change", [dict(np=(1 << 30) + 1), dict(t=(1 << 30) + 1), dict(t=(1 << 31) - 1)])
+def test_pages_refuses_numbers_past_2_30(lib, change):
+    assert _pages(lib, **change) == UNSUPPORTED
+
+
 @pytest.mark.parametrize("change,status", [
     (dict(t=-1), INVALID), (dict(q=None), INVALID), (dict(ks=None), INVALID), (dict(vs=None), INVALID), (dict(o=None), INVALID),
     (dict(bt=None), INVALID), (dict(hq=30), INVALID), (dict(hk=0), INVALID), (dict(mask=2), INVALID), (dict(dt=9), INVALID),
