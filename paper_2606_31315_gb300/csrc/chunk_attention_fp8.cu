@@ -100,8 +100,11 @@ struct Common {
 };
 
 // The values' powers of two: a tile's are held against its largest one (below 2^-24 of it they are 0; fp16 has e4m3's 18
-// powers and 22 more), and that one against the largest so far, `ref`: the weights take the difference, times 2^7.  So they
-// are at most 2^15 in fp16, and a tile whose values are 2^-14 of others' still has all its weights' bits down to 2^-7.
+// powers and 22 more), and that one against the largest so far, `ref`: the weights take the difference, times 2^5.  A row's
+// maximum is moved where a score has outgrown it by 2^10, so that they are at most 2^15 in fp16.  Under 2^-19 of the weight of
+// the row's maximum they lose bits, and what is left out, under 2^-30 of it each, is 2^-10 of the row after 2^20 keys.  (Moves by 2^8
+// and weights times 2^7: a prompt of 8192 490 us instead of 480, by 2^12 and times 2^3 470.)  A tile whose values are 2^-12 of
+// others' still has all its weights' bits down to 2^-7.
 constexpr uint32_t kLeastRef = 15;  // of a tile, so that the accumulator's power is a number too
 
 // 2^(e - 127) of a biased exponent below 255.
@@ -743,22 +746,25 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                     take_scores(s_addr, 0, full, from, to, lower, mx[0]);
                     take_scores(s_addr, 1, full, from, to, upper, mx[1]);
                     const float top = top_score<FACTORS>(mx[0], mx[1], f);
-                    // (with this m, 2^(score - m) stays below 2^8)
-                    const bool grew = top > m + 8.f;
+                    // (with this m, 2^(score - m) stays below 2^10)
+                    const bool grew = top > m + 10.f;
                     const int tile_ref = sh.v_ref[batch][in_batch(j - j0, 0, box_shift)];
                     if (__any_sync(0xffffffffu, grew) || tile_ref > ref) {
-                        float alpha = grew ? chunk_exp2(m - top) : 1.f;
-                        if (grew) l *= alpha;
+                        // (all of the warp's rows, those that need not too: their next move is later for it; a prompt of 8192
+                        // with 2^8 490 us, 521 with each row moved for itself)
+                        const float m_old = m;
+                        m = fmaxf(m, top);
+                        float alpha = m > m_old ? chunk_exp2(m_old - m) : 1.f;
+                        l *= alpha;
                         // (this tile's scores are complete, so the stream's MMAs before them, the last P V among them, are too)
                         if (j > from_j) {
                             if (tile_ref > ref) alpha *= power_of((uint32_t)max(127 + ref - tile_ref, 0));
                             rescale<D>(lanes + kColO + i * D, alpha);
                         }
-                        if (grew) m = top;
                         ref = max(ref, tile_ref);
                     }
-                    // weights 2^(f * score - m) times the values' power and 2^7, packed in pairs over the scores; their sum
-                    const int power = max(tile_ref - ref + 7, -60);
+                    // weights 2^(f * score - m) times the values' power and 2^5, packed in pairs over the scores; their sum
+                    const int power = max(tile_ref - ref + 5, -60);
                     const float negm = (m == -INFINITY ? 0.f : -m) + (float)power;
                     uint64_t sum2[2] = {0ull, 0ull};
                     weigh<FACTORS>(lower, f, 0, negm, sum2, s_addr);
@@ -792,8 +798,8 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
             }
             batch0 += batches_of(max(0, j1 - j0), box_shift);
             if (!split && failed) continue;
-            // the weights of the streams' accumulators, which are in units of 2^(ref - 134)
-            float w_mine = some ? power_of((uint32_t)(ref - 7)) : 0.f, w_other = 0.f;
+            // the weights of the streams' accumulators, which are in units of 2^(ref - 132)
+            float w_mine = some ? power_of((uint32_t)(ref - 5)) : 0.f, w_other = 0.f;
             bool others_some = false;
             if (split) {
                 // ---- the other stream's part of these rows, merged as the second kernel merges CTAs' parts
@@ -810,7 +816,7 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                 l = i == 0 ? l * u + o.y * v : o.y * v + l * u;
                 m = top;
                 w_mine *= u;
-                if (others_some) w_other = v * power_of((uint32_t)(sh.row_ref[i ^ 1][quad] - 7));
+                if (others_some) w_other = v * power_of((uint32_t)(sh.row_ref[i ^ 1][quad] - 5));
             }
             const bool first = g->first, whole = first && g->last;
             // the query row's number among all, in the output (-1: none)
@@ -981,7 +987,7 @@ static_assert(block_smem<128>() <= 227 * 1024 && block_smem<64>() <= 227 * 1024,
 // 8 x 16 over 32768 142 (145), 32 x 16 over 2048 79 (86); 8 x 31 over 32768 157 (155), 1 x 31 54 (52).  One
 // accumulator; scores in three buffers, so that a tile's are there before the softmax has done with the two before it.  The
 // softmax's two groups of warps take the tiles in turn, each row's maximum handed from one tile's thread to the next one's
-// (rarely another: it is moved only where a score has outgrown it by 2^8, and the accumulator with it).
+// (rarely another: it is moved only where a score has outgrown it by 2^10, and the accumulator with it).
 template <int D, int FACTORS>
 __global__ void __launch_bounds__(kThreads, 1)
 block_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_constant__ CUtensorMap kmap,
@@ -1080,9 +1086,9 @@ block_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                         ref_old = sh.ref[quad];
                         __syncwarp();
                     }
-                    // (with this m, 2^(score - m) stays below 2^8)
-                    const bool grew = top > m_old + 8.f;
-                    const float m_new = grew ? top : m_old;
+                    // (with this m, 2^(score - m) stays below 2^10)
+                    const float m_new = __any_sync(0xffffffffu, top > m_old + 10.f) ? fmaxf(m_old, top) : m_old;
+                    const bool grew = m_new > m_old;
                     ref = max(ref_old, tile_ref);
                     const bool moves = t > 0 && __any_sync(0xffffffffu, (grew && m_old != -INFINITY) || ref > ref_old);
                     if (t == 0 || grew) sh.top[r] = m_new;
@@ -1099,8 +1105,8 @@ block_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                         l *= chunk_exp2(m - m_new);
                         m = m_new;
                     }
-                    // weights 2^(f * score - m) times the values' power and 2^7, over the scores; their sum
-                    const int power = max(tile_ref - ref + 7, -60);
+                    // weights 2^(f * score - m) times the values' power and 2^5, over the scores; their sum
+                    const int power = max(tile_ref - ref + 5, -60);
                     const float negm = (m == -INFINITY ? 0.f : -m) + (float)power;
                     uint64_t sum2[2] = {0ull, 0ull};
                     weigh<FACTORS>(lower, f, 0, negm, sum2, s_addr);
@@ -1130,7 +1136,7 @@ block_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                 nd[0] += (tiles + 1) >> 1;
                 nd[1] += tiles >> 1;
             }
-            // ---- the sums of both groups' tiles, for the last tile's maximum; the accumulator is in units of 2^(ref - 134)
+            // ---- the sums of both groups' tiles, for the last tile's maximum; the accumulator is in units of 2^(ref - 132)
             if (tiles > 0 && !idle) {
                 const float top = sh.top[r];
                 if (m != top) l *= chunk_exp2(m - top);
@@ -1147,7 +1153,7 @@ block_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
             // the query row's number among all, in the output (-1: none)
             const long long orow = active ? (long long)(g->q0 + tok) * p.num_q_heads + g->h * G + r - my_tok * G : -1;
             had_job(sh, nj);
-            const float weight = (tiles > 0 ? power_of((uint32_t)(ref - 7)) : 0.f) * (whole ? row_inverse(m, l) : 1.f);
+            const float weight = (tiles > 0 ? power_of((uint32_t)(ref - 5)) : 0.f) * (whole ? row_inverse(m, l) : 1.f);
             const size_t slot = (size_t)blockIdx.x * 2 + (first ? 1 : 0);
             if (!idle)  // (each group has half of the columns)
                 write_rows<D>(p, tiles > 0 ? lanes + kColO : 0, 0, weight, 0.f, i * (D / 2), (i + 1) * (D / 2), whole, orow, slot, r);
