@@ -33,9 +33,9 @@
 
 namespace bp {
 namespace {
-// A work tile's fixed cost (queries in, output out), in keys: a prompt of 8192 takes 524 us with
-// 600, 520 with 800, 528 with 1000 (8 x 31 over 32768 keys 158, 154, 154).
-constexpr int kTileCost = 800;
+// A work tile's fixed cost (queries in, output out), in keys: a prompt of 8192 takes 502 us with 600, 451 with 800, 447 with
+// 1000 (decoding batches the same with all three).
+constexpr int kTileCost = 1000;
 }  // namespace
 }  // namespace bp
 
@@ -50,8 +50,16 @@ constexpr int kSoftmaxWarps = 8;                 // a thread a row, four warps a
 constexpr int kKeyWarp = 8, kMmaWarp = 9, kValueWarp = 11, kConvertWarp = 12;  // (a stream's MMA warp: kMmaWarp + stream)
 constexpr int kConvertWarps = 4;                 // 32 keys of a tile each
 constexpr int kThreads = 32 * (kConvertWarp + kConvertWarps);
-// Registers: 128 a thread at launch (512 x 128); 256 x 192 + 256 x 64 are as many.
-constexpr int kSoftmaxRegs = 192, kOtherRegs = 64;
+// Registers of the roles: 128 a thread at launch (512 x 128), as many as 256 x softmax + 128 x (convert + other).  Each role sets
+// its own in its own branch (before they part: 32 x 1 tokens over 8192 keys 148 us instead of 140, and of two values there the
+// compiler keeps to the lesser for both).  A prompt of 8192 takes 457 us with 192, 64 and 64, 447 with 200, 56 and 56, 454 with
+// 208, 48 and 48; decoding batches 140 with the first and 144 with the second.
+struct Registers {
+    int softmax, convert, other;
+};
+constexpr Registers kRegs = {200, 56, 56}, kBlockRegs = {192, 64, 64};
+static_assert(256 * kRegs.softmax + 128 * (kRegs.convert + kRegs.other) <= kThreads * 128, "the launch's registers");
+static_assert(256 * kBlockRegs.softmax + 128 * (kBlockRegs.convert + kBlockRegs.other) <= kThreads * 128, "the launch's registers");
 constexpr int kJobs = 4;                         // jobs laid out ahead
 constexpr int kBatches = 8;                      // of 32 boxes' scales: jobs and tiles that may be under way at once, and more
 
@@ -437,12 +445,21 @@ __device__ __forceinline__ void convert_values(const ChunkParams& p, Sh& sh, uin
                 const int below = sh.v_below[(batch0 + batch_of(j - j0, box_shift)) % kBatches][in_batch(j - j0, (w * 32 + h * 16) >> box_shift, box_shift)];
                 return (below < 15 ? (15 - below) << 10 : below < 25 ? 1 << (24 - below) : 0) * 0x10001u;
             };
+            // (the second half of the codes set out before the wait for a place: 64 x 1 tokens over 4096 keys 140 us instead of
+            // 144, a prompt of 8192 460 instead of 478)
+            uint4 in[2][kPieces];
+            auto bring = [&](int h) {
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k)
+                    in[h][k] = ld_shared16(raw + from[k % kForms] + (h * kPieces + k) / kForms * 8 * D);
+            };
+            bring(0);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {  // 16 keys at a time: boxes are no smaller
                 uint32_t v[kPieces][4];
 #pragma unroll
                 for (int k = 0; k < kPieces; ++k) {
-                    const uint4 c = *reinterpret_cast<const uint4*>(raw + from[k % kForms] + (h * kPieces + k) / kForms * 8 * D);
+                    const uint4 c = in[h][k];
                     v[k][0] = c.x; v[k][1] = c.y; v[k][2] = c.z; v[k][3] = c.w;
                 }
                 if (left < kKeys) {
@@ -466,6 +483,7 @@ __device__ __forceinline__ void convert_values(const ChunkParams& p, Sh& sh, uin
                         for (int c = 0; c < 8; ++c) y[k][c] = mul_f16x2(y[k][c], mul);
                 }
                 if (h == 0) {
+                    bring(1);
                     if (fine && x >= (unsigned)S::v_slots) fine = mbar_wait(&sh.v_empty[vs], (x / S::v_slots - 1) & 1, kWaitBudget);
                     fine = __all_sync(0xffffffffu, fine);
                     if (!fine) break;
@@ -675,7 +693,7 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
     auto is_split = [&](const Job& g) { return g.t * 2 * p.tokens + p.tokens >= g.B; };
 
     if (warp < kSoftmaxWarps) {
-        regs_inc<kSoftmaxRegs>();
+        regs_inc<kRegs.softmax>();
         // ================= softmax of stream i: a thread a row
         const int i = warp >> 2, quad = warp & 3, r = quad * 32 + lane;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
@@ -839,8 +857,11 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
             tc_fence_before();
         }
         if (failed && lane == 0) raise_error(p.err, kErrTimeout);
+    } else if (warp >= kConvertWarp) {
+        regs_dec<kRegs.convert>();
+        convert_values<D, false>(p, sh, smem, warp - kConvertWarp);
     } else {
-        regs_dec<kOtherRegs>();
+        regs_dec<kRegs.other>();
         if (warp == kKeyWarp) {
             bring_keys<D, false>(fp, &kmap, sh, smem);
         } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
@@ -944,10 +965,8 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                 if (!mbar_wait(&sh.drain[i], 0, kDrainBudget)) raise_error(p.err, kErrTimeout);
             }
             __syncwarp();
-        } else if (warp == kValueWarp) {
-            bring_values<D, false>(fp, &vmap, sh, smem);
         } else {
-            convert_values<D, false>(p, sh, smem, warp - kConvertWarp);
+            bring_values<D, false>(fp, &vmap, sh, smem);
         }
     }
     tc_fence_before();
@@ -1003,7 +1022,7 @@ block_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
     const uint32_t tmem = sh.tmem;
 
     if (warp < kSoftmaxWarps) {
-        regs_inc<kSoftmaxRegs>();
+        regs_inc<kBlockRegs.softmax>();
         // ================= softmax of the tiles of parity i: a thread a row
         const int i = warp >> 2, quad = warp & 3, r = quad * 32 + lane;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
@@ -1164,8 +1183,11 @@ block_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
             tc_fence_before();
         }
         if (failed && lane == 0) raise_error(p.err, kErrTimeout);
+    } else if (warp >= kConvertWarp) {
+        regs_dec<kBlockRegs.convert>();
+        convert_values<D, true>(p, sh, smem, warp - kConvertWarp);
     } else {
-        regs_dec<kOtherRegs>();
+        regs_dec<kBlockRegs.other>();
         if (warp == kKeyWarp) {
             bring_keys<D, true>(fp, &kmap, sh, smem);
         } else if (warp == kMmaWarp) {
@@ -1239,8 +1261,6 @@ block_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
             __syncwarp();
         } else if (warp == kValueWarp) {
             bring_values<D, true>(fp, &vmap, sh, smem);
-        } else if (warp >= kConvertWarp) {
-            convert_values<D, true>(p, sh, smem, warp - kConvertWarp);
         }
     }
     tc_fence_before();
