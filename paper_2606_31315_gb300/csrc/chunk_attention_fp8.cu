@@ -14,13 +14,13 @@
 // have at the end), and block_attention_fp8_kernel for calls whose work tiles all are such: blocks and single tokens.
 //
 // What bounds them (32 query and 8 KV heads of 128; times with a cold L2; floors at 6.75 TB/s and 1.93 PFLOP/s):
-//   * a prompt of 8192, 520 us of 285: a stream's chain from tile to tile, softmax 1,700 to 2,000 cycles (scores out of tensor
+//   * a prompt of 8192, 448 us of 285: a stream's chain from tile to tile, softmax 1,700 to 2,000 cycles (scores out of tensor
 //     memory 450, maximum 200, weights 900 to 1,100), the turn's 16 MMAs 1,200 and the hand-overs; two streams in turn take
-//     3,300 a pair of key tiles, 2,048 of them MMAs (which read shared memory at its full rate: 128 bytes a cycle).  A job
-//     change is 17,000 cycles, half of it the queries' way in; the query rows of a work tile are all that shares a V tile's
-//     conversion.  (A bf16 cache: 369 us, without conversions and with 16 softmax warps.)
-//   * 8 blocks of 31 over 32768 keys, 156 us of 80 (3.5 TB/s): with conversions and MMAs left out 126 to 131, a plain read of
-//     the same rows of 128 bytes 94 to 106.  (A bf16 cache: 236 us, 217 with bp_block_attention_paged.)
+//     2,900 a pair of key tiles, 2,048 of them MMAs (which read shared memory at its full rate: 128 bytes a cycle).  A job
+//     change is 17,000 cycles, half of it the queries' way in, and heads whose maxima keep growing take 3,150 a pair, which the
+//     plan does not know.  (A bf16 cache: 369 us.)
+//   * 8 blocks of 31 over 32768 keys, 142 us of 80 (3.8 TB/s): the conversion's steps one after the other, and the job changes;
+//     a plain read of the same rows of 128 bytes takes 94 to 106.  (A bf16 cache: 236 us, 217 with bp_block_attention_paged.)
 //   * one token over 2048 keys, 15 us in a graph: the plan, two copies, a tile, the merge, one after the other.
 //
 // Roles: warps 0-3 and 4-7 softmax of stream 0 and 1 (a thread a row; they read and split the queries too), warp 8 lays out
@@ -786,7 +786,7 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                     const float negm = (m == -INFINITY ? 0.f : -m) + (float)power;
                     uint64_t sum2[2] = {0ull, 0ull};
                     weigh<FACTORS>(lower, f, 0, negm, sum2, s_addr);
-                    // (their P V begins: a prompt of 8192 520 us instead of 538)
+                    // (their P V begins; a prompt of 8192, when this was built, 538 us without, 520 with)
                     tmem_st_wait();
                     tc_fence_before();
                     __syncwarp();
@@ -912,7 +912,7 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                         if (has_k) fine = mbar_wait(&sh.k_full[kslot], (xk / S::k_slots) & 1, kWaitBudget);
                         if (fine && has_v) fine = mbar_wait(&sh.v_full[vslot], (xv / S::v_slots) & 1, kWaitBudget);
                         // (the turn before the weights: a wait takes 100 to 200 cycles even where there is nothing to wait
-                        // for, and after the weights they are on the chain: 556 us instead of 538)
+                        // for, and after the weights they are on the chain: 556 us, then, instead of 538)
                         if (fine) fine = mbar_wait(&sh.turn[i], ((turn + k) & 1) ^ (i ^ 1), kWaitBudget);
                         if (fine && pv) fine = mbar_wait(&sh.half[i], my_p & 1, kWaitBudget);
                         if (!fine) break;
@@ -1002,8 +1002,8 @@ constexpr int block_smem() { return whole_sm(Shape<D, true>::tiles + (int)sizeof
 static_assert(block_smem<128>() <= 227 * 1024 && block_smem<64>() <= 227 * 1024, "a block's shared memory");
 
 // The same where every work tile has the rows of one stream: blocks and single tokens, whose keys' bytes are what counts.
-// Against the kernel above, us with a cold L2: 32 x 1 token over 8192 keys in pages of 16 150 (171), 64 x 1 over 4096 147 (168),
-// 8 x 16 over 32768 142 (145), 32 x 16 over 2048 79 (86); 8 x 31 over 32768 157 (155), 1 x 31 54 (52).  One
+// Against the kernel above, us with a cold L2: 32 x 1 token over 8192 keys in pages of 16 138 (154), 64 x 1 over 4096 142 (158),
+// 8 x 16 over 32768 132 (135), 32 x 16 over 2048 74 (79); 8 x 31 over 32768 142 (142), 1 x 31 51 (50).  One
 // accumulator; scores in three buffers, so that a tile's are there before the softmax has done with the two before it.  The
 // softmax's two groups of warps take the tiles in turn, each row's maximum handed from one tile's thread to the next one's
 // (rarely another: it is moved only where a score has outgrown it by 2^10, and the accumulator with it).
