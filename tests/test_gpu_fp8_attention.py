@@ -279,3 +279,23 @@ def test_a_cache_past_4_gib(new):
     q = torch.randn(new, 32, dim, generator=g).to(torch.bfloat16).cuda()
     far, _, _ = run(c, q, [new], [200])
     assert torch.equal(far, run(small, q, [new], [200])[0])
+
+
+@pytest.mark.parametrize("new", [1, 20, 120])
+@pytest.mark.parametrize("hkv,dim", [(2, 128), (1, 64)])
+def test_maxima_that_grow(new, hkv, dim):
+    """A row's scores rise or fall from one tile of 128 keys to the next, by less and by more than a maximum may be outgrown; the rows
+    of a warp differ, so that some move for the others' sake."""
+    c, q, lens = make([1900], [new], 4 * hkv, hkv, dim, 64, seed=5, spread=6)
+    g = torch.Generator().manual_seed(6)
+    keys = torch.arange(lens[0])
+    at = (c["table"][0].cpu().long()[keys // 64] * 64 + keys % 64).cuda()
+    k = 0.5 * torch.randn(lens[0], hkv, dim, generator=g)
+    k[:, :, 0] = (keys // 128 + 1).float()[:, None]  # (up to 16: e4m3 numbers)
+    c["k"].view(torch.uint8)[at] = k.to(torch.float8_e4m3fn).view(torch.uint8).cuda()
+    c["k_scale"].fill_(127)
+    steps = torch.tensor([3.0, -3.0, 9.0, 9.9, -9.0, 11.0, -11.0, 40.0, 0.0, -40.0, 5.0])  # of a tile, in powers of two
+    row = torch.arange(q.shape[0] * q.shape[1]).view(q.shape[0], q.shape[1])
+    q[:, :, 0] = (steps[row % len(steps)] * math.sqrt(dim) * math.log(2)).to(torch.bfloat16).cuda()
+    check(c, q, [new], lens)
+    check(c, q, [new], lens, window=700)
