@@ -243,19 +243,22 @@ __device__ __forceinline__ bool sees_nan(const Fp8Params& fp, const Job& g, int 
 
 // The boxes that a job's key tiles come in, one a page or, of larger pages, one a tile: looked up by a whole warp, 32 boxes (a
 // batch) at a time and a lane each, the next ones in flight meanwhile.  (Tile by tile, table and then scale, they alone took 1.5 us
-// a tile.)  A job begins a new batch.
+// a tile.)  A job begins a new batch.  SCALES: one, or the keys' and the values'.
+template <int SCALES>
 struct Boxes {
     const ChunkParams& p;
-    const uint8_t* scale;
+    const uint8_t* scale[SCALES];
     const Job& g;
     int rows, of_tile, ahead;  // keys of a box; boxes of a tile; tiles of a batch
     int row;                   // this lane's box of the batch at hand: its first key's row in the pool (-1: none)
-    uint32_t exponent;         // and its scale
+    uint32_t exponent[SCALES]; // and its scales
     int far_id;                // of the next batch
-    uint32_t far_exponent;
+    uint32_t far_exponent[SCALES];
 
-    __device__ __forceinline__ Boxes(const ChunkParams& params, const uint8_t* scales, const Job& job)
-        : p(params), scale(scales), g(job), rows(min(kKeys, 1 << params.page_shift)), of_tile(kKeys / rows), ahead(32 / of_tile) {
+    __device__ __forceinline__ Boxes(const ChunkParams& params, const Job& job, const uint8_t* first, const uint8_t* second = nullptr)
+        : p(params), g(job), rows(min(kKeys, 1 << params.page_shift)), of_tile(kKeys / rows), ahead(32 / of_tile) {
+        scale[0] = first;
+        if constexpr (SCALES > 1) scale[1] = second;
         look_up(g.j0);
     }
     __device__ __forceinline__ int key_of(int j) const {
@@ -265,25 +268,36 @@ struct Boxes {
     __device__ __forceinline__ void look_up(int j) {
         const int key = key_of(j), pg = key >> p.page_shift;
         far_id = -1;
-        far_exponent = 127;
+#pragma unroll
+        for (int i = 0; i < SCALES; ++i) far_exponent[i] = 127;
         if (key / kKeys < g.j1 && key < g.n) {
             far_id = pg < p.pages_per_seq ? __ldg(p.block_table + (size_t)g.s * p.pages_per_seq + pg) : -1;
             if ((unsigned)far_id >= (unsigned)p.num_pages) {
                 raise_error(p.err, kErrDeviceArg);
                 far_id = 0;
             }
-            far_exponent = __ldg(scale + (size_t)far_id * p.num_kv_heads + g.h);
+#pragma unroll
+            for (int i = 0; i < SCALES; ++i) far_exponent[i] = __ldg(scale[i] + (size_t)far_id * p.num_kv_heads + g.h);
         }
     }
     // The batch that begins with tile j.
     __device__ __forceinline__ void next(int j) {
         row = far_id < 0 ? -1 : (far_id << p.page_shift) + (key_of(j) & ((1 << p.page_shift) - 1));
-        exponent = far_exponent;
-        if (exponent == 255) {
-            raise_error(p.err, kErrDeviceArg);
-            exponent = 254;
+#pragma unroll
+        for (int i = 0; i < SCALES; ++i) {
+            exponent[i] = far_exponent[i];
+            if (exponent[i] == 255) {
+                raise_error(p.err, kErrDeviceArg);
+                exponent[i] = 254;
+            }
         }
         look_up(j + ahead);
+    }
+    // The largest of the values' scales (the last ones looked up) in the tile of this lane's box.
+    __device__ __forceinline__ uint32_t tile_ref() const {
+        uint32_t ref = row >= 0 ? max(exponent[SCALES - 1], kLeastRef) : kLeastRef;
+        for (int o = 1; o < of_tile; o <<= 1) ref = max(ref, __shfl_xor_sync(0xffffffffu, ref, o));
+        return ref;
     }
     // The keys of tile j's boxes.
     __device__ __forceinline__ uint32_t keys(int j) const { return min(of_tile, (g.n - j * kKeys + rows - 1) / rows) * rows; }
@@ -309,7 +323,9 @@ __device__ __forceinline__ void had_job(Sh& sh, unsigned& nj) {
     ++nj;
 }
 
-// A warp's role: this CTA's part of the line, laid out in jobs; K tiles of codes through their ring.
+// A warp's role: this CTA's part of the line, laid out in jobs; K tiles of codes through their ring.  It brings all that the
+// softmax reads of the scales, the values' too: a tile's arrival on k_full is what its scores wait for, while V's copies (and what
+// their warp writes) may come later than those.
 template <int D, bool FEW, class Sh>
 __device__ __forceinline__ void bring_keys(const Fp8Params& fp, const CUtensorMap* kmap, Sh& sh, uint8_t* smem) {
     using S = Shape<D, FEW>;
@@ -341,10 +357,11 @@ __device__ __forceinline__ void bring_keys(const Fp8Params& fp, const CUtensorMa
         lay_out(after);  // one ahead of the copies
         if (!ok) break;
         if (have && g.j1 > g.j0) {
-            Boxes box(p, fp.k_scale, g);
+            Boxes<2> box(p, g, fp.k_scale, fp.v_scale);
             for (int j = g.j0; j < g.j1 && ok; ++batch) {
                 box.next(j);
-                sh.k_exp[batch % kBatches][lane] = (uint8_t)box.exponent;
+                sh.k_exp[batch % kBatches][lane] = (uint8_t)box.exponent[0];
+                sh.v_ref[batch % kBatches][lane] = (uint8_t)box.tile_ref();
                 __syncwarp();
                 for (int k = 0; k < box.ahead && j < g.j1; ++k, ++j, ++x) {
                     const int slot = x % S::k_slots;
@@ -383,13 +400,11 @@ __device__ __forceinline__ void bring_values(const Fp8Params& fp, const CUtensor
         if (g.first && !g.last)
             left = make_int4(left.x | kHasTail, g.q0 + g.t * 2 * p.tokens, min(2 * p.tokens, g.B - g.t * 2 * p.tokens), g.h);
         if (g.j1 <= g.j0) continue;
-        Boxes box(p, fp.v_scale, g);
+        Boxes<1> box(p, g, fp.v_scale);
         for (int j = g.j0; j < g.j1 && fine; ++batch) {
             box.next(j);
-            uint32_t ref = box.row >= 0 ? max(box.exponent, kLeastRef) : kLeastRef;
-            for (int o = 1; o < box.of_tile; o <<= 1) ref = max(ref, __shfl_xor_sync(0xffffffffu, ref, o));
-            sh.v_ref[batch % kBatches][lane] = (uint8_t)ref;
-            sh.v_below[batch % kBatches][lane] = (uint8_t)(box.row >= 0 ? ref - box.exponent : 0u);
+            const uint32_t ref = box.tile_ref();
+            sh.v_below[batch % kBatches][lane] = (uint8_t)(box.row >= 0 ? ref - box.exponent[0] : 0u);
             __syncwarp();
             for (int k = 0; k < box.ahead && j < g.j1; ++k, ++j, ++x) {
                 const int slot = x % S::raw_slots;

@@ -1,0 +1,53 @@
+"""What the warps of the attention over a cache in 8 bits hand to one another: scales, row maxima and sums that differ from job to job,
+so that one taken before it is there, or from another job, shows as a wrong power of two."""
+import pytest
+import torch
+
+import paper_2606_31315_gb300 as bp
+from _fp8 import attention, random_cache
+
+pytestmark = pytest.mark.gpu
+
+
+def offsets(lengths):
+    return torch.tensor([0, *torch.tensor(lengths).cumsum(0).tolist()], dtype=torch.int32, device="cuda")
+
+
+def make(ctxs, news, hq, hkv, dim, page, seed, spread):
+    g = torch.Generator().manual_seed(seed)
+    lens = [c + n for c, n in zip(ctxs, news)]
+    c = random_cache(g, lens, hkv, dim, page, spread)
+    # (rows of sizes from 2^-6 to 2: what one row says of its size is not another's)
+    size = torch.pow(2.0, torch.randint(-6, 2, (sum(news), hq, 1), generator=g).float())
+    q = (torch.randn(sum(news), hq, dim, generator=g) * size).to(torch.bfloat16).cuda()
+    return c, q, lens
+
+
+def check(c, q, news, lens, times=3, cold=()):
+    """The call, some times over, against 64 bits; `cold`: tensors that are not in L2 when it begins, the others are."""
+    hkv = c["k"].shape[1]
+    ws = bp.workspace(bp.chunk_attention_workspace_size(len(news), len(q), q.shape[1], hkv, q.shape[2]), "cuda")
+    o, z, bound, z_bound = attention(c, q, news, lens, True, 0)
+    cu_q, cu_kv = offsets(news), offsets(lens)
+    flush = torch.empty(64 << 20, device="cuda")
+    for _ in range(times):
+        if cold:
+            flush.zero_()
+            for name, x in c.items():
+                if torch.is_tensor(x) and name not in cold:
+                    x.view(torch.uint8).sum()
+        out, lse = torch.full(q.shape, 7.0, device="cuda", dtype=torch.bfloat16), torch.full(q.shape[:2], 7.0, device="cuda")
+        bp.chunk_attention_paged_fp8(q, c["k"], c["k_scale"], c["v"], c["v_scale"], cu_q, cu_kv, c["table"], c["page"], max(news),
+                                     max(lens), out=out, lse=lse, ws=ws)
+        assert bp.get_status(ws) == 0
+        assert ((out.double() - o).abs() <= bound).all() and ((lse.double() - z).abs() <= z_bound).all()
+
+
+@pytest.mark.parametrize("new", [1, 16, 100])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_scales_of_values_that_come_late(new, page, dim):
+    """The values' scales come from memory, all else from L2: they may be the last to be there."""
+    ctxs = [3 + 97 * s % 1500 for s in range(24)]
+    c, q, lens = make(ctxs, [new] * 24, 8, 2, dim, page, 11, 6)
+    check(c, q, [new] * 24, lens, cold=("v_scale", "v"))
