@@ -702,8 +702,13 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
     const int G = p.group;
     if (!begin<D, false>(p, &kmap, &vmap, sh, smem, 2)) return;
     const uint32_t tmem = sh.tmem;
-    // of a split job's streams, row maxima and sums: where the second query tile is otherwise
-    float2 (*const row)[kTileM] = reinterpret_cast<float2 (*)[kTileM]>(smem + S::q_bytes);
+    // Of a split job's streams, a row's maximum and sum: where the second query tile is otherwise, those of 32 rows where these rows'
+    // queries are.  The two warps that have the rows write and read both, and their barriers are the only ones in between.
+    constexpr int kRowsBytes = 32 * 128;  // of 32 rows of a query tile (its first part)
+    static_assert(2 * 32 * sizeof(float2) <= kRowsBytes && 4 * kRowsBytes <= S::q_bytes, "a warp's rows hold them");
+    auto row = [&](int stream, int r) -> float2& {
+        return reinterpret_cast<float2*>(smem + S::q_bytes + (r >> 5) * kRowsBytes)[stream * 32 + (r & 31)];
+    };
     // whether a job's rows are one stream's: then both take them, and every other key tile
     auto is_split = [&](const Job& g) { return g.t * 2 * p.tokens + p.tokens >= g.B; };
 
@@ -744,9 +749,9 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                 uint32_t top = 0;
                 if (mine == i) top = split_queries<D>(fp.q, at, smem + i * S::q_bytes + quad * 32 * 128);
                 if (split) {  // (the other stream's threads learn of it)
-                    if (i == 0) row[0][r].x = __uint_as_float(top);
+                    if (i == 0) row(0, r).x = __uint_as_float(top);
                     named_barrier(1 + quad, 64);
-                    if (i == 1) top = __float_as_uint(row[0][r].x);
+                    if (i == 1) top = __float_as_uint(row(0, r).x);
                 }
                 // the row times 2^(7 - e) is below 256; 2^(e - 7) of it is put back with the softmax's scale
                 row_scale = p.scale_log2 * __uint_as_float((max(top >> 7, 8u) - 7) << 23);
@@ -836,14 +841,14 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
             bool others_some = false;
             if (split) {
                 // ---- the other stream's part of these rows, merged as the second kernel merges CTAs' parts
-                row[i][r] = make_float2(m, l);
+                row(i, r) = make_float2(m, l);
                 if (lane == 0) sh.row_ref[i][quad] = some ? ref : 0;
                 if (named_barrier_or(1 + quad, 64, failed)) {
                     failed = true;
                     continue;
                 }
                 others_some = a + (i ^ 1) < b;
-                const float2 o = row[i ^ 1][r];
+                const float2 o = row(i ^ 1, r);
                 const float top = fmaxf(m, o.x);
                 const float u = m == top ? 1.f : chunk_exp2(m - top), v = o.x == top ? 1.f : chunk_exp2(o.x - top);
                 l = i == 0 ? l * u + o.y * v : o.y * v + l * u;

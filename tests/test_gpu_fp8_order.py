@@ -51,3 +51,14 @@ def test_scales_of_values_that_come_late(new, page, dim):
     ctxs = [3 + 97 * s % 1500 for s in range(24)]
     c, q, lens = make(ctxs, [new] * 24, 8, 2, dim, page, 11, 6)
     check(c, q, [new] * 24, lens, cold=("v_scale", "v"))
+
+
+@pytest.mark.parametrize("hq,hkv,dim", [(32, 8, 128), (8, 8, 64), (12, 4, 128)])
+@pytest.mark.parametrize("more", [1, 9, 30])
+def test_tiles_of_one_stream_among_others(hq, hkv, dim, more):
+    """Many work tiles to a CTA, by turns of both streams and of one, which both streams then share: the rows' maxima and sums of
+    those lie where the others' queries are."""
+    tile = 2 * (128 * hkv // hq)
+    news = [tile + more if s % 3 else more for s in range(60)]
+    c, q, lens = make([17 * s % 300 for s in range(60)], news, hq, hkv, dim, 32, 12, 3)
+    check(c, q, news, lens)
