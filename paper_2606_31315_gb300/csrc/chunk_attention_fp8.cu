@@ -748,10 +748,10 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                 const int64_t at = active ? (int64_t)(g->q0 + tok) * fp.q_stride + (g->h * G + r - my_tok * G) * D : -1;
                 uint32_t top = 0;
                 if (mine == i) top = split_queries<D>(fp.q, at, smem + i * S::q_bytes + quad * 32 * 128);
-                if (split) {  // (the other stream's threads learn of it)
-                    if (i == 0) row(0, r).x = __uint_as_float(top);
+                if (split) {  // (the other stream's threads learn of it, where they themselves write their sums later)
+                    if (i == 0) row(1, r).x = __uint_as_float(top);
                     named_barrier(1 + quad, 64);
-                    if (i == 1) top = __float_as_uint(row(0, r).x);
+                    if (i == 1) top = __float_as_uint(row(1, r).x);
                 }
                 // the row times 2^(7 - e) is below 256; 2^(e - 7) of it is put back with the softmax's scale
                 row_scale = p.scale_log2 * __uint_as_float((max(top >> 7, 8u) - 7) << 23);
@@ -1005,7 +1005,8 @@ struct BlockShared : Common<D, true> {
     uint64_t decided[4][2];                          // of 32 rows, by the tile's parity: what follows is as after it
     float top[kTileM];                               // of a row: its maximum so far
     int ref[4];                                      // the values' power so far (the same in all of them)
-    float row[2][kTileM];                            // of the two groups of warps: at the end row sums
+    float row[2][kTileM];                            // of the two groups of warps: at the end row sums (before that the second has
+                                                     // the size of a row's queries)
     __device__ void init() {
         mbar_init(&q_ready, 4);
         mbar_init(&drain, 1);
@@ -1072,15 +1073,16 @@ block_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
             float m = -INFINITY, l = 0.f, row_scale = 1.f;
             if (tiles > 0) {
                 if (!idle) {
-                    // ---- the queries of these rows, two parts each, to shared memory; the other group learns of their size
+                    // ---- the queries of these rows, two parts each, to shared memory; the other group learns of their size,
+                    // where it writes its sums itself later (this group's may be there before it has read that)
                     uint32_t top = 0;
                     if (i == 0) {
                         const int64_t at = active ? (int64_t)(g->q0 + tok) * fp.q_stride + (g->h * G + r - my_tok * G) * D : -1;
                         top = split_queries<D>(fp.q, at, smem + quad * 32 * 128);
-                        sh.row[0][r] = __uint_as_float(top);
+                        sh.row[1][r] = __uint_as_float(top);
                     }
                     named_barrier(1 + quad, 64);
-                    if (i == 1) top = __float_as_uint(sh.row[0][r]);
+                    if (i == 1) top = __float_as_uint(sh.row[1][r]);
                     // the row times 2^(7 - e) is below 256; 2^(e - 7) of it is put back with the softmax's scale
                     row_scale = p.scale_log2 * __uint_as_float((max(top >> 7, 8u) - 7) << 23);
                     if (top >= 0x7f80u && hi > lo) l = __uint_as_float(0x7fc00000u);  // a NaN or an infinity: the row is none

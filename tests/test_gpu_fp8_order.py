@@ -62,3 +62,19 @@ def test_tiles_of_one_stream_among_others(hq, hkv, dim, more):
     news = [tile + more if s % 3 else more for s in range(60)]
     c, q, lens = make([17 * s % 300 for s in range(60)], news, hq, hkv, dim, 32, 12, 3)
     check(c, q, news, lens)
+
+
+@pytest.mark.parametrize("hq,hkv,dim", [(32, 8, 128), (8, 2, 64), (12, 12, 128)])
+def test_blocks_of_a_single_key_tile(hq, hkv, dim):
+    """Jobs that are over after one tile, many to a CTA: a row's sum is there while its queries' size is still handed on."""
+    news = [1 + s % 16 for s in range(200)]
+    c, q, lens = make([11 * s % 112 for s in range(200)], news, hq, hkv, dim, 16, 13, 3)
+    check(c, q, news, lens)
+
+
+@pytest.mark.parametrize("hkv,dim", [(2, 128), (4, 64)])
+def test_chunks_of_a_single_key_tile(hkv, dim):
+    """The same of tiles that two streams share, in the kernel for longer chunks."""
+    news = [1 + s % 20 for s in range(199)] + [70]
+    c, q, lens = make([11 * s % 100 for s in range(200)], news, 4 * hkv, hkv, dim, 16, 14, 3)
+    check(c, q, news, lens)
