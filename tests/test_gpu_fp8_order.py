@@ -28,6 +28,11 @@ def check(c, q, news, lens, times=3, cold=()):
     hkv = c["k"].shape[1]
     ws = bp.workspace(bp.chunk_attention_workspace_size(len(news), len(q), q.shape[1], hkv, q.shape[2]), "cuda")
     o, z, bound, z_bound = attention(c, q, news, lens, True, 0)
+    # (`bound` is of what fp16 holds in 11 bits.  A weight times 2^5 at least, where the row's largest is 1 at least, is off by half of
+    # fp16's least step, 2^-25: 2^-30 of the row's sum for each of its keys, times a value of at most 448 2^(b - 127).  Rows whose
+    # scores are hundreds apart have columns with nothing else)
+    most = torch.pow(2.0, c["v_scale"].double().amax(0) - 127).repeat_interleave(q.shape[1] // hkv)
+    bound = bound + max(lens) * 2.0 ** -30 * 448 * most[None, :, None]
     cu_q, cu_kv = offsets(news), offsets(lens)
     flush = torch.empty(64 << 20, device="cuda")
     for _ in range(times):
@@ -40,7 +45,8 @@ def check(c, q, news, lens, times=3, cold=()):
         bp.chunk_attention_paged_fp8(q, c["k"], c["k_scale"], c["v"], c["v_scale"], cu_q, cu_kv, c["table"], c["page"], max(news),
                                      max(lens), out=out, lse=lse, ws=ws)
         assert bp.get_status(ws) == 0
-        assert ((out.double() - o).abs() <= bound).all() and ((lse.double() - z).abs() <= z_bound).all()
+        over, z_over = float(((out.double() - o).abs() / bound).max()), float(((lse.double() - z).abs() / z_bound).max())
+        assert over <= 1 and z_over <= 1, (over, z_over)
 
 
 @pytest.mark.parametrize("new", [1, 16, 100])
