@@ -249,8 +249,11 @@ BP_API int bp_chunk_attention_paged(const void* q, int64_t q_stride, const void*
  * Rows from cu_new[num_seqs] on are padding.  A page may belong to one sequence of the call.  workspace: at least 256 bytes.
  *
  * bp_chunk_attention_paged_fp8 is bp_chunk_attention_paged over such a cache: the same arguments, limits, masks, workspace
- * size and errors.  Nothing is rounded that a bf16 cache of the same values would not round.  A key or a value that is not
- * a number makes the rows that see it NaN (whole, with their lse), and no others.  A scale of 255 sets BP_ERR_DEVICE_FLAG.
+ * size and errors.  A weight times its value's scale is rounded to 11 bits, or by up to 2^-29 of the row's largest such
+ * product: of the keys that the row sees, so that hidden ones cost it nothing.  Values lose bits where their scale is more than
+ * 2^75 below another one's of the sequence and head.  Scores are to be below 2^22 in size (fp32 has no fraction left for them
+ * further on); a row with larger ones may be NaN.  A key or a value that is not a number makes the rows that see it NaN (whole,
+ * with their lse), and no others.  A scale of 255 sets BP_ERR_DEVICE_FLAG.
  * ------------------------------------------------------------------------------- */
 BP_API int bp_kv_append_fp8(void* k_cache, void* k_scale, void* v_cache, void* v_scale, const void* k_new, int64_t k_stride,
                             const void* v_new, int64_t v_stride, const int32_t* cu_new, const int32_t* cu_kv,

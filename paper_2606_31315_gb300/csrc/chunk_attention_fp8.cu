@@ -3,12 +3,11 @@
 //
 //   O_i = sum_j softmax_j(scale <q_i, 2^a k_j>) 2^b v_j      a, b: of key j's page
 //
-// Nothing is rounded that a bf16 cache would not round:
 //   * S = Q K^T on the codes as they lie in memory, kind::f8f6f4.  A query row, scaled by a power of two to at most 256, is the
 //     sum of two e4m3 numbers: bf16's 8 bits are twice 4.  (Elements below 2^-9 of the row's largest lose what is under
 //     2^-16 of it.)  The row's and the page's powers multiply the scores in the softmax.
 //   * P V in fp16, which holds every e4m3 number; four warps turn a tile's codes into them, in shared memory.  The weights take
-//     the values' powers of two.
+//     the values' powers of two, and are rounded to 11 bits, or at 2^-29 of the row's largest.
 // The line of work and the merge are chunk_attention.cu's.  Two kernels: chunk_attention_fp8_kernel for any call, its two streams a
 // query tile each (where a work tile has the rows of one only, both take them, and every other key tile, and add what they
 // have at the end), and block_attention_fp8_kernel for calls whose work tiles all are such: blocks and single tokens.
@@ -99,21 +98,35 @@ struct Common {
     uint64_t k_full[S::k_slots], k_empty[S::k_slots], raw_full[S::raw_slots], raw_empty[S::raw_slots];
     uint64_t v_full[S::v_slots], v_empty[S::v_slots];
     uint64_t job_full[kJobs], job_empty[kJobs];
-    // The scales of the boxes (Boxes), 32 at a time: of keys; of values how far below the largest one of their tile, as
-    // powers of two, and that one.  Biased exponents.
-    uint8_t k_exp[kBatches][32], v_below[kBatches][32], v_ref[kBatches][32];
+    // The scales of the boxes (Boxes), 32 at a time: of keys, bf16 numbers; of values biased exponents, what the weights take of theirs, the least
+    // of that in the box's tile, and what is left for the values themselves.
+    alignas(16) uint16_t k_power[kBatches][32];
+    alignas(8) uint8_t v_exp[kBatches][32], v_low[kBatches][32], v_below[kBatches][32];
     Job job[kJobs];
     int job_nan[kJobs];                              // a code among its values is not a number
     uint32_t tmem;
 };
 
-// The values' powers of two: a tile's are held against its largest one (below 2^-24 of it they are 0; fp16 has e4m3's 18
-// powers and 22 more), and that one against the largest so far, `ref`: the weights take the difference, times 2^5.  A row's
-// maximum is moved where a score has outgrown it by 2^10, so that they are at most 2^15 in fp16.  Under 2^-19 of the weight of
-// the row's maximum they lose bits, and what is left out, under 2^-30 of it each, is 2^-10 of the row after 2^20 keys.  (Moves by 2^8
-// and weights times 2^7: a prompt of 8192 490 us instead of 480, by 2^12 and times 2^3 470.)  A tile whose values are 2^-12 of
-// others' still has all its weights' bits down to 2^-7.
-constexpr uint32_t kLeastRef = 15;  // of a tile, so that the accumulator's power is a number too
+// The values' powers of two, 2^(e - 127): the weights take them, so that P V has the values as their codes say.  With a row's
+// scores x (in powers of two) and e of their keys, M near the largest x + e that the row has seen, and m near its largest x,
+//
+//   P = 2^(x + e - M + 5)    O = 2^(M - m - 132) sum P code    l = sum 2^(x - m), of the same exponentials
+//
+// What a row cannot see has no part in its M: hidden keys cost it no bits.  M and m are whole numbers.  M is moved where x + e
+// has outgrown it by 2^10 (and a half, for top_score's rounding), so that P is below 2^16 in fp16; m where x + e less the tile's least
+// e has, which may put it 2^kReach above the largest x.  P has all its 11 bits from 2^-18 of the row's largest on (that is
+// 2^4 at least), and below is off by 2^-29 of it (2^-25 in fp16): 2^-11 of a row after 2^18 keys.  (Moves at 2^8 and P times 2^7: a
+// prompt of 8192 490 us instead of 480, at 2^12 and times 2^3 470.)
+//
+// l has to be exact where P is not.  In fp32 an exponential is there down to 2^-126, so e is held within 2^-kReach of the
+// largest of the job's scales so far, which leaves what is 2^-60 of a row's largest weight.  What a scale lies below that is
+// multiplied into its values, which fp16 holds to 2^-24 (a code whole down to 2^-15).  It happens in pages of zeros.
+//
+// With one power a tile for all of its values, and the weights against the largest so far, pages of 16 were 5 % faster (32 x 1 token
+// over 8192 keys 142 us instead of 151, chunks among decoding sequences 117 instead of 123, others the same), but a page of
+// large values that a row could not see took its bits.
+constexpr uint32_t kReach = 60;
+constexpr uint32_t kLeastExp = 15;  // and no lower, so that O's power is a number in fp32 (the codes have 2^-15, as said)
 
 // 2^(e - 127) of a biased exponent below 255.
 __device__ __forceinline__ float power_of(uint32_t e) { return __uint_as_float(e ? e << 23 : 0x400000u); }
@@ -252,6 +265,7 @@ struct Boxes {
     int rows, of_tile, ahead;  // keys of a box; boxes of a tile; tiles of a batch
     int row;                   // this lane's box of the batch at hand: its first key's row in the pool (-1: none)
     uint32_t exponent[SCALES]; // and its scales
+    uint32_t most = 0;         // the largest of the values' ones so far (the last that are looked up)
     int far_id;                // of the next batch
     uint32_t far_exponent[SCALES];
 
@@ -291,13 +305,18 @@ struct Boxes {
                 exponent[i] = 254;
             }
         }
+        most = max(most, __reduce_max_sync(0xffffffffu, row >= 0 ? exponent[SCALES - 1] : 0u));
         look_up(j + ahead);
     }
-    // The largest of the values' scales (the last ones looked up) in the tile of this lane's box.
-    __device__ __forceinline__ uint32_t tile_ref() const {
-        uint32_t ref = row >= 0 ? max(exponent[SCALES - 1], kLeastRef) : kLeastRef;
-        for (int o = 1; o < of_tile; o <<= 1) ref = max(ref, __shfl_xor_sync(0xffffffffu, ref, o));
-        return ref;
+    // What the weights take of this lane's scale of values.
+    __device__ __forceinline__ uint32_t of_weights() const {
+        return max(max(exponent[SCALES - 1], kLeastExp), most > kReach ? most - kReach : 0u);
+    }
+    // The least of it in the box's tile.
+    __device__ __forceinline__ uint32_t least_of_weights() const {
+        uint32_t least = row >= 0 ? of_weights() : 255u;
+        for (int o = 1; o < of_tile; o <<= 1) least = min(least, __shfl_xor_sync(0xffffffffu, least, o));
+        return least;
     }
     // The keys of tile j's boxes.
     __device__ __forceinline__ uint32_t keys(int j) const { return min(of_tile, (g.n - j * kKeys + rows - 1) / rows) * rows; }
@@ -360,8 +379,10 @@ __device__ __forceinline__ void bring_keys(const Fp8Params& fp, const CUtensorMa
             Boxes<2> box(p, g, fp.k_scale, fp.v_scale);
             for (int j = g.j0; j < g.j1 && ok; ++batch) {
                 box.next(j);
-                sh.k_exp[batch % kBatches][lane] = (uint8_t)box.exponent[0];
-                sh.v_ref[batch % kBatches][lane] = (uint8_t)box.tile_ref();
+                sh.k_power[batch % kBatches][lane] = (uint16_t)(__float_as_uint(power_of(box.exponent[0])) >> 16);
+                const uint32_t least = box.least_of_weights();
+                sh.v_exp[batch % kBatches][lane] = (uint8_t)(box.row >= 0 ? box.of_weights() : least);
+                sh.v_low[batch % kBatches][lane] = (uint8_t)least;
                 __syncwarp();
                 for (int k = 0; k < box.ahead && j < g.j1; ++k, ++j, ++x) {
                     const int slot = x % S::k_slots;
@@ -403,8 +424,7 @@ __device__ __forceinline__ void bring_values(const Fp8Params& fp, const CUtensor
         Boxes<1> box(p, g, fp.v_scale);
         for (int j = g.j0; j < g.j1 && fine; ++batch) {
             box.next(j);
-            const uint32_t ref = box.tile_ref();
-            sh.v_below[batch % kBatches][lane] = (uint8_t)(box.row >= 0 ? ref - box.exponent[0] : 0u);
+            sh.v_below[batch % kBatches][lane] = (uint8_t)(box.of_weights() - box.exponent[0]);
             __syncwarp();
             for (int k = 0; k < box.ahead && j < g.j1; ++k, ++j, ++x) {
                 const int slot = x % S::raw_slots;
@@ -591,27 +611,41 @@ __device__ __forceinline__ bool begin(const ChunkParams& p, const CUtensorMap* k
     return true;
 }
 
-// What both softmaxes do with a tile's scores.  Weights 2^(f * score - m) of a row's columns [64 h, 64 h + 64), x, times 2^power
-// with `negm` = power - m: in pairs, fp16 as the converted values are, to tensor memory at `to`; their sums.
-template <int FACTORS>
-__device__ __forceinline__ void weigh(const uint32_t (&x)[4][16], const float (&f)[FACTORS], int h, float negm, uint64_t (&sum2)[2], uint32_t to) {
-    const uint64_t negm2 = pack_f32x2(negm, negm);
+// M and m of a row that has seen nothing: below every score, and a number, so that no weight needs a test.
+constexpr float kNothing = -3.0e38f;
+// A whole number below 2^8 as 2^23 more, from its bits alone (a conversion would take the exponentials' pipe).
+__device__ __forceinline__ float plus_2_23(uint32_t e) { return __uint_as_float(0x4b000000u | e); }
+
+// What both softmaxes do with a tile's scores.  P = 2^(f * x + e + base) of a row's columns [64 h, 64 h + 64), in pairs, fp16 as the
+// converted values are, to tensor memory at `to`; their sums times 2^(low - e) to sum2.  The e as plus_2_23, at least low; base
+// is 2^23 lower.  APART: the 64 columns have one e, which their sum takes at the end (the block kernel with large pages, 64 x 1 tokens over
+// 4096 keys, 142 us and 146 with each pair's own; the other kernel the other way round, a prompt of 8192 459 and 443).
+template <int FACTORS, bool APART>
+__device__ __forceinline__ void weigh(const uint32_t (&x)[4][16], const float (&f)[FACTORS], const float (&e)[FACTORS], int h, float base,
+                                      uint32_t low, uint64_t (&sum2)[2], uint32_t to) {
+    static_assert(!APART || FACTORS == 2, "one e");
+    uint64_t apart[2] = {0ull, 0ull};
+    // 2^(low - e): of e's bits the lowest 8 are left, at the exponent's place
+    auto below = [&](int i) { return __uint_as_float(((127 + low) << 23) + __float_as_uint(e[i]) * 0xff800000u); };
 #pragma unroll
     for (int c = 0; c < 4; c += 2) {
         uint32_t pk[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const float factor = f[(h * 4 + c + (e >> 3)) * FACTORS / 8];
-            const uint32_t* y = &x[c + (e >> 3)][2 * (e & 7)];
+        for (int k = 0; k < 16; ++k) {
+            const int block = c + (k >> 3), i = (h * 4 + block) * FACTORS / 8;
+            const float factor = f[i], add = base + e[i], part = below(i);
+            const uint32_t* y = &x[block][2 * (k & 7)];
             float u, w;
-            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(y[0]), __uint_as_float(y[1])), pack_f32x2(factor, factor), negm2), u, w);
+            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(y[0]), __uint_as_float(y[1])), pack_f32x2(factor, factor), pack_f32x2(add, add)), u, w);
             u = chunk_exp2(u);
             w = chunk_exp2(w);
-            sum2[e & 1] = add_f32x2(sum2[e & 1], pack_f32x2(u, w));
-            pk[e] = pack_f16x2(u, w);  // 11 bits
+            if constexpr (APART) apart[k & 1] = add_f32x2(apart[k & 1], pack_f32x2(u, w));
+            else sum2[k & 1] = fma_f32x2(pack_f32x2(u, w), pack_f32x2(part, part), sum2[k & 1]);
+            pk[k] = pack_f16x2(u, w);  // 11 bits
         }
         tmem_st16(to + h * 32 + c * 8, pk);
     }
+    if constexpr (APART) sum2[0] = fma_f32x2(add_f32x2(apart[0], apart[1]), pack_f32x2(below(h), below(h)), sum2[0]);
 }
 // Scores of columns [64 h, 64 h + 64) at `at`, those outside [from, to) struck out unless the whole tile is seen; the maxima
 // of 16 columns each.
@@ -635,22 +669,74 @@ __device__ __forceinline__ void take_scores(uint32_t at, int h, bool full, int f
         }
     }
 }
-// The largest of a row's scores times their factors, of the 16 columns' maxima.
-template <int FACTORS>
-__device__ __forceinline__ float top_score(const float (&lower)[4], const float (&upper)[4], const float (&f)[FACTORS]) {
-    float top = -INFINITY;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-        if constexpr (FACTORS == 2) {
-            if (c % 4 == 0) {
-                const float (&m)[4] = c ? upper : lower;
-                top = fmaxf(top, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * f[c / 4]);
-            }
+// The factors of a tile's scores and the values' powers, of kKeys / FACTORS keys each; the tile's boxes begin at place `at` of the
+// batch.  Factors are finite and above 0, so that a hidden column's -inf stays one.
+template <int FACTORS, class Sh>
+__device__ __forceinline__ void take_scales(const Sh& sh, unsigned batch, int at, int box_shift, float row_scale, float (&f)[FACTORS], float (&e)[FACTORS]) {
+    auto factor = [&](uint32_t power) { return fmaxf(fminf(row_scale * __uint_as_float(power), 3.4e38f), 1.2e-38f); };
+    if constexpr (FACTORS == 8) {  // pages of 16 or 32: of their 8 or 4 boxes at once
+        uint32_t k[4], v[2];
+        if (box_shift == 4) {
+            const uint4 a = *reinterpret_cast<const uint4*>(&sh.k_power[batch][at]);
+            const uint2 b = *reinterpret_cast<const uint2*>(&sh.v_exp[batch][at]);
+            k[0] = a.x, k[1] = a.y, k[2] = a.z, k[3] = a.w, v[0] = b.x, v[1] = b.y;
         } else {
-            top = fmaxf(top, (c < 4 ? lower[c & 3] : upper[c & 3]) * f[c]);
+            const uint2 a = *reinterpret_cast<const uint2*>(&sh.k_power[batch][at]);
+            const uint32_t b = *reinterpret_cast<const uint32_t*>(&sh.v_exp[batch][at]);
+            k[0] = __byte_perm(a.x, 0, 0x1010), k[1] = __byte_perm(a.x, 0, 0x3232), k[2] = __byte_perm(a.y, 0, 0x1010), k[3] = __byte_perm(a.y, 0, 0x3232);
+            v[0] = __byte_perm(b, 0, 0x1100), v[1] = __byte_perm(b, 0, 0x3322);
+        }
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            f[c] = factor(c & 1 ? k[c >> 1] & 0xffff0000u : k[c >> 1] << 16);
+            e[c] = __uint_as_float(__byte_perm(v[c >> 2], 0x4b000000u, 0x7540 | (c & 3)));  // plus_2_23
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < FACTORS; ++c) {
+            const int box = at + (c * (kKeys / FACTORS) >> box_shift);
+            f[c] = factor((uint32_t)sh.k_power[batch][box] << 16);
+            e[c] = plus_2_23(sh.v_exp[batch][box]);
         }
     }
+}
+// The largest of a row's scores times their factors, of the 16 columns' maxima, with the values' powers: 2^23 more, and so rounded to
+// whole numbers (below 0: halves).
+template <int FACTORS>
+__device__ __forceinline__ float top_score(const float (&lower)[4], const float (&upper)[4], const float (&f)[FACTORS], const float (&e)[FACTORS]) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < FACTORS; ++i) {
+        float most;
+        if constexpr (FACTORS == 2) {
+            const float (&m)[4] = i ? upper : lower;
+            most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+        } else {
+            most = i < 4 ? lower[i & 3] : upper[i & 3];
+        }
+        top = fmaxf(top, fmaf(most, f[i], e[i]));
+    }
     return top;
+}
+// A row's sum, moved where `top`, which no score of a tile is above, has outgrown m.
+__device__ __forceinline__ void move_sum(float top, float& m, float& l) {
+    if (top > m + 10.f) {
+        const float m_new = ceilf(top);
+        l *= chunk_exp2(m - m_new);
+        m = m_new;
+    }
+}
+// M - m of a row, 0 where its scores overflow.
+__device__ __forceinline__ int power_between(float M, float m) { return M < INFINITY ? (int)fmaxf(M - m, -1e6f) : 0; }
+// A row's (m, l) with l in [1/2, 1): what it weighs is then no larger than the values, and log2 l is small.  Returns what m grew by.
+__device__ __forceinline__ int level(float& m, float& l) {
+    if (m == kNothing) m = -INFINITY;
+    const uint32_t e = __float_as_uint(l) >> 23;
+    if (e - 1u >= 254u) return 0;  // 0, or not a number
+    const int k = (int)e - 126;
+    m += (float)k;
+    l = __uint_as_float(__float_as_uint(l) - ((uint32_t)k << 23));
+    return k;
 }
 // The accumulator's columns of a warp's rows times alpha.
 template <int D>
@@ -671,7 +757,6 @@ template <int D>
 struct Shared : Common<D, false> {
     uint64_t q_ready[2], drain[2], turn[2];
     uint64_t s[2], half[2], p[2], o[2];              // of a stream: scores, a half of the weights, all of them, the accumulator
-    int row_ref[2][4];                               // of a split job's streams: what their accumulators are in units of
     __device__ void init() {
         for (int i = 0; i < 2; ++i) {
             mbar_init(&q_ready[i], 4);
@@ -702,12 +787,12 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
     const int G = p.group;
     if (!begin<D, false>(p, &kmap, &vmap, sh, smem, 2)) return;
     const uint32_t tmem = sh.tmem;
-    // Of a split job's streams, a row's maximum and sum: where the second query tile is otherwise, those of 32 rows where these rows'
+    // Of a split job's streams, a row's m, l and its accumulator's power: where the second query tile is otherwise, those of 32 rows where these rows'
     // queries are.  The two warps that have the rows write and read both, and their barriers are the only ones in between.
     constexpr int kRowsBytes = 32 * 128;  // of 32 rows of a query tile (its first part)
-    static_assert(2 * 32 * sizeof(float2) <= kRowsBytes && 4 * kRowsBytes <= S::q_bytes, "a warp's rows hold them");
-    auto row = [&](int stream, int r) -> float2& {
-        return reinterpret_cast<float2*>(smem + S::q_bytes + (r >> 5) * kRowsBytes)[stream * 32 + (r & 31)];
+    static_assert(2 * 32 * sizeof(float4) <= kRowsBytes && 4 * kRowsBytes <= S::q_bytes, "a warp's rows hold them");
+    auto row = [&](int stream, int r) -> float4& {
+        return reinterpret_cast<float4*>(smem + S::q_bytes + (r >> 5) * kRowsBytes)[stream * 32 + (r & 31)];
     };
     // whether a job's rows are one stream's: then both take them, and every other key tile
     auto is_split = [&](const Job& g) { return g.t * 2 * p.tokens + p.tokens >= g.B; };
@@ -742,7 +827,7 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
             const int hi = !active ? 0x7fffffff : p.causal ? max(0, pos + 1) : g->n;
             const int lo = active && p.window > 0 ? max(0, pos + 1 - p.window) : 0;
             const bool idle = !__any_sync(0xffffffffu, active);  // the same in both warps of these rows
-            float m = -INFINITY, l = 0.f, row_scale = 1.f;
+            float M = kNothing, m = kNothing, l = 0.f, row_scale = 1.f;
             if (j1 > j0 && b > a && !idle) {
                 // ---- the queries of this warp's rows, two parts each, to shared memory
                 const int64_t at = active ? (int64_t)(g->q0 + tok) * fp.q_stride + (g->h * G + r - my_tok * G) * D : -1;
@@ -764,7 +849,6 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
             }
             const int step = split ? 2 : 1, from_j = split ? a + i : a;  // (a split job's a is its j0)
             int from = lo - from_j * kKeys, to = hi - from_j * kKeys;    // columns that the row sees
-            int ref = 0;  // the largest power of two of the stream's values so far, biased (0: none yet)
 #pragma unroll 1
             for (int j = from_j; j < b; j += step, ++ns, from -= step * kKeys, to -= step * kKeys) {
                 failed = !__all_sync(0xffffffffu, mbar_wait(&sh.s[i], ns & 1, kWaitBudget));
@@ -772,49 +856,40 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                 tc_fence_after();
                 if (!idle) {
                     const bool full = __all_sync(0xffffffffu, from <= 0 && to >= kKeys);
-                    // the factors of the scores, of kKeys / FACTORS keys each; finite and above 0, so that a hidden column's
-                    // -inf stays one
                     const unsigned batch = (batch0 + batch_of(j - j0, box_shift)) % kBatches;
-                    float f[FACTORS];
-#pragma unroll
-                    for (int c = 0; c < FACTORS; ++c)
-                        f[c] = fmaxf(fminf(row_scale * power_of(sh.k_exp[batch][in_batch(j - j0, c * (kKeys / FACTORS) >> box_shift, box_shift)]), 3.4e38f), 1.2e-38f);
+                    const int boxes = in_batch(j - j0, 0, box_shift);
+                    float f[FACTORS], e[FACTORS];
+                    take_scales<FACTORS>(sh, batch, boxes, box_shift, row_scale, f, e);
                     uint32_t lower[4][16], upper[4][16];
                     float mx[2][4];
                     take_scores(s_addr, 0, full, from, to, lower, mx[0]);
                     take_scores(s_addr, 1, full, from, to, upper, mx[1]);
-                    const float top = top_score<FACTORS>(mx[0], mx[1], f);
-                    // (with this m, 2^(score - m) stays below 2^10)
-                    const bool grew = top > m + 10.f;
-                    const int tile_ref = sh.v_ref[batch][in_batch(j - j0, 0, box_shift)];
-                    if (__any_sync(0xffffffffu, grew) || tile_ref > ref) {
+                    float top = top_score<FACTORS>(mx[0], mx[1], f, e);
+                    const uint32_t low = sh.v_low[batch][boxes];
+                    move_sum(top - plus_2_23(low), m, l);
+                    top -= 8388608.f;
+                    // (with this M, P stays below 2^15)
+                    if (__any_sync(0xffffffffu, top > M + 10.f)) {
                         // (all of the warp's rows, those that need not too: their next move is later for it; a prompt of 8192
                         // with 2^8 490 us, 521 with each row moved for itself)
-                        const float m_old = m;
-                        m = fmaxf(m, top);
-                        float alpha = m > m_old ? chunk_exp2(m_old - m) : 1.f;
-                        l *= alpha;
+                        const float M_old = M;
+                        M = fmaxf(M, ceilf(top));
                         // (this tile's scores are complete, so the stream's MMAs before them, the last P V among them, are too)
-                        if (j > from_j) {
-                            if (tile_ref > ref) alpha *= power_of((uint32_t)max(127 + ref - tile_ref, 0));
-                            rescale<D>(lanes + kColO + i * D, alpha);
-                        }
-                        ref = max(ref, tile_ref);
+                        if (j > from_j) rescale<D>(lanes + kColO + i * D, M > M_old ? chunk_exp2(M_old - M) : 1.f);
                     }
-                    // weights 2^(f * score - m) times the values' power and 2^5, packed in pairs over the scores; their sum
-                    const int power = max(tile_ref - ref + 5, -60);
-                    const float negm = (m == -INFINITY ? 0.f : -m) + (float)power;
+                    // P in pairs over the scores, and its sum
+                    const float base = 5.f - 8388608.f - M;
                     uint64_t sum2[2] = {0ull, 0ull};
-                    weigh<FACTORS>(lower, f, 0, negm, sum2, s_addr);
+                    weigh<FACTORS, false>(lower, f, e, 0, base, low, sum2, s_addr);
                     // (their P V begins; a prompt of 8192, when this was built, 538 us without, 520 with)
                     tmem_st_wait();
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sh.half[i]);
-                    weigh<FACTORS>(upper, f, 1, negm, sum2, s_addr);
+                    weigh<FACTORS, false>(upper, f, e, 1, base, low, sum2, s_addr);
                     float u, w;
                     unpack_f32x2(add_f32x2(sum2[0], sum2[1]), u, w);
-                    l = fmaf(u + w, __uint_as_float((uint32_t)(127 - power) << 23), l);
+                    l = fmaf(u + w, chunk_exp2(M - m - 5.f - (float)low), l);
                     tmem_st_wait();
                 } else if (lane == 0) {
                     mbar_arrive(&sh.half[i]);
@@ -836,33 +911,34 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
             }
             batch0 += batches_of(max(0, j1 - j0), box_shift);
             if (!split && failed) continue;
-            // the weights of the streams' accumulators, which are in units of 2^(ref - 132)
-            float w_mine = some ? power_of((uint32_t)(ref - 5)) : 0.f, w_other = 0.f;
+            // the weights of the streams' accumulators, and their powers of two
+            float w_mine = some ? 1.f : 0.f, w_other = 0.f;
+            int unit_mine = power_between(M, m) - 132, unit_other = 0;
+            unit_mine -= level(m, l);
             bool others_some = false;
             if (split) {
                 // ---- the other stream's part of these rows, merged as the second kernel merges CTAs' parts
-                row(i, r) = make_float2(m, l);
-                if (lane == 0) sh.row_ref[i][quad] = some ? ref : 0;
+                row(i, r) = make_float4(m, l, __int_as_float(unit_mine), 0.f);
                 if (named_barrier_or(1 + quad, 64, failed)) {
                     failed = true;
                     continue;
                 }
                 others_some = a + (i ^ 1) < b;
-                const float2 o = row(i ^ 1, r);
+                const float4 o = row(i ^ 1, r);
                 const float top = fmaxf(m, o.x);
                 const float u = m == top ? 1.f : chunk_exp2(m - top), v = o.x == top ? 1.f : chunk_exp2(o.x - top);
                 l = i == 0 ? l * u + o.y * v : o.y * v + l * u;
                 m = top;
                 w_mine *= u;
-                if (others_some) w_other = v * power_of((uint32_t)(sh.row_ref[i ^ 1][quad] - 5));
+                if (others_some) w_other = v, unit_other = __float_as_int(o.z);
             }
             const bool first = g->first, whole = first && g->last;
             // the query row's number among all, in the output (-1: none)
             const long long orow = active ? (long long)(g->q0 + tok) * p.num_q_heads + g->h * G + r - my_tok * G : -1;
             had_job(sh, nj);
             const float inv = whole ? row_inverse(m, l) : 1.f;
-            w_mine *= inv;
-            w_other *= inv;
+            w_mine = ldexpf(w_mine * inv, unit_mine);
+            w_other = ldexpf(w_other * inv, unit_other);
             const size_t slot = (size_t)blockIdx.x * 2 + (first ? 1 : 0);
             if (!idle) {
                 // (a split job's two warps have half of the columns each)
@@ -1003,10 +1079,8 @@ struct BlockShared : Common<D, true> {
     uint64_t q_ready, drain, o;
     uint64_t s[3], p[3];                             // of a score buffer: scores, weights
     uint64_t decided[4][2];                          // of 32 rows, by the tile's parity: what follows is as after it
-    float top[kTileM];                               // of a row: its maximum so far
-    int ref[4];                                      // the values' power so far (the same in all of them)
-    float row[2][kTileM];                            // of the two groups of warps: at the end row sums (before that the second has
-                                                     // the size of a row's queries)
+    float top[kTileM];                               // of a row: M so far
+    uint32_t size[kTileM];                           // the bits of a row's largest query element
     __device__ void init() {
         mbar_init(&q_ready, 4);
         mbar_init(&drain, 1);
@@ -1041,6 +1115,11 @@ block_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
     const int G = p.group;
     if (!begin<D, true>(p, &kmap, &vmap, sh, smem, 1)) return;
     const uint32_t tmem = sh.tmem;
+    // At a job's end a row's m and l, of the two groups of warps: where its queries were (the job's MMAs are done; the two warps
+    // that have 32 rows read both before one of them brings the next queries there).
+    constexpr int kRowsBytes = 32 * 128;
+    static_assert(2 * 32 * sizeof(float2) <= kRowsBytes && 4 * kRowsBytes <= S::q_bytes, "a warp's rows hold them");
+    auto row = [&](int group, int r) -> float2& { return reinterpret_cast<float2*>(smem + (r >> 5) * kRowsBytes)[group * 32 + (r & 31)]; };
 
     if (warp < kSoftmaxWarps) {
         regs_inc<kBlockRegs.softmax>();
@@ -1070,19 +1149,18 @@ block_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
             const int hi = !active ? 0x7fffffff : p.causal ? max(0, pos + 1) : g->n;
             const int lo = active && p.window > 0 ? max(0, pos + 1 - p.window) : 0;
             const bool idle = !__any_sync(0xffffffffu, active);  // the same in both warps of these rows
-            float m = -INFINITY, l = 0.f, row_scale = 1.f;
+            float M = kNothing, m = kNothing, l = 0.f, row_scale = 1.f;  // (m and l of this group's tiles)
             if (tiles > 0) {
                 if (!idle) {
-                    // ---- the queries of these rows, two parts each, to shared memory; the other group learns of their size,
-                    // where it writes its sums itself later (this group's may be there before it has read that)
+                    // ---- the queries of these rows, two parts each, to shared memory; the other group learns of their size
                     uint32_t top = 0;
                     if (i == 0) {
                         const int64_t at = active ? (int64_t)(g->q0 + tok) * fp.q_stride + (g->h * G + r - my_tok * G) * D : -1;
                         top = split_queries<D>(fp.q, at, smem + quad * 32 * 128);
-                        sh.row[1][r] = __uint_as_float(top);
+                        sh.size[r] = top;
                     }
                     named_barrier(1 + quad, 64);
-                    if (i == 1) top = __float_as_uint(sh.row[1][r]);
+                    if (i == 1) top = sh.size[r];
                     // the row times 2^(7 - e) is below 256; 2^(e - 7) of it is put back with the softmax's scale
                     row_scale = p.scale_log2 * __uint_as_float((max(top >> 7, 8u) - 7) << 23);
                     if (top >= 0x7f80u && hi > lo) l = __uint_as_float(0x7fc00000u);  // a NaN or an infinity: the row is none
@@ -1094,7 +1172,6 @@ block_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                 }
             }
             int from = lo - (j0 + i) * kKeys, to = hi - (j0 + i) * kKeys;  // columns that the row sees
-            int ref = 0;  // the largest power of two of the values so far, biased (0: none yet)
 #pragma unroll 1
             for (int t = i; t < tiles; t += 2, from -= 2 * kKeys, to -= 2 * kKeys) {
                 const unsigned x = x0 + t;
@@ -1104,57 +1181,47 @@ block_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                 tc_fence_after();
                 if (!idle) {
                     const bool full = __all_sync(0xffffffffu, from <= 0 && to >= kKeys);
-                    // the factors of the scores, of kKeys / FACTORS keys each; finite and above 0, so that a hidden column's
-                    // -inf stays one
                     const unsigned batch = (batch0 + batch_of(t, box_shift)) % kBatches;
-                    float f[FACTORS];
-#pragma unroll
-                    for (int c = 0; c < FACTORS; ++c)
-                        f[c] = fmaxf(fminf(row_scale * power_of(sh.k_exp[batch][in_batch(t, c * (kKeys / FACTORS) >> box_shift, box_shift)]), 3.4e38f), 1.2e-38f);
+                    const int boxes = in_batch(t, 0, box_shift);
+                    float f[FACTORS], e[FACTORS];
+                    take_scales<FACTORS>(sh, batch, boxes, box_shift, row_scale, f, e);
                     uint32_t lower[4][16], upper[4][16];
                     float mx[2][4];
                     take_scores(s_addr, 0, full, from, to, lower, mx[0]);
                     take_scores(s_addr, 1, full, from, to, upper, mx[1]);
-                    const float top = top_score<FACTORS>(mx[0], mx[1], f);
-                    const int tile_ref = sh.v_ref[batch][in_batch(t, 0, box_shift)];
-                    // ---- (m, ref) as the tile before left them
-                    float m_old = -INFINITY;
-                    int ref_old = 0;
+                    const float top_low = top_score<FACTORS>(mx[0], mx[1], f, e), top = top_low - 8388608.f;
+                    // ---- M as the tile before left it
+                    float M_old = kNothing;
                     if (t > 0) {
                         failed = !__all_sync(0xffffffffu, mbar_wait(&sh.decided[quad][i ^ 1], (nd[i ^ 1] + ((t - 1) >> 1)) & 1, kWaitBudget));
                         if (failed) break;
-                        m_old = sh.top[r];
-                        ref_old = sh.ref[quad];
+                        M_old = sh.top[r];
                         __syncwarp();
                     }
-                    // (with this m, 2^(score - m) stays below 2^10)
-                    const float m_new = __any_sync(0xffffffffu, top > m_old + 10.f) ? fmaxf(m_old, top) : m_old;
-                    const bool grew = m_new > m_old;
-                    ref = max(ref_old, tile_ref);
-                    const bool moves = t > 0 && __any_sync(0xffffffffu, (grew && m_old != -INFINITY) || ref > ref_old);
-                    if (t == 0 || grew) sh.top[r] = m_new;
-                    if (lane == 0 && (t == 0 || ref > ref_old)) sh.ref[quad] = ref;
+                    // (with this M, P stays below 2^15)
+                    M = __any_sync(0xffffffffu, top > M_old + 10.f) ? fmaxf(M_old, ceilf(top)) : M_old;
+                    const bool grew = M > M_old;
+                    const bool moves = t > 0 && __any_sync(0xffffffffu, grew && M_old != kNothing);
+                    if (t == 0 || grew) sh.top[r] = M;
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sh.decided[quad][i]);
                     if (moves) {  // the accumulator with them, once the tile before is in it
                         failed = !__all_sync(0xffffffffu, mbar_wait(&sh.v_empty[(x - 1) % S::v_slots], ((x - 1) / S::v_slots) & 1, kWaitBudget));
                         if (failed) break;
                         tc_fence_after();
-                        rescale<D>(lanes + kColO, (grew ? chunk_exp2(m_old - m_new) : 1.f) * power_of((uint32_t)max(127 + ref_old - ref, 0)));
+                        rescale<D>(lanes + kColO, grew ? chunk_exp2(M_old - M) : 1.f);
                     }
-                    if (m != m_new) {
-                        l *= chunk_exp2(m - m_new);
-                        m = m_new;
-                    }
-                    // weights 2^(f * score - m) times the values' power and 2^5, over the scores; their sum
-                    const int power = max(tile_ref - ref + 5, -60);
-                    const float negm = (m == -INFINITY ? 0.f : -m) + (float)power;
+                    const uint32_t low = sh.v_low[batch][boxes];
+                    move_sum(top_low - plus_2_23(low), m, l);
+                    // P over the scores, and its sum
+                    const float base = 5.f - 8388608.f - M;
                     uint64_t sum2[2] = {0ull, 0ull};
-                    weigh<FACTORS>(lower, f, 0, negm, sum2, s_addr);
-                    weigh<FACTORS>(upper, f, 1, negm, sum2, s_addr);
+                    weigh<FACTORS, FACTORS == 2>(lower, f, e, 0, base, low, sum2, s_addr);
+                    weigh<FACTORS, FACTORS == 2>(upper, f, e, 1, base, low, sum2, s_addr);
                     float u, w;
                     unpack_f32x2(add_f32x2(sum2[0], sum2[1]), u, w);
-                    l = fmaf(u + w, __uint_as_float((uint32_t)(127 - power) << 23), l);
+                    // (M is of both groups' tiles and m of this one's: where they are that far apart, these weights are nothing)
+                    l = fmaf(u + w, chunk_exp2(fminf(M - m - 5.f - (float)low, 127.f)), l);
                     tmem_st_wait();
                 }
                 tc_fence_before();
@@ -1177,24 +1244,25 @@ block_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                 nd[0] += (tiles + 1) >> 1;
                 nd[1] += tiles >> 1;
             }
-            // ---- the sums of both groups' tiles, for the last tile's maximum; the accumulator is in units of 2^(ref - 132)
-            if (tiles > 0 && !idle) {
-                const float top = sh.top[r];
-                if (m != top) l *= chunk_exp2(m - top);
-                m = top;
-                ref = sh.ref[quad];
-            }
-            sh.row[i][r] = l;
+            // ---- the sums of both groups' tiles
+            if (tiles > 0 && !idle) M = sh.top[r];
+            row(i, r) = make_float2(m, l);
             if (named_barrier_or(1 + quad, 64, failed)) {
                 failed = true;
                 continue;
             }
-            l = sh.row[0][r] + sh.row[1][r];
+            {
+                const float2 x = row(0, r), y = row(1, r);
+                m = fmaxf(x.x, y.x);
+                l = x.y * (x.x == m ? 1.f : chunk_exp2(x.x - m)) + y.y * (y.x == m ? 1.f : chunk_exp2(y.x - m));
+            }
+            int unit = power_between(M, m) - 132;
+            unit -= level(m, l);
             const bool first = g->first, whole = first && g->last;
             // the query row's number among all, in the output (-1: none)
             const long long orow = active ? (long long)(g->q0 + tok) * p.num_q_heads + g->h * G + r - my_tok * G : -1;
             had_job(sh, nj);
-            const float weight = (tiles > 0 ? power_of((uint32_t)(ref - 5)) : 0.f) * (whole ? row_inverse(m, l) : 1.f);
+            const float weight = tiles > 0 ? ldexpf(whole ? row_inverse(m, l) : 1.f, unit) : 0.f;
             const size_t slot = (size_t)blockIdx.x * 2 + (first ? 1 : 0);
             if (!idle)  // (each group has half of the columns)
                 write_rows<D>(p, tiles > 0 ? lanes + kColO : 0, 0, weight, 0.f, i * (D / 2), (i + 1) * (D / 2), whole, orow, slot, r);
