@@ -249,7 +249,8 @@ BP_API int bp_chunk_attention_paged(const void* q, int64_t q_stride, const void*
  * Rows from cu_new[num_seqs] on are padding.  A page may belong to one sequence of the call.  workspace: at least 256 bytes.
  *
  * bp_chunk_attention_paged_fp8 is bp_chunk_attention_paged over such a cache: the same arguments, limits, masks, workspace
- * size and errors.  A weight times its value's scale is rounded to 11 bits, or by up to 2^-29 of the row's largest such
+ * size and errors.  Queries are held as two 4-bit parts with one power of two a row: exact from 2^-9 of the row's largest
+ * element on, off by up to 2^-16 of that below (and of 2^-119 in rows whose elements all are smaller).  A weight times its value's scale is rounded to 11 bits, or by up to 2^-29 of the row's largest such
  * product: of the keys that the row sees, so that hidden ones cost it nothing.  Values lose bits where their scale is more than
  * 2^75 below another one's of the sequence and head.  Scores are to be below 2^22 in size (fp32 has no fraction left for them
  * further on); a row with larger ones may be NaN.  A key or a value that is not a number makes the rows that see it NaN (whole,

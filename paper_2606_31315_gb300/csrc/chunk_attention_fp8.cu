@@ -4,8 +4,12 @@
 //   O_i = sum_j softmax_j(scale <q_i, 2^a k_j>) 2^b v_j      a, b: of key j's page
 //
 //   * S = Q K^T on the codes as they lie in memory, kind::f8f6f4.  A query row, scaled by a power of two to at most 256, is the
-//     sum of two e4m3 numbers: bf16's 8 bits are twice 4.  (Elements below 2^-9 of the row's largest lose what is under
-//     2^-16 of it.)  The row's and the page's powers multiply the scores in the softmax.
+//     sum of two e4m3 numbers: bf16's 8 bits are twice 4.  Elements below 2^-9 of the row's largest are off by up to 2^-16 of it:
+//     fewer bits than the caller's, and a choice.  A third part would be half as many MMAs again, on accumulators of its own
+//     that tensor memory has no room for (the parts' scales differ); K in fp16 would be V's conversion a second time.  The scores
+//     of Gaussian queries lose less than their own sum in fp32 does; those of a row with one element 256 times as large, where
+//     the keys are 0, as much as the queries' own rounding to bf16.  The row's and the page's powers multiply the scores in the
+//     softmax.
 //   * P V in fp16, which holds every e4m3 number; four warps turn a tile's codes into them, in shared memory.  The weights take
 //     the values' powers of two, and are rounded to 11 bits, or at 2^-29 of the row's largest.
 // The line of work and the merge are chunk_attention.cu's.  Two kernels: chunk_attention_fp8_kernel for any call, its two streams a
