@@ -281,7 +281,8 @@ BP_API int bp_chunk_attention_paged_fp8(const void* q, int64_t q_stride, const v
  *
  *   block_table  [num_seqs][pages_per_seq] int32, in/out: entries of pages taken are written, the others stay as they are
  *   free_pages   [num_pages] int32, in/out: the ids of free pages come first; num_free [1] int32, in/out: how many
- *   total_new    entries of positions [int32] and slots [int64], each of which may be NULL
+ *   total_new    entries of positions [int32] and slots [int64], each of which may be NULL (with total_new 0 one that is not
+ *            NULL is not written, and says that there is room for no new token)
  *   cu_new, cu_kv  [num_seqs+1] int32 out, may be NULL: prefix sums of the new tokens and of new_lens, as bp_kv_append,
  *            bp_qk_norm_rope (positions) and the attentions read them
  *   missing      [1] int32 out, may be NULL: 0, or how many pages there are too few.  Then nothing is changed: cu_new

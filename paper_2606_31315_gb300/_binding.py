@@ -540,7 +540,7 @@ def pages_update(block_table, old_lens, new_lens, free_pages, num_free, page_siz
 
     block_table int32 [S, pages_per_seq], old_lens / new_lens int32 [S], free_pages int32 [num_pages], num_free int32 [1] on
     the device; the table, the list and its length are updated in place.  total_new: how many new tokens positions (int32) and
-    slots (int64) have room for; None: neither is wanted.  Returns (positions, slots, cu_new, cu_kv, missing)."""
+    slots (int64) have room for (more new tokens are reported in `ws`, and nothing changes); None: neither is wanted.  Returns (positions, slots, cu_new, cu_kv, missing)."""
     lib = load()
     i32 = torch.int32  # (written out: a helper's loop over these took 1.5 us of a call's 10)
     if not (block_table.dtype is i32 and old_lens.dtype is i32 and new_lens.dtype is i32 and free_pages.dtype is i32 and
@@ -566,8 +566,9 @@ def pages_update(block_table, old_lens, new_lens, free_pages, num_free, page_siz
             slots = _empty(total_new, torch.int64, dev, stream)
         elif slots.dtype is not torch.int64 or slots.numel() != total_new or not (slots.is_cuda and slots.is_contiguous()):
             raise ValueError("slots must be a contiguous int64 CUDA tensor of total_new entries")
-        if total_new:  # (an empty tensor has no address)
-            pp, sp = positions.data_ptr(), slots.data_ptr()
+        # (an empty tensor has no address, and NULL says that they are not wanted: room for none is given with an address that
+        # nothing is written at)
+        pp, sp = (positions.data_ptr(), slots.data_ptr()) if total_new else (num_free.data_ptr(), None)
     if cu_new is None:
         cu_new = _empty(s + 1, i32, dev, stream)
     elif cu_new.dtype is not i32 or cu_new.numel() != s + 1 or not (cu_new.is_cuda and cu_new.is_contiguous()):
