@@ -15,7 +15,7 @@ def i32(x):
 @pytest.mark.parametrize("room", [0, 5, 6])
 def test_more_new_tokens_than_there_is_room_for(room):
     """Room for none is room too: 6 new tokens are one too many for 5, and six too many for 0, which is the default."""
-    table, free, count, ws = i32([[3, 9]]), i32([0, 1, 2, 4]), i32([4]), bp.workspace(256, "cuda")
+    table, free, count, ws = i32([[3, 9]]), i32([0, 1, 2, 4] + [0] * 6), i32([4]), bp.workspace(256, "cuda")
     keep = [x.clone() for x in (table, free, count)]
     got = bp.pages_update(table, i32([14]), i32([20]), free, count, 16, *([room] if room else []), ws=ws)
     fits = room == 6
@@ -30,7 +30,7 @@ def test_more_new_tokens_than_there_is_room_for(room):
 
 def test_no_new_tokens_and_no_room():
     """Sequences that shrink or stay need none."""
-    table, free, count, ws = i32([[3, 9], [1, 0]]), i32([2, 4, 0, 0]), i32([2]), bp.workspace(256, "cuda")
+    table, free, count, ws = i32([[3, 9], [1, 0]]), i32([2, 4] + [0] * 8), i32([2]), bp.workspace(256, "cuda")
     got = bp.pages_update(table, i32([20, 5]), i32([3, 5]), free, count, 16, ws=ws)
     assert bp.get_status(ws) == 0 and int(count) == 3 and free[:3].tolist() == [2, 4, 9]
     assert got[0].numel() == 0 and got[2].tolist() == [0, 0, 0] and got[3].tolist() == [0, 3, 8]
