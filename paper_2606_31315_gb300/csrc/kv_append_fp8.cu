@@ -108,7 +108,11 @@ __device__ __forceinline__ void append_unit(const AppendParams& p, const Unit& u
     }
     uint8_t* const to = p.a.cache[kv] + ((((int64_t)page << p.page_shift) * H) + head) * D;  // the page's first row
     uint8_t* const scale = p.a.scale[kv] + (int64_t)page * H + head;
-    const int was = off > 0 ? min((int)*scale, 254) : 0;
+    const int was = off > 0 ? *scale : 0;
+    if (was == 255) {  // (no power of two: the rows before are none that a scale could be found for)
+        if (t == 0) raise_error(p.a.err_word, kErrDeviceArg);
+        return;
+    }
 #pragma unroll
     for (int k = 0; k < kKept<T>; ++k)
         if (t + k * THREADS < n) top = kept[k].top(top);
