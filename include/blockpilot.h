@@ -247,7 +247,7 @@ BP_API int bp_chunk_attention_paged(const void* q, int64_t q_stride, const void*
  * Limits: head_dim a multiple of 16, page_size * (head_dim / 16)^2 < 2^32; 16-byte aligned pointers and strides;
  * num_kv_heads <= 65535.  A page that is to receive rows and has no place in the table or the pool sets BP_ERR_DEVICE_FLAG
  * and is not written, nor is a head of a page that held rows before at a scale of 255; so do rows before key 0.
- * Rows from cu_new[num_seqs] on are padding.  A page may belong to one sequence of the call.  workspace: at least 256 bytes.
+ * Rows before cu_new[0] and from cu_new[num_seqs] on are padding.  A page may belong to one sequence of the call.  workspace: at least 256 bytes.
  *
  * bp_chunk_attention_paged_fp8 is bp_chunk_attention_paged over such a cache: the same arguments, limits, masks, workspace
  * size and errors.  Queries are held as two 4-bit parts with one power of two a row: exact from 2^-9 of the row's largest

@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_fp8_kernel(const __g
         const int first = __ldg(a.cu_new + s), end = __ldg(a.cu_new + s + 1);
         const int len = __ldg(a.cu_kv + s + 1) - __ldg(a.cu_kv + s), pos = len - (end - first) + t - first;
         const int off = pos & ((1 << p.page_shift) - 1);
-        if (t < all && (t == first || off == 0))
+        if (t >= first && t < min(end, all) && (t == first || off == 0))
             units[atomicAdd(&count, 1)] = Unit{t, min((1 << p.page_shift) - off, min(end, all) - t), s, len >= end - first ? pos : -1};
     }
     __syncthreads();

@@ -59,3 +59,19 @@ def test_a_page_at_a_scale_of_255(new, page):
     assert bp.get_status(ws) == 6
     for m in "kv":
         same(c, m, *wanted[m])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("first", [1, 21, 150])
+def test_rows_before_the_first_sequence(dtype, page, first):
+    """Offsets that begin inside the rows, as for a part of a batch: the rows before are no one's, and those behind."""
+    ctxs, news = [200, 30, 5], [90, 1, 17]
+    c, k, v = make(ctxs, news, page, 42, first + sum(news) + 70, dtype)
+    wanted = {m: after(c, m, x, ctxs, news, first=first) for m, x in (("k", k), ("v", v))}
+    ws = bp.workspace(256, "cuda")
+    bp.kv_append_fp8(c["k"], c["k_scale"], c["v"], c["v_scale"], k, v, offsets(news, first),
+                     offsets([a + n for a, n in zip(ctxs, news)], 7), c["table"], page, ws=ws)
+    assert bp.get_status(ws) == 0
+    for m in "kv":
+        same(c, m, *wanted[m])
