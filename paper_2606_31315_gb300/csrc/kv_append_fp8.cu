@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_fp8_kernel(const __g
         const int len = __ldg(a.cu_kv + s + 1) - __ldg(a.cu_kv + s), pos = len - (end - first) + t - first;
         const int off = pos & ((1 << p.page_shift) - 1);
         if (t >= first && t < min(end, all) && (t == first || off == 0))
-            units[atomicAdd(&count, 1)] = Unit{t, min((1 << p.page_shift) - off, min(end, all) - t), s, len >= end - first ? pos : -1};
+            units[atomicAdd(&count, 1)] = Unit{t, min((1 << p.page_shift) - off, min(end, all) - t), s, pos};  // (below 0: before key 0)
     }
     __syncthreads();
     const int n = count;  // (their order is that of arrival: each is by itself)

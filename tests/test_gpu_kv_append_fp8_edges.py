@@ -75,3 +75,22 @@ def test_rows_before_the_first_sequence(dtype, page, first):
     assert bp.get_status(ws) == 0
     for m in "kv":
         same(c, m, *wanted[m])
+
+
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("keys", [0, 1, 16, 50, 99])
+def test_fewer_keys_than_new_rows(page, keys):
+    """The rows before key 0 are reported and not written; the others are, as the attention reads them."""
+    news, lens = [100, 6], [keys, 20]
+    c, k, v = make([0, 14], [100, 6], page, 43)
+    wanted = {}
+    for m, x in (("k", k), ("v", v)):
+        ref = Append(c[m].view(torch.uint8).cpu().numpy(), c[m + "_scale"].cpu().numpy(), page)
+        ref(x[100 - keys:100].float().cpu().numpy(), 0, c["table"][0].cpu().numpy())
+        ref(x[100:].float().cpu().numpy(), 14, c["table"][1].cpu().numpy())
+        wanted[m] = (ref.codes, ref.scale)
+    ws = bp.workspace(256, "cuda")
+    bp.kv_append_fp8(c["k"], c["k_scale"], c["v"], c["v_scale"], k, v, offsets(news), offsets(lens), c["table"], page, ws=ws)
+    assert bp.get_status(ws) == 6
+    for m in "kv":
+        same(c, m, *wanted[m])
