@@ -245,7 +245,7 @@ BP_API int bp_chunk_attention_paged(const void* q, int64_t q_stride, const void*
  * a page begun: they are not keys.  (After a rollback into a page its scale stays as the dropped rows left it.)
  *   k_new, v_new  rows of [num_kv_heads][head_dim] dtype (bf16 or fp32), *_stride elements from a token to the next
  * Limits: head_dim a multiple of 16, page_size * (head_dim / 16)^2 < 2^32; 16-byte aligned pointers and strides;
- * num_kv_heads <= 65535.  A page that is to receive rows and has no place in the table or the pool sets BP_ERR_DEVICE_FLAG
+ * num_kv_heads <= 65535, total_new <= 2^30.  A page that is to receive rows and has no place in the table or the pool sets BP_ERR_DEVICE_FLAG
  * and is not written, nor is a head of a page that held rows before at a scale of 255; so do rows before key 0.
  * Rows before cu_new[0] and from cu_new[num_seqs] on are padding.  A page may belong to one sequence of the call.  workspace: at least 256 bytes.
  *

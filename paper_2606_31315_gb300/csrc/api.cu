@@ -324,7 +324,7 @@ int bp_kv_append_fp8(void* k_cache, void* k_scale, void* v_cache, void* v_scale,
     if (dtype != BP_F32 && dtype != BP_BF16) return BP_ERR_INVALID_ARG;
     const int64_t row = (int64_t)num_kv_heads * head_dim, step = dtype == BP_BF16 ? 8 : 4;
     if (k_stride < row || v_stride < row) return BP_ERR_INVALID_ARG;
-    if (head_dim % 16 != 0 || num_kv_heads > 65535) return BP_ERR_UNSUPPORTED;
+    if (head_dim % 16 != 0 || num_kv_heads > 65535 || total_new > 1 << 30) return BP_ERR_UNSUPPORTED;
     const long long pieces = head_dim / 16;  // (the kernel divides the numbers of a page's pieces by them in 32 bits)
     if (pieces >= 1 << 16 || pieces * pieces * page_size >= 1ll << 32) return BP_ERR_UNSUPPORTED;
     if (!aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) ||
