@@ -215,10 +215,26 @@ __global__ void __launch_bounds__(THREADS) pages_update_kernel(const __grid_cons
     if (writes) {
         if (a.cu_new)
             for (int s = tid; s <= n; s += THREADS) a.cu_new[s] = done ? tokens[s] : 0;
-        if (a.cu_kv && tid == 0) {
-            a.cu_kv[0] = 0;
-            if (!done)  // the lengths stay (rare: by one thread)
-                for (int s = 0, sum = 0; s < n; ++s) a.cu_kv[s + 1] = sum += max(0, __ldg(a.old_lens + s));
+        if (a.cu_kv && tid == 0) a.cu_kv[0] = 0;
+        if (a.cu_kv && !done) {  // the lengths stay: their prefix sums (1024 sequences 4.7 us a call, 12.2 by one thread)
+            for (int base = 0, before = 0; base < n; base += THREADS) {
+                const int s = base + tid;
+                int sum = s < n ? max(0, __ldg(a.old_lens + s)) : 0;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int y = __shfl_up_sync(0xffffffffu, sum, o);
+                    if (lane >= o) sum += y;
+                }
+                if (lane == 31) warp_sums[0][warp] = sum;
+                __syncthreads();
+                sum += before;
+                for (int w = 0; w < kWarps; ++w) {
+                    if (w < warp) sum += warp_sums[0][w];
+                    before += warp_sums[0][w];
+                }
+                if (s < n) a.cu_kv[s + 1] = sum;
+                __syncthreads();
+            }
         }
         if (a.missing && tid == 0) *a.missing = missing;
     }
