@@ -169,3 +169,24 @@ def test_large_scores(new, dim, power, sign):
     # (a product of three fp32 numbers, one of them rounded before)
     score = sign * 2.0 ** power * (448.0 if sign > 0 else 1.0) * dim ** -0.5
     assert ((lse.double() - score).abs() <= 2.0 ** -21 * abs(score) + 2.0 ** -20).all()
+
+
+@pytest.mark.parametrize("new", [1, 31, 200])
+@pytest.mark.parametrize("page", [16, 128])
+@pytest.mark.parametrize("exps", [3, 40])
+def test_long_contexts_cut_and_merged(new, page, exps):
+    """Parts of a row from several CTAs, each with powers of its own."""
+    c, q, lens = make([9000, 4000], [new, new], 2, 128, page, 27, exps)
+    check(c, q, [new, new], lens)
+    check(c, q, [new, new], lens, window=3000)
+
+
+@pytest.mark.parametrize("new", [1, 24, 100])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("exponent,power", [(0, 115), (1, 114), (254, -130), (250, -126)])
+def test_the_ends_of_the_keys_scales(new, page, exponent, power):
+    """Keys of 2^(exponent - 127) times a code, queries of 2^power: scores of an ordinary size."""
+    c, q, lens = make([300], [new], 2, 64, page, 28)
+    c["k_scale"].fill_(exponent)
+    q = torch.ldexp(q.double().cpu(), torch.tensor(power)).to(torch.bfloat16).cuda()
+    check(c, q, [new], lens)
