@@ -16,15 +16,16 @@
 // query tile each (where a work tile has the rows of one only, both take them, and every other key tile, and add what they
 // have at the end), and block_attention_fp8_kernel for calls whose work tiles all are such: blocks and single tokens.
 //
-// What bounds them (32 query and 8 KV heads of 128; times with a cold L2; floors at 6.75 TB/s and 1.93 PFLOP/s):
-//   * a prompt of 8192, 448 us of 285: a stream's chain from tile to tile, softmax 1,700 to 2,000 cycles (scores out of tensor
-//     memory 450, maximum 200, weights 900 to 1,100), the turn's 16 MMAs 1,200 and the hand-overs; two streams in turn take
-//     2,900 a pair of key tiles, 2,048 of them MMAs (which read shared memory at its full rate: 128 bytes a cycle).  A job
-//     change is 17,000 cycles, half of it the queries' way in, and heads whose maxima keep growing take 3,150 a pair, which the
-//     plan does not know.  (A bf16 cache: 369 us.)
-//   * 8 blocks of 31 over 32768 keys, 142 us of 80 (3.8 TB/s): the conversion's steps one after the other, and the job changes;
-//     a plain read of the same rows of 128 bytes takes 94 to 106.  (A bf16 cache: 236 us, 217 with bp_block_attention_paged.)
-//   * one token over 2048 keys, 15 us in a graph: the plan, two copies, a tile, the merge, one after the other.
+// What bounds them (32 query and 8 KV heads of 128, pages of 64; floors at 6.75 TB/s and 1.93 PFLOP/s).  Times in this file are of single
+// calls, events around each, L2 flushed before: some 8 us more than the kernels alone.
+//   * a prompt of 8192, 446 us of 285: a stream's chain from tile to tile (scores out of tensor memory, maximum, weights, the turn's
+//     16 MMAs and the hand-overs); two streams in turn take 2,840 cycles a pair of key tiles, 2,048 of them MMAs (which read shared
+//     memory at its full rate: 128 bytes a cycle).  A job change is 18,000 cycles, half of it the queries' way in, and heads whose
+//     maxima keep growing take up to 3,300 a pair, which the plan does not know.  (A bf16 cache: 369 us.)
+//   * 8 blocks of 31 over 32768 keys, 139 to 144 us of 80 (3.9 TB/s): the conversion's steps one after the other, and the job
+//     changes; a plain read of the same rows of 128 bytes takes 94 to 106.  (A bf16 cache: 236 us, 217 with
+//     bp_block_attention_paged.)
+//   * one token over 2048 keys, 21 us: the plan, two copies, a tile, the merge, one after the other.
 //
 // Roles: warps 0-3 and 4-7 softmax of stream 0 and 1 (a thread a row; they read and split the queries too), warp 8 lays out
 // the jobs and issues K's TMA copies, 9 and 10 issue the streams' MMAs, 11 V's copies and what the merge has to know, 12-15
@@ -36,8 +37,12 @@
 
 namespace bp {
 namespace {
-// A work tile's fixed cost (queries in, output out), in keys: a prompt of 8192 takes 502 us with 600, 451 with 800, 447 with
-// 1000 (decoding batches the same with all three).
+// A work tile's fixed cost (queries in, output out), in keys.  One number for all calls; us with a cold L2 at 400, 700, 1000, 1400:
+//   a prompt of 8192                       535  466  446  455    the same, heads of 64                   408  368  376  384
+//   16 and 32 chunks among single tokens   139  130  125  133    (pages of 64)                           171  148  142  142
+//   16 x 100 tokens over 1000 keys          76   73   72   71    8 x 300 to 1000 tokens, heads of 64      98  100   99  101
+//   4 x 2001 in a window, heads of 64       56   58   56   58    8 x 64 over 4096                         62   61   60   65
+// Blocks and single tokens, 8 x 31 over 32768 to 64 x 1 over 4096: within 3 % with all four.
 constexpr int kTileCost = 1000;
 }  // namespace
 }  // namespace bp
@@ -102,8 +107,8 @@ struct Common {
     uint64_t k_full[S::k_slots], k_empty[S::k_slots], raw_full[S::raw_slots], raw_empty[S::raw_slots];
     uint64_t v_full[S::v_slots], v_empty[S::v_slots];
     uint64_t job_full[kJobs], job_empty[kJobs];
-    // The scales of the boxes (Boxes), 32 at a time: of keys, bf16 numbers; of values biased exponents, what the weights take of theirs, the least
-    // of that in the box's tile, and what is left for the values themselves.
+    // The scales of the boxes (Boxes), 32 at a time: of keys, bf16 numbers; of values, biased exponents, what the weights take of
+    // them, the least of that in the box's tile, and what is left for the values themselves.
     alignas(16) uint16_t k_power[kBatches][32];
     alignas(8) uint8_t v_exp[kBatches][32], v_low[kBatches][32], v_below[kBatches][32];
     Job job[kJobs];
@@ -791,8 +796,9 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
     const int G = p.group;
     if (!begin<D, false>(p, &kmap, &vmap, sh, smem, 2)) return;
     const uint32_t tmem = sh.tmem;
-    // Of a split job's streams, a row's m, l and its accumulator's power: where the second query tile is otherwise, those of 32 rows where these rows'
-    // queries are.  The two warps that have the rows write and read both, and their barriers are the only ones in between.
+    // Of a split job's streams, a row's m, l and its accumulator's power: where the second query tile is otherwise, those of 32 rows
+    // where these rows' queries are.  The two warps that have the rows write and read both, and their barriers are the only ones in
+    // between.
     constexpr int kRowsBytes = 32 * 128;  // of 32 rows of a query tile (its first part)
     static_assert(2 * 32 * sizeof(float4) <= kRowsBytes && 4 * kRowsBytes <= S::q_bytes, "a warp's rows hold them");
     auto row = [&](int stream, int r) -> float4& {
@@ -872,7 +878,7 @@ chunk_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                     const uint32_t low = sh.v_low[batch][boxes];
                     move_sum(top - plus_2_23(low), m, l);
                     top -= 8388608.f;
-                    // (with this M, P stays below 2^15)
+                    // (with this M, P stays below 2^16)
                     if (__any_sync(0xffffffffu, top > M + 10.f)) {
                         // (all of the warp's rows, those that need not too: their next move is later for it; a prompt of 8192
                         // with 2^8 490 us, 521 with each row moved for itself)
@@ -1101,8 +1107,8 @@ constexpr int block_smem() { return whole_sm(Shape<D, true>::tiles + (int)sizeof
 static_assert(block_smem<128>() <= 227 * 1024 && block_smem<64>() <= 227 * 1024, "a block's shared memory");
 
 // The same where every work tile has the rows of one stream: blocks and single tokens, whose keys' bytes are what counts.
-// Against the kernel above, us with a cold L2: 32 x 1 token over 8192 keys in pages of 16 138 (154), 64 x 1 over 4096 142 (158),
-// 8 x 16 over 32768 132 (135), 32 x 16 over 2048 74 (79); 8 x 31 over 32768 142 (142), 1 x 31 51 (50).  One
+// Against the kernel above, us with a cold L2: 32 x 1 token over 8192 keys in pages of 16 151 (173), 64 x 1 over 4096 140 (164),
+// 32 x 16 over 2048 81 (85), 8 x 16 over 32768 129 (131); 8 x 31 over 32768 139 (138), 1 x 31 52 (50).  One
 // accumulator; scores in three buffers, so that a tile's are there before the softmax has done with the two before it.  The
 // softmax's two groups of warps take the tiles in turn, each row's maximum handed from one tile's thread to the next one's
 // (rarely another: it is moved only where a score has outgrown it by 2^10, and the accumulator with it).
@@ -1202,7 +1208,7 @@ block_attention_fp8_kernel(const __grid_constant__ Fp8Params fp, const __grid_co
                         M_old = sh.top[r];
                         __syncwarp();
                     }
-                    // (with this M, P stays below 2^15)
+                    // (with this M, P stays below 2^16)
                     M = __any_sync(0xffffffffu, top > M_old + 10.f) ? fmaxf(M_old, ceilf(top)) : M_old;
                     const bool grew = M > M_old;
                     const bool moves = t > 0 && __any_sync(0xffffffffu, grew && M_old != kNothing);

@@ -13,10 +13,13 @@
 // A page's new rows are a unit, which has one owner: nothing is summed or ordered by atomics.  A block has a few tokens of
 // one head of K or V; its threads look which of them begin a unit (a sequence's first new token, or a page's first row), then
 // units of many rows are the whole block's, others a warp's.  A thread keeps its rows' pieces in registers between the
-// maximum and the rounding, four of 16 elements (two of fp32); what is more (pages above 64 rows of 128) is read again, from L2.
+// maximum and the rounding, four of 16 elements (two of fp32); what is more (units above 64 rows of 128, 32 of fp32) is read
+// again, from L2.
 //
-// Bound by memory: bf16 in, a byte an element out.  In graphs, 8 KV heads of 128: 8192 tokens 11.6 us (50 MB, 4.4 TB/s: the
-// units' chain, look-up, loads, maximum, stores, once a block), 32 x 16 tokens 4.5, one token 2.4, a launch and three round trips.
+// Bound by memory: bf16 in, a byte an element out.  In graphs, 8 KV heads of 128: 8192 tokens 15.9 us over inputs in turn that L2
+// does not hold (50 MB, 3.2 TB/s), 11.7 over the same ones: the units' chain, look-up, loads, maximum, stores, once a block.  32 x 16
+// tokens 4.4, one token 2.3, a launch and three round trips.  Where the scale of a page that was begun before grows, its rows are
+// read, rounded and written too: 3.7 us more for 59 rows in each of 32 sequences, 3.9 for 63 in one.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -219,7 +222,8 @@ int launch_kv_append_fp8(const KvAppendFp8Args& a, cudaStream_t stream) {
     while ((1 << p.page_shift) < a.page_size) ++p.page_shift;
     p.piece_inverse = (unsigned)(((1ull << 32) + a.head_dim / 16 - 1) / (a.head_dim / 16));
     // as many tokens a block as a sequence brings, so that neither units wait for one another nor blocks find none (us in graphs,
-    // against always 4 and always 64: 32 sequences of 16 tokens 4.5, 6.7, 10.4; 256 of 1 6.7, 6.6, 20.8; 1 of 8192 11.6, 35.7, 11.6)
+    // over the same inputs, against always 4 and always 64: 32 sequences of 16 tokens 4.5, 6.7, 10.4; 256 of 1 6.7, 6.6, 20.8; 1 of
+    // 8192 11.6, 35.7, 11.6)
     p.tokens = 4;
     while (p.tokens < std::min(kAppendTokens, a.page_size) && p.tokens * 2 * (long long)a.num_seqs <= a.total_new) p.tokens *= 2;
     cudaLaunchConfig_t cfg = {};
