@@ -245,17 +245,21 @@ BP_API int bp_chunk_attention_paged(const void* q, int64_t q_stride, const void*
  * a page begun: they are not keys.  (After a rollback into a page its scale stays as the dropped rows left it.)
  *   k_new, v_new  rows of [num_kv_heads][head_dim] dtype (bf16 or fp32), *_stride elements from a token to the next
  * Limits: head_dim a multiple of 16, page_size * (head_dim / 16)^2 < 2^32; 16-byte aligned pointers and strides;
- * num_kv_heads <= 65535, total_new <= 2^30.  A page that is to receive rows and has no place in the table or the pool sets BP_ERR_DEVICE_FLAG
- * and is not written, nor is a head of a page that held rows before at a scale of 255; so do rows before key 0.
- * Rows before cu_new[0] and from cu_new[num_seqs] on are padding.  A page may belong to one sequence of the call.  workspace: at least 256 bytes.
+ * num_kv_heads <= 65535, total_new <= 2^30.  A page that is to receive rows and has no place in the table or the pool sets
+ * BP_ERR_DEVICE_FLAG and is not written, nor are a head of a page that held rows before at a scale of 255 and rows before key 0.
+ * Rows before cu_new[0] and from cu_new[num_seqs] on are padding.  A page may belong to one sequence of the call.  workspace: at
+ * least 256 bytes.
  *
  * bp_chunk_attention_paged_fp8 is bp_chunk_attention_paged over such a cache: the same arguments, limits, masks, workspace
- * size and errors.  Queries are held as two 4-bit parts with one power of two a row: exact from 2^-9 of the row's largest
- * element on, off by up to 2^-16 of that below (and of 2^-119 in rows whose elements all are smaller).  A weight times its value's scale is rounded to 11 bits, or by up to 2^-29 of the row's largest such
- * product: of the keys that the row sees, so that hidden ones cost it nothing.  Values lose bits where their scale is more than
- * 2^75 below another one's of the sequence and head.  Scores are to be below 2^22 in size (fp32 has no fraction left for them
- * further on); a row with larger ones may be NaN.  A key or a value that is not a number makes the rows that see it NaN (whole,
- * with their lse), and no others.  A scale of 255 sets BP_ERR_DEVICE_FLAG.
+ * size and errors.  What it rounds beside a score's sum in fp32 and the output:
+ *   queries are held as two 4-bit parts with one power of two a row: exact from 2^-9 of the row's largest element on, off by up to
+ *   2^-16 of that below (and of 2^-119 in rows whose elements all are smaller);
+ *   a weight times its value's scale is rounded to 11 bits, or by up to 2^-29 of the row's largest such product: of the keys that
+ *   the row sees, so that hidden ones cost it nothing;
+ *   values lose bits where their scale is more than 2^75 below another one's of the sequence and head.
+ * Scores are to be below 2^22 in size (fp32 has no fraction left for them further on); a row with larger ones may be NaN.  A key or
+ * a value that is not a number makes the rows that see it NaN (whole, with their lse), and no others.  A scale of 255 sets
+ * BP_ERR_DEVICE_FLAG.
  * ------------------------------------------------------------------------------- */
 BP_API int bp_kv_append_fp8(void* k_cache, void* k_scale, void* v_cache, void* v_scale, const void* k_new, int64_t k_stride,
                             const void* v_new, int64_t v_stride, const int32_t* cu_new, const int32_t* cu_kv,

@@ -681,7 +681,8 @@ __device__ __forceinline__ void take_scores(uint32_t at, int h, bool full, int f
 // The factors of a tile's scores and the values' powers, of kKeys / FACTORS keys each; the tile's boxes begin at place `at` of the
 // batch.  Factors are finite and above 0, so that a hidden column's -inf stays one.
 template <int FACTORS, class Sh>
-__device__ __forceinline__ void take_scales(const Sh& sh, unsigned batch, int at, int box_shift, float row_scale, float (&f)[FACTORS], float (&e)[FACTORS]) {
+__device__ __forceinline__ void take_scales(const Sh& sh, unsigned batch, int at, int box_shift, float row_scale, float (&f)[FACTORS],
+                                            float (&e)[FACTORS]) {
     auto factor = [&](uint32_t power) { return fmaxf(fminf(row_scale * __uint_as_float(power), 3.4e38f), 1.2e-38f); };
     if constexpr (FACTORS == 8) {  // pages of 16 or 32: of their 8 or 4 boxes at once
         uint32_t k[4], v[2];
@@ -692,7 +693,8 @@ __device__ __forceinline__ void take_scales(const Sh& sh, unsigned batch, int at
         } else {
             const uint2 a = *reinterpret_cast<const uint2*>(&sh.k_power[batch][at]);
             const uint32_t b = *reinterpret_cast<const uint32_t*>(&sh.v_exp[batch][at]);
-            k[0] = __byte_perm(a.x, 0, 0x1010), k[1] = __byte_perm(a.x, 0, 0x3232), k[2] = __byte_perm(a.y, 0, 0x1010), k[3] = __byte_perm(a.y, 0, 0x3232);
+            k[0] = __byte_perm(a.x, 0, 0x1010), k[1] = __byte_perm(a.x, 0, 0x3232);
+            k[2] = __byte_perm(a.y, 0, 0x1010), k[3] = __byte_perm(a.y, 0, 0x3232);
             v[0] = __byte_perm(b, 0, 0x1100), v[1] = __byte_perm(b, 0, 0x3322);
         }
 #pragma unroll
@@ -712,7 +714,8 @@ __device__ __forceinline__ void take_scales(const Sh& sh, unsigned batch, int at
 // The largest of a row's scores times their factors, of the 16 columns' maxima, with the values' powers: 2^23 more, and so rounded to
 // whole numbers (below 0: halves).
 template <int FACTORS>
-__device__ __forceinline__ float top_score(const float (&lower)[4], const float (&upper)[4], const float (&f)[FACTORS], const float (&e)[FACTORS]) {
+__device__ __forceinline__ float top_score(const float (&lower)[4], const float (&upper)[4], const float (&f)[FACTORS],
+                                           const float (&e)[FACTORS]) {
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < FACTORS; ++i) {
