@@ -256,7 +256,7 @@ BP_API int bp_chunk_attention_paged(const void* q, int64_t q_stride, const void*
  *   2^-16 of that below (and of 2^-119 in rows whose elements all are smaller);
  *   a weight times its value's scale is rounded to 11 bits, or by up to 2^-29 of the row's largest such product: of the keys that
  *   the row sees, so that hidden ones cost it nothing;
- *   values lose bits where their scale is more than 2^75 below another one's of the sequence and head.
+ *   values lose bits where their scale is more than 2^75 below another one's of the sequence and head, and are 0 from 2^85 on.
  * Scores are to be below 2^22 in size (fp32 has no fraction left for them further on); a row with larger ones may be NaN.  A key or
  * a value that is not a number makes the rows that see it NaN (whole, with their lse), and no others.  A scale of 255 sets
  * BP_ERR_DEVICE_FLAG.

@@ -24,8 +24,9 @@ def exponents(c, s, n):
 def allowance(c, q, news, lens, causal, window):
     """What a row may be off by beyond `attention`'s bound, whose 11 bits of a weight fp16 has down to its least step: a weight times
     its page's scale is off by 2^-29 of the row's largest such product at most (2^-25, half of fp16's least step, where the
-    largest is 2^4 at least), for each key that the row sees, times a code of at most 448; and a value by 2^-25 of 2^-60 of the sequence's
-    largest scale.  [tokens, heads]"""
+    largest is 2^4 at least), for each key that the row sees, times a code of at most 448; and a value by 448 2^-25 of 2^-60 of the
+    sequence's largest scale (what its scale is below that is multiplied into it in fp16: off by 2^-25 down to 2^-24, and 0 from 2^-25 on,
+    which fp16 does not have).  [tokens, heads]"""
     hkv, out, first = c["k"].shape[1], torch.zeros(q.shape[:2], dtype=torch.float64, device="cuda"), 0
     for s, (b, n) in enumerate(zip(news, lens)):
         k, e = keys_of(c, "k", s, n).nan_to_num(), exponents(c, s, n)
@@ -37,7 +38,7 @@ def allowance(c, q, news, lens, causal, window):
             kv = h // (q.shape[1] // hkv)
             x = torch.where(seen, q[first:first + b, h].double() @ k[:, kv].T * q.shape[2] ** -0.5, -math.inf)
             products = torch.softmax(x, 1) * torch.pow(2.0, e[:, kv])
-            out[first:first + b, h] = n * 2.0 ** -29 * 448 * products.amax(1) + 2.0 ** -85 * torch.pow(2.0, e[:, kv].max())
+            out[first:first + b, h] = n * 2.0 ** -29 * 448 * products.amax(1) + 448 * 2.0 ** -85 * torch.pow(2.0, e[:, kv].max())
         first += b
     return out
 
